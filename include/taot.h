@@ -254,6 +254,137 @@ taot_status taot_round_schedule(const int32_t* n, const int64_t* spill, const in
                                 uint32_t* status, void* ws, size_t ws_bytes, void* stream);
 
 /* ------------------------------------------------------------------------ */
+/* Around the planner: what makes the routing ids, and what carries a plan out
+ * on the tokens.  The calls below take rows of floating values of one of three
+ * types; rows may begin at any address that the type allows.  Sums, scores,
+ * norms and statistics are in 32 bits and each output is rounded once. */
+typedef enum {
+  TAOT_BF16 = 0,
+  TAOT_F16 = 1,
+  TAOT_F32 = 2,
+} taot_dtype;
+
+#define TAOT_MAX_WIDTH 32768      /* columns of a row of the norm                */
+#define TAOT_MAX_TOP_K 64         /* experts chosen per token                    */
+#define TAOT_MAX_ROUTE_GROUPS 256 /* groups of experts                           */
+
+/* Residual addition and root-mean-square norm, with an 8-bit output.
+ *   h = x + residual,  s = 1 / sqrt(mean_c h^2 + eps),  y = h * s * weight
+ *   x        [T][H] dtype    residual [T][H] dtype, nullable (h = x)
+ *   weight   [H]    weight_dtype: dtype or TAOT_F32
+ *   eps      >= 0, finite
+ *   group    columns that share a scale: a power of two from 8 to 512 (the last
+ *            group of a row may be short), or 0: one scale a row
+ * Outputs (each nullable; q and scale together):
+ *   h        [T][H] dtype    the sum, rounded where it is stored only
+ *   y        [T][H] dtype
+ *   q        [T][H] 8 bits   e4m3 of y / scale, to nearest even
+ *   scale    [T][ceil(H / group)] float (or [T]): max |y| of the group / 448
+ *            (of at least 1e-30, so that a group of zeros has q = 0); a group
+ *            with an infinity has scale infinity, and NaN where y is infinite;
+ *            a NaN is NaN in q and does not enter the maximum
+ *   rstd     [T]    float    s, for the gradient
+ * x and residual may be h or y's own storage only if the pointers are equal.
+ * Limits: 1 <= H <= TAOT_MAX_WIDTH, 0 <= T <= 2^31 - 1. */
+taot_status taot_add_rms_norm(const void* x, const void* residual, const void* weight, int64_t T, int32_t H,
+                              int32_t dtype, int32_t weight_dtype, float eps, int32_t group, void* h, void* y,
+                              void* q, float* scale, float* rstd, void* stream);
+/* Its gradient (the rounding to 8 bits counts as the identity):
+ *   dx = dh + s * (g - h * s^2 * mean_c(g * h)) with g = dy * weight,
+ *   dweight = sum_t dy * h * s
+ *   dy, h    [T][H] dtype    dh [T][H] dtype, nullable: what reaches h itself
+ *   rstd     [T]    float
+ * Outputs: dx [T][H] dtype, the gradient of x and of the residual alike;
+ * dweight [H] float (zero where T = 0; the same bits on every run). */
+size_t taot_add_rms_norm_backward_workspace_size(int64_t T, int32_t H);
+taot_status taot_add_rms_norm_backward(const void* dy, const void* dh, const void* h, const float* rstd,
+                                       const void* weight, int64_t T, int32_t H, int32_t dtype,
+                                       int32_t weight_dtype, void* dx, float* dweight, void* ws, size_t ws_bytes,
+                                       void* stream);
+
+/* Routing flags. */
+#define TAOT_ROUTE_SIGMOID 0x1u   /* scores are sigmoid(x), not softmax(x)         */
+#define TAOT_ROUTE_RENORM 0x2u    /* weights of a token sum to `scale`             */
+#define TAOT_ROUTE_GROUP_TWO 0x4u /* a group counts as the sum of its two largest
+                                     keys, not as its largest                    */
+/* Routing of tokens to experts.  Score s_e = softmax_e(x) or sigmoid(x_e); key_e =
+ * s_e + bias_e, or x_e where there is no bias (the same order, without the
+ * score's rounding).  Experts fall into `groups` equal runs; those of the best
+ * `top_groups` stay, and the k largest keys among them are chosen, in
+ * descending order.  Equal keys or groups: the lower index first.
+ * Weights: scale * s_e; with RENORM scale * softmax over the chosen x, or
+ * scale * s_e / (sum of the chosen s + 1e-20) for the sigmoid.  The bias enters
+ * the choice only.
+ *   logits   [T][E] dtype    bias [E] float, nullable
+ * Outputs: ids [T][k] int32, weights [T][k] float.  As [B][R][tokens * k], ids
+ * are what taot_plan_loads takes.
+ * An expert whose logit or key is NaN or -infinity is not chosen (a logit of
+ * +infinity counts as the largest float); where a token has fewer than k
+ * others, its last ids are -1 with weight 0, which taot_plan_loads skips and
+ * counts.
+ * Limits: 1 <= k <= min(E, TAOT_MAX_TOP_K), E <= TAOT_MAX_EXPERTS, groups
+ * divides E, groups <= TAOT_MAX_ROUTE_GROUPS, 1 <= top_groups <= groups with
+ * at least k experts in them, 0 <= T <= 2^31 - 1. */
+taot_status taot_route(const void* logits, const float* bias, int64_t T, int32_t E, int32_t k, int32_t groups,
+                       int32_t top_groups, float scale, uint32_t flags, int32_t dtype, int32_t* ids, float* weights,
+                       void* stream);
+/* Its gradient by the logits, for the choice as it was made: dweights [T][k]
+ * float, logits [T][E], ids [T][k] (distinct within a token; -1: no gradient)
+ * -> dlogits [T][E] dtype, zero for experts that the weights do not depend on.
+ * flags and scale as in the call that chose (GROUP_TWO has no effect). */
+taot_status taot_route_backward(const float* dweights, const void* logits, const int32_t* ids, int64_t T, int32_t E,
+                                int32_t k, float scale, uint32_t flags, int32_t dtype, void* dlogits, void* stream);
+
+/* Where a schedule sends each routed copy.  Copy i of source rank r is the j-th
+ * occurrence of its expert e among the rank's ids.  The guest slots of e, in
+ * ascending slot order, take X[r][slot] occurrences each (a negative share
+ * counts as 0), e's home rank the rest.  The send buffer of a source rank holds
+ * its copies ordered by destination rank; within a rank by instance (its own
+ * experts ascending, then its guest slots); within an instance in the order of
+ * i.
+ *   ids      [B][rows][N] int32  routing ids of source ranks rank0 .. rank0 + rows - 1
+ *                             (one rank's own: rows = 1; all: rank0 = 0, rows = R)
+ *   home     [E] int32, slot_expert [B][R*K] int32, X [B][R][R*K] int32: as in and
+ *                             from taot_round_schedule (both may be null for K = 0)
+ * Outputs:
+ *   pos      [B][rows][N] int32  row of the send buffer; p < 0: the copy goes
+ *                             nowhere (its id is no expert, or is left to an expert
+ *                             whose home is no rank), and row ~p, behind all
+ *                             others, is the one it leaves empty
+ *   offsets  [B][rows][E+R*K+1] int32  first row of each instance, in send order;
+ *                             the last entry is the number of copies that go
+ *                             somewhere.  (Instances of experts whose home is no
+ *                             rank come last and are empty.)
+ *   sends    [B][rows][R] int32  copies that go to each rank
+ *   status   [B] uint32       TAOT_ST_BAD_ID, TAOT_ST_BAD_INPUT (home), nullable
+ * Limits: those of taot_plan_loads and taot_round_schedule, 0 <= rank0,
+ * rank0 + rows <= R. */
+size_t taot_dispatch_map_workspace_size(int32_t B, int32_t rows, int64_t N, int32_t R, int32_t E, int32_t K);
+taot_status taot_dispatch_map(const int32_t* ids, int32_t B, int32_t rows, int32_t rank0, int64_t N,
+                              const int32_t* home, int32_t R, int32_t E, int32_t K, const int32_t* slot_expert,
+                              const int32_t* X, int32_t* pos, int32_t* offsets, int32_t* sends, uint32_t* status,
+                              void* ws, size_t ws_bytes, void* stream);
+/* Rows of tokens into the send buffer: out[row][pos[i]] = x[row][i / k], row by
+ * row of `rows`, for N = tokens * k copies; a dropped copy's row is zero.  A row is
+ * row_bytes bytes of any type.  x_more / out_more: a second array that goes the same
+ * way (the scales of 8-bit rows), null with more_bytes = 0.
+ *   x [rows][tokens][row_bytes], pos [rows][tokens * k], out [rows][tokens * k][row_bytes]
+ * Its gradient is taot_combine_rows without weights. */
+taot_status taot_dispatch_rows(const void* x, int64_t row_bytes, const void* x_more, int64_t more_bytes,
+                               int64_t rows, int64_t tokens, int32_t k, const int32_t* pos, void* out,
+                               void* out_more, void* stream);
+/* The way back: out[row][t] = sum_j weights[row][t k + j] * y[row][pos[row][t k + j]];
+ * dropped copies add nothing, weights may be null (all 1).
+ *   y [rows][tokens * k][H] dtype, weights [rows][tokens * k] float, out [rows][tokens][H] dtype */
+taot_status taot_combine_rows(const void* y, const int32_t* pos, const float* weights, int64_t rows, int64_t tokens,
+                              int32_t k, int32_t H, int32_t dtype, void* out, void* stream);
+/* Its gradient: dy[row][pos[i]] = weights[i] * dout[i / k] (zero in a dropped copy's
+ * row), dweights[i] = <dout[i / k], y[pos[i]]> (0 for a dropped copy). */
+taot_status taot_combine_rows_backward(const void* dout, const void* y, const int32_t* pos, const float* weights,
+                                       int64_t rows, int64_t tokens, int32_t k, int32_t H, int32_t dtype, void* dy,
+                                       float* dweights, void* stream);
+
+/* ------------------------------------------------------------------------ */
 /* Host helper: topology-preference matrices from a cost matrix (Sec. A.3
  * topology preference B: 1 intra-node, w_inter < 1 inter-node, 0 for the home
  * rank; Sec. A.4 topology bonus).  With cmin the smallest off-diagonal cost:

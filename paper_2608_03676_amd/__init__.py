@@ -9,6 +9,12 @@ calls raise if the library is not built or a tensor is not on the GPU.
 Steps (paper Sec. 3.2 / Appendix A): plan_loads (expert-load histogram and
 marginals), sinkhorn_batched (Phase 1), round_schedule (Phases 2 and 3);
 plan_step chains them.
+
+Around them: add_rms_norm (residual addition, norm, 8-bit output) and route
+(logits to expert ids, which plan_loads reads, and weights) before; then
+dispatch_map (the schedule on the single copies), dispatch_rows and
+combine_rows (rows to the send buffer and back).  The *_backward calls are
+their gradients.
 """
 from __future__ import annotations
 
@@ -26,6 +32,7 @@ LIB_PATH = os.path.join(HERE, "libtaot.so")
 ST_BAD_ID, ST_BAD_INPUT, ST_ZERO_MASS, ST_UNFILLED, ST_STREAMED = 0x1, 0x2, 0x4, 0x8, 0x10
 SK_NO_COLCAP, SK_FORCE_STREAM, SK_NO_REGISTER, SK_WAVES_1, SK_DENSE, SK_LINEAR = 0x1, 0x2, 0x4, 0x8, 0x10, 0x20
 SCH_NO_TOPO, SCH_NO_FLOW, SCH_ROW_PRIORITY = 0x1, 0x2, 0x4  # Phase-2 ablations (round_schedule flags)
+ROUTE_SIGMOID, ROUTE_RENORM, ROUTE_GROUP_TWO = 0x1, 0x2, 0x4  # route flags
 STATUS_NAMES = {0: "ok", 1: "invalid argument", 2: "unsupported shape", 3: "workspace", 4: "launch"}
 
 _lib = None
@@ -61,6 +68,26 @@ def lib():
         L.taot_round_schedule_workspace_size.argtypes = [_I32, _I32, _I32, _I32]
         L.taot_round_schedule.restype = ctypes.c_int
         L.taot_round_schedule.argtypes = [_P] * 9 + [_I32] * 4 + [_F64, _I64, _U32] + [_P] * 6 + [_P, _SZ, _P]
+        L.taot_add_rms_norm.restype = ctypes.c_int
+        L.taot_add_rms_norm.argtypes = [_P] * 3 + [_I64, _I32, _I32, _I32, _F32, _I32] + [_P] * 6
+        L.taot_add_rms_norm_backward_workspace_size.restype = _SZ
+        L.taot_add_rms_norm_backward_workspace_size.argtypes = [_I64, _I32]
+        L.taot_add_rms_norm_backward.restype = ctypes.c_int
+        L.taot_add_rms_norm_backward.argtypes = [_P] * 5 + [_I64, _I32, _I32, _I32, _P, _P, _P, _SZ, _P]
+        L.taot_route.restype = ctypes.c_int
+        L.taot_route.argtypes = [_P, _P, _I64] + [_I32] * 4 + [_F32, _U32, _I32, _P, _P, _P]
+        L.taot_route_backward.restype = ctypes.c_int
+        L.taot_route_backward.argtypes = [_P] * 3 + [_I64, _I32, _I32, _F32, _U32, _I32, _P, _P]
+        L.taot_dispatch_map_workspace_size.restype = _SZ
+        L.taot_dispatch_map_workspace_size.argtypes = [_I32, _I32, _I64, _I32, _I32, _I32]
+        L.taot_dispatch_map.restype = ctypes.c_int
+        L.taot_dispatch_map.argtypes = [_P, _I32, _I32, _I32, _I64, _P, _I32, _I32, _I32] + [_P] * 7 + [_SZ, _P]
+        L.taot_dispatch_rows.restype = ctypes.c_int
+        L.taot_dispatch_rows.argtypes = [_P, _I64, _P, _I64, _I64, _I64, _I32] + [_P] * 4
+        L.taot_combine_rows.restype = ctypes.c_int
+        L.taot_combine_rows.argtypes = [_P] * 3 + [_I64, _I64, _I32, _I32, _I32, _P, _P]
+        L.taot_combine_rows_backward.restype = ctypes.c_int
+        L.taot_combine_rows_backward.argtypes = [_P] * 4 + [_I64, _I64, _I32, _I32, _I32, _P, _P, _P]
         L.taot_topology_pref.restype = ctypes.c_int
         L.taot_topology_pref.argtypes = [_P, _I32, _P, _P]
         _lib = L
@@ -259,6 +286,293 @@ def plan_step(ids, home, C, E: int, eps: float, iters: int, K: int, Bpref=None, 
     sched = round_schedule(loads.n, loads.spill, loads.spare, loads.excess, loads.alpha, home, flow.T,
                            Bpref, Bauct, K, price_step, t_max, stream=stream, flags=flags)
     return Plan(loads, flow, sched)
+
+
+# ---- around the planner: the ids' source, and a plan's execution on the tokens ----
+
+_DTYPE = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}
+
+
+def _rows(t: torch.Tensor, name: str, like: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Checks a contiguous GPU tensor of bfloat16, float16 or float32 (the type of `like`)."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise TypeError(f"{name} must be a GPU tensor")
+    if t.dtype not in _DTYPE or (like is not None and t.dtype != like.dtype):
+        want = "bfloat16, float16 or float32" if like is None else like.dtype
+        raise TypeError(f"{name} must be {want}, got {t.dtype}")
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    return t
+
+
+def _shape(t: torch.Tensor, name: str, shape):
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
+
+
+def _empty(shape, dtype, device, stream) -> torch.Tensor:
+    """New memory of the stream that the call's work goes to: what used it before is done when that work begins, and
+    it is not handed out again before that work is done."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
+def _into(t: Optional[torch.Tensor], name: str, shape, dtype, device, stream) -> torch.Tensor:
+    """The caller's output tensor, checked, or a new one."""
+    if t is None:
+        return _empty(shape, dtype, device, stream)
+    _shape(_dev(t, name, dtype), name, shape)
+    return t
+
+
+def _room(workspace: Optional[torch.Tensor], nbytes: int, device, stream) -> torch.Tensor:
+    if workspace is None:
+        return _empty((max(int(nbytes), 1),), torch.uint8, device, stream)
+    if not workspace.is_cuda or not workspace.is_contiguous():
+        raise ValueError("workspace must be a contiguous GPU tensor")
+    return workspace
+
+
+@dataclasses.dataclass
+class Norm:
+    y: Optional[torch.Tensor] = None      # [..., H], x's type
+    q: Optional[torch.Tensor] = None      # [..., H] float8_e4m3fn
+    scale: Optional[torch.Tensor] = None  # [..., ceil(H / group)] float32 ([..., 1] for group = 0)
+    rstd: Optional[torch.Tensor] = None   # [...] float32
+    h: Optional[torch.Tensor] = None      # [..., H], x's type: x + residual (x itself without a residual)
+
+
+def add_rms_norm(x: torch.Tensor, weight: torch.Tensor, eps: float, residual: Optional[torch.Tensor] = None,
+                 group: Optional[int] = None, out: Optional[Norm] = None, stream=None) -> Norm:
+    """h = x + residual, y = h * rsqrt(mean(h^2) + eps) * weight over the last dimension (taot_add_rms_norm).
+    weight: [H] of x's type or float32.  group: also y in 8 bits with a scale for each `group` columns (a power
+    of two from 8 to 512), 0: one scale a row; None: no 8-bit output."""
+    _rows(x, "x")
+    H = x.shape[-1] if x.dim() else 0
+    if weight.dtype != torch.float32:
+        _rows(weight, "weight", x)
+    _shape(_rows(weight, "weight"), "weight", (H,))
+    if residual is not None:
+        _shape(_rows(residual, "residual", x), "residual", x.shape)
+    lead, dev = x.shape[:-1], x.device
+    if out is None:
+        out = Norm()
+    out.y = _into(out.y, "out.y", x.shape, x.dtype, dev, stream)
+    out.rstd = _into(out.rstd, "out.rstd", lead, torch.float32, dev, stream)
+    out.h = x if residual is None else _into(out.h, "out.h", x.shape, x.dtype, dev, stream)
+    q = s = None
+    if group is not None:
+        q = out.q = _into(out.q, "out.q", x.shape, torch.float8_e4m3fn, dev, stream)
+        n = -(-H // group) if group > 0 else 1
+        s = out.scale = _into(out.scale, "out.scale", (*lead, n), torch.float32, dev, stream)
+    T = x.numel() // H if H else 0
+    _check("taot_add_rms_norm", lib().taot_add_rms_norm(
+        x.data_ptr(), _ptr(residual), weight.data_ptr(), T, H, _DTYPE[x.dtype], _DTYPE[weight.dtype], float(eps),
+        int(group or 0), None if residual is None else out.h.data_ptr(), out.y.data_ptr(), _ptr(q), _ptr(s),
+        out.rstd.data_ptr(), _stream(stream)))
+    return out
+
+
+@dataclasses.dataclass
+class NormGrad:
+    dx: Optional[torch.Tensor] = None       # [..., H], h's type: the gradient of x and of the residual
+    dweight: Optional[torch.Tensor] = None  # [H] float32
+
+
+def add_rms_norm_backward(dy: torch.Tensor, h: torch.Tensor, rstd: torch.Tensor, weight: torch.Tensor,
+                          dh: Optional[torch.Tensor] = None, out: Optional[NormGrad] = None,
+                          workspace: Optional[torch.Tensor] = None, stream=None) -> NormGrad:
+    """Gradient of add_rms_norm (taot_add_rms_norm_backward) from its h and rstd: dy reaches y, dh reaches h."""
+    _rows(h, "h")
+    H = h.shape[-1] if h.dim() else 0
+    _shape(_rows(dy, "dy", h), "dy", h.shape)
+    if dh is not None:
+        _shape(_rows(dh, "dh", h), "dh", h.shape)
+    if weight.dtype != torch.float32:
+        _rows(weight, "weight", h)
+    _shape(_rows(weight, "weight"), "weight", (H,))
+    _shape(_dev(rstd, "rstd", torch.float32), "rstd", h.shape[:-1])
+    if out is None:
+        out = NormGrad()
+    out.dx = _into(out.dx, "out.dx", h.shape, h.dtype, h.device, stream)
+    out.dweight = _into(out.dweight, "out.dweight", (H,), torch.float32, h.device, stream)
+    T = h.numel() // H if H else 0
+    ws = _room(workspace, lib().taot_add_rms_norm_backward_workspace_size(T, H), h.device, stream)
+    _check("taot_add_rms_norm_backward", lib().taot_add_rms_norm_backward(
+        dy.data_ptr(), _ptr(dh), h.data_ptr(), rstd.data_ptr(), weight.data_ptr(), T, H, _DTYPE[h.dtype],
+        _DTYPE[weight.dtype], out.dx.data_ptr(), out.dweight.data_ptr(), ws.data_ptr(),
+        ws.numel() * ws.element_size(), _stream(stream)))
+    return out
+
+
+@dataclasses.dataclass
+class Routing:
+    ids: Optional[torch.Tensor] = None      # [..., top_k] int32, -1: none
+    weights: Optional[torch.Tensor] = None  # [..., top_k] float32
+
+
+def route(logits: torch.Tensor, top_k: int, bias: Optional[torch.Tensor] = None, groups: int = 1,
+          top_groups: int = 1, scale: float = 1.0, flags: int = 0, out: Optional[Routing] = None,
+          stream=None) -> Routing:
+    """Chooses top_k of the E experts of each token by logits [..., E] and weighs them (taot_route; flags ROUTE_*).
+    With logits [B][R][tokens][E], ids.view(B, R, -1) is plan_loads' input."""
+    _rows(logits, "logits")
+    E = logits.shape[-1] if logits.dim() else 0
+    if bias is not None:
+        _shape(_dev(bias, "bias", torch.float32), "bias", (E,))
+    shape = (*logits.shape[:-1], top_k)
+    if out is None:
+        out = Routing()
+    out.ids = _into(out.ids, "out.ids", shape, torch.int32, logits.device, stream)
+    out.weights = _into(out.weights, "out.weights", shape, torch.float32, logits.device, stream)
+    T = logits.numel() // E if E else 0
+    _check("taot_route", lib().taot_route(
+        logits.data_ptr(), _ptr(bias), T, E, int(top_k), int(groups), int(top_groups), float(scale), int(flags),
+        _DTYPE[logits.dtype], out.ids.data_ptr(), out.weights.data_ptr(), _stream(stream)))
+    return out
+
+
+def route_backward(dweights: torch.Tensor, logits: torch.Tensor, ids: torch.Tensor, scale: float = 1.0,
+                   flags: int = 0, out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """Gradient of route's weights by the logits (taot_route_backward): [..., E] of the logits' type."""
+    _rows(logits, "logits")
+    E = logits.shape[-1] if logits.dim() else 0
+    top_k = ids.shape[-1]
+    shape = (*logits.shape[:-1], top_k)
+    _shape(_dev(ids, "ids", torch.int32), "ids", shape)
+    _shape(_dev(dweights, "dweights", torch.float32), "dweights", shape)
+    out = _into(out, "out", logits.shape, logits.dtype, logits.device, stream)
+    T = logits.numel() // E if E else 0
+    _check("taot_route_backward", lib().taot_route_backward(
+        dweights.data_ptr(), logits.data_ptr(), ids.data_ptr(), T, E, top_k, float(scale), int(flags),
+        _DTYPE[logits.dtype], out.data_ptr(), _stream(stream)))
+    return out
+
+
+@dataclasses.dataclass
+class Dispatch:
+    pos: Optional[torch.Tensor] = None      # [B][rows][N] int32 row of the send buffer (p < 0: nowhere)
+    offsets: Optional[torch.Tensor] = None  # [B][rows][E + R*K + 1] int32 first row of each instance
+    sends: Optional[torch.Tensor] = None    # [B][rows][R] int32 copies for each rank
+    status: Optional[torch.Tensor] = None   # [B] int32 (uint32 bits)
+
+
+def dispatch_map(ids: torch.Tensor, home: torch.Tensor, slot_expert: torch.Tensor, X: torch.Tensor, K: int,
+                 rank0: int = 0, out: Optional[Dispatch] = None, workspace: Optional[torch.Tensor] = None,
+                 stream=None) -> Dispatch:
+    """Where a schedule sends each routed copy (taot_dispatch_map).  ids [B][rows][N] of the source ranks rank0 ..
+    rank0 + rows - 1; slot_expert [B][R*K] and X [B][R][R*K] of the schedule."""
+    _dev(ids, "ids", torch.int32)
+    _dev(home, "home", torch.int32)
+    _dev(slot_expert, "slot_expert", torch.int32)
+    _dev(X, "X", torch.int32)
+    if ids.dim() != 3 or X.dim() != 3 or home.dim() != 1:
+        raise ValueError("ids must be [B][rows][N], X [B][R][R*K] and home [E]")
+    B, rows, N = ids.shape
+    E, R = home.shape[0], X.shape[1]
+    S = R * K
+    _shape(X, "X", (B, R, S))
+    _shape(slot_expert, "slot_expert", (B, S))
+    dev = ids.device
+    if out is None:
+        out = Dispatch()
+    out.pos = _into(out.pos, "out.pos", (B, rows, N), torch.int32, dev, stream)
+    out.offsets = _into(out.offsets, "out.offsets", (B, rows, E + S + 1), torch.int32, dev, stream)
+    out.sends = _into(out.sends, "out.sends", (B, rows, R), torch.int32, dev, stream)
+    out.status = _into(out.status, "out.status", (B,), torch.int32, dev, stream)
+    ws = _room(workspace, lib().taot_dispatch_map_workspace_size(B, rows, N, R, E, K), dev, stream)
+    _check("taot_dispatch_map", lib().taot_dispatch_map(
+        ids.data_ptr(), B, rows, int(rank0), N, home.data_ptr(), R, E, int(K), slot_expert.data_ptr(), X.data_ptr(),
+        out.pos.data_ptr(), out.offsets.data_ptr(), out.sends.data_ptr(), out.status.data_ptr(), ws.data_ptr(),
+        ws.numel() * ws.element_size(), _stream(stream)))
+    return out
+
+
+def _tokens(pos: torch.Tensor, lead, name: str):
+    """(rows, tokens, top_k) of positions [..., N] and a tensor of shape [*lead, tokens, ...]."""
+    _dev(pos, "pos", torch.int32)
+    N, tokens = pos.shape[-1], lead[-1]
+    if tuple(pos.shape[:-1]) != tuple(lead[:-1]) or (N % tokens if tokens else N):
+        raise ValueError(f"{name} of {tuple(lead)} tokens does not go with positions of shape {tuple(pos.shape)}")
+    rows = 1
+    for d in lead[:-1]:
+        rows *= d
+    return rows, tokens, N // tokens if tokens else 1
+
+
+def dispatch_rows(x: torch.Tensor, pos: torch.Tensor, scale: Optional[torch.Tensor] = None,
+                  out: Optional[torch.Tensor] = None, out_scale: Optional[torch.Tensor] = None, stream=None):
+    """Tokens' rows x [..., tokens, H] (any type) at their places of the send buffer, [..., N, H] for pos [..., N]
+    (taot_dispatch_rows).  With scale [..., tokens, G]: (rows, scales).  Its gradient is combine_rows, no weights."""
+    if not isinstance(x, torch.Tensor) or not x.is_cuda:
+        raise TypeError("x must be a GPU tensor")
+    if not x.is_contiguous():
+        raise ValueError("x must be contiguous")
+    lead = x.shape[:-1]
+    rows, tokens, k = _tokens(pos, lead, "x")
+    out = _into(out, "out", (*pos.shape, x.shape[-1]), x.dtype, x.device, stream)
+    more = 0
+    if scale is not None:
+        _shape(_dev(scale, "scale", torch.float32), "scale", (*lead, scale.shape[-1]))
+        out_scale = _into(out_scale, "out_scale", (*pos.shape, scale.shape[-1]), torch.float32, x.device, stream)
+        more = 4 * scale.shape[-1]
+    _check("taot_dispatch_rows", lib().taot_dispatch_rows(
+        x.data_ptr(), x.shape[-1] * x.element_size(), _ptr(scale), more, rows, tokens, k, pos.data_ptr(),
+        out.data_ptr(), _ptr(out_scale) if scale is not None else None, _stream(stream)))
+    return out if scale is None else (out, out_scale)
+
+
+def combine_rows(y: torch.Tensor, pos: torch.Tensor, weights: Optional[torch.Tensor] = None, top_k: int = 1,
+                 out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """Weighted sum of each token's top_k rows of y [..., N, H] back in the tokens' order, [..., N / top_k, H]
+    (taot_combine_rows).  weights [..., N] float32 or None (all 1), as route gives them: [..., tokens, top_k] too."""
+    _rows(y, "y")
+    _shape(_dev(pos, "pos", torch.int32), "pos", y.shape[:-1])
+    N, H = y.shape[-2:]
+    if top_k < 1 or N % top_k:
+        raise ValueError(f"{N} copies are not top_k = {top_k} of each token")
+    if weights is not None and _dev(weights, "weights", torch.float32).numel() != pos.numel():
+        raise ValueError("weights must have a value for each copy")
+    lead = (*y.shape[:-2], N // top_k)
+    out = _into(out, "out", (*lead, H), y.dtype, y.device, stream)
+    rows, tokens, _ = _tokens(pos, lead, "y")
+    _check("taot_combine_rows", lib().taot_combine_rows(
+        y.data_ptr(), pos.data_ptr(), _ptr(weights), rows, tokens, int(top_k), H, _DTYPE[y.dtype], out.data_ptr(),
+        _stream(stream)))
+    return out
+
+
+@dataclasses.dataclass
+class CombineGrad:
+    dy: Optional[torch.Tensor] = None        # [..., N, H], y's type
+    dweights: Optional[torch.Tensor] = None  # [..., N] float32
+
+    def __iter__(self):
+        return iter((self.dy, self.dweights))
+
+
+def combine_rows_backward(dout: torch.Tensor, y: torch.Tensor, pos: torch.Tensor, weights: torch.Tensor,
+                          out: Optional[CombineGrad] = None, stream=None) -> CombineGrad:
+    """Gradient of combine_rows by y and the weights (taot_combine_rows_backward).  Without weights the gradient is
+    dispatch_rows(dout, pos)."""
+    _rows(y, "y")
+    _rows(dout, "dout", y)
+    _shape(_dev(pos, "pos", torch.int32), "pos", y.shape[:-1])
+    H = y.shape[-1]
+    rows, tokens, k = _tokens(pos, dout.shape[:-1], "dout")
+    _shape(dout, "dout", (*dout.shape[:-1], H))
+    if _dev(weights, "weights", torch.float32).numel() != pos.numel():
+        raise ValueError("weights must have a value for each copy")
+    if out is None:
+        out = CombineGrad()
+    out.dy = _into(out.dy, "out.dy", y.shape, y.dtype, y.device, stream)
+    out.dweights = _into(out.dweights, "out.dweights", weights.shape, torch.float32, y.device, stream)
+    _check("taot_combine_rows_backward", lib().taot_combine_rows_backward(
+        dout.data_ptr(), y.data_ptr(), pos.data_ptr(), weights.data_ptr(), rows, tokens, k, H, _DTYPE[y.dtype],
+        out.dy.data_ptr(), out.dweights.data_ptr(), _stream(stream)))
+    return out
 
 
 @dataclasses.dataclass

@@ -99,4 +99,34 @@ taot_status launch_schedule(const int32_t* n, const int64_t* spill, const int64_
                             hipStream_t stream);
 size_t schedule_ws(int32_t B, int32_t R, int32_t E, int32_t K);
 
+taot_status launch_add_rms_norm(const void* x, const void* residual, const void* weight, int64_t rows, int32_t H,
+                                int32_t dtype, int32_t weight_dtype, float eps, int32_t group, void* h, void* y,
+                                uint8_t* q, float* scale, float* rstd, hipStream_t stream);
+taot_status launch_add_rms_norm_backward(const void* dy, const void* dh, const void* h, const float* rstd,
+                                         const void* weight, int64_t rows, int32_t H, int32_t dtype,
+                                         int32_t weight_dtype, void* dx, float* dweight, void* ws,
+                                         hipStream_t stream);
+size_t add_rms_norm_backward_ws(int64_t rows, int32_t H);
+
+taot_status launch_route(const void* logits, const float* bias, int64_t T, int32_t E, int32_t k, int32_t groups,
+                         int32_t top_groups, float scale, uint32_t flags, int32_t dtype, int32_t* ids,
+                         float* weights, hipStream_t stream);
+taot_status launch_route_backward(const float* dweights, const void* logits, const int32_t* ids, int64_t T,
+                                  int32_t E, int32_t k, float scale, uint32_t flags, int32_t dtype, void* dlogits,
+                                  hipStream_t stream);
+
+taot_status launch_dispatch_map(const int32_t* ids, int32_t B, int32_t rows, int32_t rank0, int64_t N,
+                                const int32_t* home, int32_t R, int32_t E, int32_t K, const int32_t* slot_expert,
+                                const int32_t* X, int32_t* pos, int32_t* offsets, int32_t* sends, uint32_t* status,
+                                void* ws, hipStream_t stream);
+size_t dispatch_map_ws(int32_t B, int32_t rows, int64_t N, int32_t R, int32_t E, int32_t K);
+taot_status launch_dispatch_rows(const void* x, int64_t row_bytes, const void* x_more, int64_t more_bytes,
+                                 int64_t rows, int64_t tokens, int32_t k, const int32_t* pos, void* out,
+                                 void* out_more, hipStream_t stream);
+taot_status launch_combine_rows(const void* y, const int32_t* pos, const float* weights, int64_t rows, int64_t tokens,
+                                int32_t k, int32_t H, int32_t dtype, void* out, hipStream_t stream);
+taot_status launch_combine_rows_backward(const void* dout, const void* y, const int32_t* pos, const float* weights,
+                                         int64_t rows, int64_t tokens, int32_t k, int32_t H, int32_t dtype, void* dy,
+                                         float* dweights, hipStream_t stream);
+
 }  // namespace taot

@@ -1,0 +1,112 @@
+// Rows of 16- and 32-bit floating values: eight at a time as 32-bit floats, and
+// reductions over neighbouring lanes of a wave.
+#pragma once
+
+#include "common.h"
+
+namespace taot {
+
+typedef float f32x8 __attribute__((ext_vector_type(8)));
+
+// Eight values of type T at any address that T allows: a row of odd length
+// starts off every wider boundary, and the memory system takes 16-byte
+// accesses there as well.
+template <typename T>
+struct Row8 {
+  typedef T vec __attribute__((ext_vector_type(8)));
+  typedef __attribute__((aligned(sizeof(T)))) vec at;
+};
+
+template <typename T>
+__device__ __forceinline__ f32x8 load8(const T* p) {
+  return __builtin_convertvector(*reinterpret_cast<const typename Row8<T>::at*>(p), f32x8);
+}
+
+// The first n of eight values (n < 8), zeros behind them.
+template <typename T>
+__device__ __forceinline__ f32x8 load_head(const T* p, int n) {
+  f32x8 v;
+#pragma unroll
+  for (int u = 0; u < 8; ++u) v[u] = u < n ? (float)p[u] : 0.f;
+  return v;
+}
+
+// n values from p (0 and less: none), zeros behind them.
+template <typename T>
+__device__ __forceinline__ f32x8 load_row(const T* p, int n) {
+  if (n >= 8) return load8(p);
+  return load_head(p, n);
+}
+
+// Rounds to nearest even.
+template <typename T>
+__device__ __forceinline__ void store_row(T* p, f32x8 v, int n) {
+  if (n >= 8) {
+    *reinterpret_cast<typename Row8<T>::at*>(p) = __builtin_convertvector(v, typename Row8<T>::vec);
+    return;
+  }
+#pragma unroll
+  for (int u = 0; u < 8; ++u)
+    if (u < n) p[u] = (T)v[u];
+}
+
+// The same from a vector of T or of floats, chosen at run time by a value that
+// all lanes share.
+template <typename T>
+__device__ __forceinline__ f32x8 load_row_either(const void* base, bool f32, int64_t col, int n) {
+  return f32 ? load_row(static_cast<const float*>(base) + col, n) : load_row(static_cast<const T*>(base) + col, n);
+}
+
+// ---- lanes -------------------------------------------------------------------
+// The value of the lane that step S pairs this one with: S = 0, 1: the lane
+// whose number differs in bit S; 2: the mirror image in a half row of 8 lanes;
+// 3: in a row of 16.  After steps 0..S of a reduction every lane of a block of
+// 2^(S+1) lanes holds the block's result.  All lanes have to be active.
+template <int S>
+__device__ __forceinline__ int lane_step(int v) {
+  static_assert(S >= 0 && S < 4, "steps within a row of 16 lanes");
+  constexpr int ctrl = S == 0 ? 0xB1 : S == 1 ? 0x4E : S == 2 ? 0x141 : 0x140;
+  return __builtin_amdgcn_mov_dpp(v, ctrl, 0xF, 0xF, false);
+}
+template <int S>
+__device__ __forceinline__ float lane_step(float v) {
+  return __int_as_float(lane_step<S>(__float_as_int(v)));
+}
+
+// Result of `op` over blocks of L neighbouring lanes (L a power of two), in
+// every lane of the block; op has to commute.  The order is fixed.
+template <int L, typename V, typename Op>
+__device__ __forceinline__ V block_reduce(V v, Op op) {
+  if constexpr (L >= 2) v = op(v, lane_step<0>(v));
+  if constexpr (L >= 4) v = op(v, lane_step<1>(v));
+  if constexpr (L >= 8) v = op(v, lane_step<2>(v));
+  if constexpr (L >= 16) v = op(v, lane_step<3>(v));
+  if constexpr (L >= 32) v = op(v, __shfl_xor(v, 16, kWave));
+  if constexpr (L >= 64) v = op(v, __shfl_xor(v, 32, kWave));
+  return v;
+}
+
+struct MaxOp {
+  __device__ __forceinline__ float operator()(float a, float b) const { return fmaxf(a, b); }
+  __device__ __forceinline__ int operator()(int a, int b) const { return max(a, b); }
+};
+struct MinOp {
+  __device__ __forceinline__ int operator()(int a, int b) const { return min(a, b); }
+};
+struct SumOp {
+  __device__ __forceinline__ float operator()(float a, float b) const { return a + b; }
+};
+
+// The maximum over blocks of `lanes` neighbouring lanes, `lanes` a power of two
+// that the whole wave shares.
+__device__ __forceinline__ float block_max(float v, int lanes) {
+  if (lanes >= 2) v = fmaxf(v, lane_step<0>(v));
+  if (lanes >= 4) v = fmaxf(v, lane_step<1>(v));
+  if (lanes >= 8) v = fmaxf(v, lane_step<2>(v));
+  if (lanes >= 16) v = fmaxf(v, lane_step<3>(v));
+  if (lanes >= 32) v = fmaxf(v, __shfl_xor(v, 16, kWave));
+  if (lanes >= 64) v = fmaxf(v, __shfl_xor(v, 32, kWave));
+  return v;
+}
+
+}  // namespace taot

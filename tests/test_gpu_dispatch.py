@@ -1,0 +1,367 @@
+"""dispatch_map against a direct walk through the definition (whole numbers:
+equal), dispatch_rows (copies: equal), combine_rows and its gradient against the
+formulas in 64 bits.
+
+Sums: k products of 32 bits, k + 1 roundings of 2^-24 a term; an inner product
+over H columns passes through at most H / 64 + 10 additions a term.  u is half a
+unit in the last place of the output's type."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2608_03676_amd as taot
+
+pytestmark = pytest.mark.gpu
+
+TYPES = [torch.bfloat16, torch.float16, torch.float32]
+U = {torch.bfloat16: 2.0 ** -8, torch.float16: 2.0 ** -11, torch.float32: 2.0 ** -24}
+LOW = {torch.bfloat16: 0.0, torch.float16: 2.0 ** -25, torch.float32: 0.0}
+
+
+def oracle_map(ids, home, slot_expert, X, K, rank0):
+    B, rows, N = ids.shape
+    R, E = X.shape[1], len(home)
+    S = R * K
+    inst = []                                   # (kind, id) in send order
+    edge = [0]
+    for r in range(R):
+        inst += [("own", e) for e in range(E) if home[e] == r]
+        inst += [("guest", s) for s in range(r * K, (r + 1) * K)]
+        edge.append(len(inst))
+    lost = [("own", e) for e in range(E) if not 0 <= home[e] < R]
+    number = {v: i for i, v in enumerate(inst + lost)}
+    pos = np.zeros((B, rows, N), np.int32)
+    offsets = np.zeros((B, rows, E + S + 1), np.int32)
+    sends = np.zeros((B, rows, R), np.int32)
+    for b in range(B):
+        slots = {}
+        for s in range(S):
+            if 0 <= slot_expert[b, s] < E:
+                slots.setdefault(int(slot_expert[b, s]), []).append(s)
+        for q in range(rows):
+            left = {e: [[s, max(int(X[b, rank0 + q, s]), 0)] for s in v] for e, v in slots.items()}
+            where = np.empty(N, np.int64)
+            for i, e in enumerate(ids[b, q].tolist()):
+                if not 0 <= e < E:
+                    where[i] = E + S
+                    continue
+                go = left.get(e, [])
+                while go and go[0][1] == 0:
+                    go.pop(0)
+                if go:
+                    go[0][1] -= 1
+                    where[i] = number[("guest", go[0][0])]
+                else:
+                    where[i] = number[("own", e)]
+            order = np.argsort(where, kind="stable")
+            p = np.empty(N, np.int64)
+            p[order] = np.arange(N)
+            placed = int((where < len(inst)).sum())
+            pos[b, q] = np.where(p < placed, p, ~p)
+            count = np.bincount(where, minlength=E + S + 1)[:E + S]
+            offsets[b, q] = np.minimum(np.concatenate([[0], np.cumsum(count)]), placed)
+            at = np.concatenate([[0], np.cumsum(count)])
+            sends[b, q] = [at[edge[r + 1]] - at[edge[r]] for r in range(R)]
+    return pos, offsets, sends
+
+
+def _instance(B, R, rows, E, K, N, seed, bad=0.0, wild=False, zipf=1.1):
+    rng = np.random.default_rng(seed)
+    p = np.arange(1, E + 1) ** -zipf
+    p = rng.permutation(p / p.sum())
+    ids = rng.choice(E, size=(B, rows, N), p=p).astype(np.int32)
+    if bad:
+        hit = rng.random(ids.shape) < bad
+        ids[hit] = rng.choice([-1, E, E + 5, 2 ** 31 - 1, -2 ** 31], size=int(hit.sum()))
+    home = rng.integers(0, R, size=E).astype(np.int32)
+    S = R * K
+    hot = rng.integers(0, E, size=max(1, min(E, S // 3 + 1)))
+    slot = hot[rng.integers(0, len(hot), size=(B, S))].astype(np.int32)
+    slot[rng.random((B, S)) < 0.2] = -1
+    X = rng.integers(0, max(2, 2 * N // max(1, E // 2) + 2), size=(B, R, S)).astype(np.int32)
+    if wild:
+        X[rng.random(X.shape) < 0.1] = -3
+        X[rng.random(X.shape) < 0.05] = 2 ** 31 - 1
+        slot[rng.random(slot.shape) < 0.1] = E + 7
+    return ids, home, slot, X
+
+
+def _run(gpu, ids, home, slot, X, K, rank0):
+    t = [torch.from_numpy(a).to(gpu) for a in (ids, home, slot, X)]
+    return taot.dispatch_map(*t, K, rank0=rank0)
+
+
+def _check_map(gpu, ids, home, slot, X, K, rank0=0):
+    m = _run(gpu, ids, home, slot, X, K, rank0)
+    pos, offsets, sends = oracle_map(ids, home, slot, X, K, rank0)
+    assert np.array_equal(m.pos.cpu().numpy(), pos)
+    assert np.array_equal(m.offsets.cpu().numpy(), offsets)
+    assert np.array_equal(m.sends.cpu().numpy(), sends)
+    E = len(home)
+    for b in range(ids.shape[0]):
+        want = (1 if ((ids[b] < 0) | (ids[b] >= E)).any() else 0) | (2 if ((home < 0) | (home >= X.shape[1])).any() else 0)
+        assert int(m.status[b]) == want
+    return m
+
+
+@pytest.mark.parametrize("N", [0, 1, 2, 63, 64, 65, 255, 256, 257, 1023, 1024, 1025, 5000])
+def test_lengths(gpu, N):
+    print(f"[map] N = {N}", flush=True)
+    _check_map(gpu, *_instance(2, 4, 4, 12, 2, N, seed=N), 2)
+
+
+@pytest.mark.parametrize("B,R,rows,E,K,N", [(1, 1, 1, 1, 0, 100), (1, 1, 1, 1, 1, 100), (3, 5, 2, 7, 1, 700),
+                                            (1, 16, 16, 64, 2, 2048), (2, 24, 3, 49, 4, 1500), (1, 8, 1, 300, 3, 4099),
+                                            (1, 64, 2, 256, 2, 8192), (1, 7, 7, 5, 64, 300), (1, 32, 1, 4096, 2, 9000),
+                                            (1, 300, 1, 384, 2, 3000)])
+def test_shapes(gpu, B, R, rows, E, K, N):
+    print(f"[map] B = {B}, R = {R}, rows = {rows}, E = {E}, K = {K}, N = {N}", flush=True)
+    _check_map(gpu, *_instance(B, R, rows, E, K, N, seed=R + E), K, rank0=R - rows)
+
+
+def test_most_experts_and_ranks(gpu):
+    _check_map(gpu, *_instance(1, 2048, 1, 32768, 2, 40000, seed=3, zipf=0.3), 2, rank0=2047)
+
+
+def test_many_copies_of_one_expert(gpu):
+    ids, home, slot, X = _instance(1, 600, 1, 8, 4, 6000, seed=8)
+    slot[:] = 3
+    ids[:] = 3
+    X[:] = np.arange(2400, dtype=np.int32) % 4
+    _check_map(gpu, ids, home, slot, X, 4, rank0=17)
+
+
+def test_ids_that_are_no_expert_and_shares_that_are_none(gpu):
+    for seed in range(4):
+        ids, home, slot, X = _instance(2, 6, 6, 20, 3, 900, seed=seed, bad=0.1 * seed, wild=True)
+        _check_map(gpu, ids, home, slot, X, 3)
+
+
+def test_experts_without_a_home(gpu):
+    ids, home, slot, X = _instance(2, 6, 6, 20, 3, 900, seed=5, bad=0.05)
+    home[[0, 7, 19]] = [-1, 6, 1000]
+    _check_map(gpu, ids, home, slot, X, 3)
+    home[:] = -1
+    m = _check_map(gpu, ids, home, slot, X, 3)
+    assert (m.offsets[..., -1] < 900).all()
+    m = _check_map(gpu, ids, home, np.full_like(slot, -1), X, 3)
+    assert not m.offsets.any() and (m.pos < 0).all()
+
+
+def test_long_rows(gpu):
+    """Several chunks a wave, against the same map of a stable sort."""
+    ids, home, slot, X = _instance(1, 3, 3, 40, 2, 300001, seed=2)
+    m = _run(gpu, ids, home, slot, X, 2, 0)
+    pos, offsets, sends = oracle_map(ids, home, slot, X, 2, 0)
+    assert np.array_equal(m.pos.cpu().numpy(), pos) and np.array_equal(m.offsets.cpu().numpy(), offsets)
+    assert np.array_equal(m.sends.cpu().numpy(), sends)
+
+
+def test_many_rows(gpu):
+    """More rows of short chunks than the waves that are wanted: longer chunks."""
+    ids, home, slot, X = _instance(40, 25, 25, 30, 1, 17000, seed=4)
+    m = _run(gpu, ids, home, slot, X, 1, 0)
+    for b in (0, 17, 39):
+        for r in (0, 12, 24):
+            pos, offsets, sends = oracle_map(ids[b:b + 1, r:r + 1], home, slot[b:b + 1], X[b:b + 1], 1, r)
+            assert np.array_equal(m.pos[b, r].cpu().numpy(), pos[0, 0])
+            assert np.array_equal(m.offsets[b, r].cpu().numpy(), offsets[0, 0])
+            assert np.array_equal(m.sends[b, r].cpu().numpy(), sends[0, 0])
+
+
+def test_one_rank_is_its_row_of_all(gpu):
+    ids, home, slot, X = _instance(2, 9, 9, 30, 2, 1300, seed=6)
+    m = _run(gpu, ids, home, slot, X, 2, 0)
+    for r in (0, 4, 8):
+        one = _run(gpu, np.ascontiguousarray(ids[:, r:r + 1]), home, slot, X, 2, r)
+        assert torch.equal(one.pos[:, 0], m.pos[:, r]) and torch.equal(one.offsets[:, 0], m.offsets[:, r])
+        assert torch.equal(one.sends[:, 0], m.sends[:, r])
+
+
+def test_a_schedule_is_carried_out(gpu):
+    """With the planner's own schedule each guest slot receives X copies of its expert from each rank."""
+    import workloads as W
+    w = W.WORKLOADS[0]
+    ids = torch.from_numpy(W.problem_ids_host(w, 0)[None]).to(gpu)
+    home, C = torch.from_numpy(W.home_map(w)).to(gpu), torch.from_numpy(W.cost_matrix(w)).to(gpu)
+    plan = taot.plan_step(ids, home, C, w.E, w.eps, w.iters, w.K)
+    s = plan.schedule
+    m = taot.dispatch_map(ids, home, s.slot_expert, s.X, w.K)
+    off = m.offsets.cpu().numpy()
+    h = home.cpu().numpy()
+    first = np.searchsorted(h, np.arange(w.R + 1))  # block homes are sorted
+    at = np.array([q + first[q // w.K + 1] for q in range(w.R * w.K)])
+    got = off[0][:, at + 1] - off[0][:, at]
+    assert np.array_equal(got, s.X[0].cpu().numpy()) and got.sum() > 0
+    q = taot.plan_quality(plan.loads.load_r, home, s, w.K)
+    assert torch.equal(m.sends[0].sum(0, dtype=torch.int64), q.load_after[0])
+
+
+def test_a_kept_workspace_and_another_stream(gpu):
+    ids, home, slot, X = _instance(1, 8, 8, 64, 2, 3000, seed=1)
+    t = [torch.from_numpy(a).to(gpu) for a in (ids, home, slot, X)]
+    ws = torch.full((int(taot.lib().taot_dispatch_map_workspace_size(1, 8, 3000, 8, 64, 2)),), 0xA5, dtype=torch.uint8, device=gpu)
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    m = taot.dispatch_map(*t, 2, workspace=ws, stream=s)
+    m2 = taot.dispatch_map(*t, 2, workspace=ws, stream=s)
+    s.synchronize()
+    pos, offsets, sends = oracle_map(ids, home, slot, X, 2, 0)
+    for x in (m, m2):
+        assert np.array_equal(x.pos.cpu().numpy(), pos) and np.array_equal(x.sends.cpu().numpy(), sends)
+    with pytest.raises(taot.TaotError) as e:
+        taot.dispatch_map(*t, 2, workspace=ws[:1000])
+    assert e.value.code == 3
+
+
+# ---- rows ---------------------------------------------------------------------------
+
+def _positions(rows, N, seed, dropped=0.0):
+    rng = np.random.default_rng(seed)
+    pos = np.stack([rng.permutation(N) for _ in range(rows)]).astype(np.int32) if N else np.zeros((rows, 0), np.int32)
+    out = pos.copy()
+    for r in range(rows):
+        kept = int(round(N * (1 - dropped)))
+        out[r] = np.where(pos[r] < kept, pos[r], ~pos[r])
+    return out
+
+
+@pytest.mark.parametrize("tokens,k,width", [(1, 1, 1), (3, 2, 5), (7, 8, 16), (5, 3, 17), (9, 4, 1000), (4, 6, 1024),
+                                            (6, 2, 2048), (5, 8, 2050), (3, 64, 4099)])
+@pytest.mark.parametrize("dropped", [0.0, 0.3, 1.0])
+def test_rows(gpu, tokens, k, width, dropped):
+    N = tokens * k
+    pos = _positions(2, N, seed=width, dropped=dropped)
+    g = torch.Generator().manual_seed(width)
+    t = torch.from_numpy(pos).to(gpu)
+    for x in (torch.randint(0, 256, (2, tokens, width), generator=g).byte(),
+              torch.randn(2, tokens, width, generator=g).half(), torch.randn(2, tokens, width, generator=g)):
+        scale = torch.randn(2, tokens, 1 + width // 128, generator=g)
+        out, more = taot.dispatch_rows(x.to(gpu), t, scale=scale.to(gpu))
+        alone = taot.dispatch_rows(x.to(gpu), t)
+        assert torch.equal(alone, out)
+        for got, src in ((out.cpu(), x), (more.cpu(), scale)):
+            want = torch.zeros((2, N, src.shape[2]), dtype=src.dtype)
+            for r in range(2):
+                for i in range(N):
+                    if pos[r, i] >= 0:
+                        want[r, pos[r, i]] = src[r, i // k]
+            assert torch.equal(got, want)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("tokens,k,H", [(1, 1, 1), (3, 2, 7), (5, 3, 8), (7, 8, 100), (4, 6, 1024), (6, 5, 1032),
+                                        (5, 8, 2051), (2, 64, 4096), (3, 9, 9000)])
+@pytest.mark.parametrize("dropped", [0.0, 0.4])
+def test_combine_and_its_gradient(gpu, dtype, tokens, k, H, dropped):
+    N = tokens * k
+    pos = _positions(2, N, seed=H, dropped=dropped)
+    g = torch.Generator().manual_seed(H + k)
+    y = torch.randn(2, N, H, generator=g).to(dtype)
+    w = torch.rand(2, N, generator=g)
+    d = torch.randn(2, tokens, H, generator=g).to(dtype)
+    if dropped:  # what lies in the rows that no copy reaches is not read
+        for r in range(2):
+            y[r, int((pos[r] >= 0).sum()):] = float("nan")
+    P = torch.from_numpy(np.where(pos >= 0, pos, 0)).long()
+    there = torch.from_numpy(pos >= 0)
+    Y = torch.stack([y[r, P[r]] for r in range(2)]).double()
+    Y = torch.where(there[:, :, None], Y, torch.zeros_like(Y)).view(2, tokens, k, H)
+    t = torch.from_numpy(pos).to(gpu)
+    for weights in (w, None):
+        W = (torch.ones_like(w) if weights is None else w).double().view(2, tokens, k, 1)
+        out = taot.combine_rows(y.to(gpu), t, weights=None if weights is None else w.to(gpu), top_k=k).double().cpu()
+        want, size = (W * Y).sum(2), (W * Y).abs().sum(2)
+        assert ((out - want).abs() <= U[dtype] * want.abs() + LOW[dtype] + (k + 1) * 2.0 ** -24 * size).all()
+    c = taot.combine_rows_backward(d.to(gpu), y.to(gpu), t, w.to(gpu))
+    D = d.double()[:, :, None, :]
+    dots, size = (D * Y).sum(3).view(2, N), (D * Y).abs().sum(3).view(2, N)
+    assert ((c.dweights.double().cpu() - dots).abs() <= (H / 64 + 10) * 2.0 ** -24 * size).all()
+    full = (w.double().view(2, tokens, k, 1) * D).view(2, N, H)
+    want = torch.zeros(2, N, H, dtype=torch.float64)
+    for r in range(2):
+        want[r, P[r][there[r]]] = full[r][there[r]]
+    got = c.dy.double().cpu()
+    assert ((got - want).abs() <= (U[dtype] + 2.0 ** -24) * want.abs() + LOW[dtype]).all()
+
+
+def test_there_and_back_are_each_others_gradient(gpu):
+    """<dispatch(x), z> = <x, combine(z)>, and the weights' gradient against differences (exact here: linear)."""
+    pos = torch.from_numpy(_positions(1, 60, seed=1, dropped=0.2)).to(gpu)
+    g = torch.Generator().manual_seed(3)
+    x, z, w, v = (torch.randn(s, generator=g).to(gpu) for s in ((1, 20, 33), (1, 60, 33), (1, 60), (1, 60)))
+    there = (taot.dispatch_rows(x, pos).double() * z.double()).sum()
+    back = (x.double() * taot.combine_rows(z, pos, top_k=3).double()).sum()
+    assert abs(there - back) <= 1e-5 * 20 * 33
+    c = taot.combine_rows_backward(x, z, pos, w)
+    a, b = (taot.combine_rows(z, pos, weights=w + s * v, top_k=3).double() for s in (1.0, -1.0))
+    want = (x.double() * (a - b) / 2).sum()
+    assert abs(want - (c.dweights.double() * v.double()).sum()) <= 1e-5 * (c.dweights * v).abs().sum()
+
+
+def test_rows_beyond_32_bits(gpu):
+    """Offsets past 2^32 bytes: the last rows of a buffer of 4.3 GB."""
+    tokens, k, H = 66000, 1, 65536
+    pos = torch.arange(tokens, dtype=torch.int32, device=gpu)[None]
+    x = torch.zeros(1, tokens, H, dtype=torch.uint8, device=gpu)
+    x[0, -1] = 7
+    x[0, -2, ::2] = 9
+    out = taot.dispatch_rows(x, pos)
+    assert torch.equal(out[0, -3:], x[0, -3:])
+    del x, out
+    y = torch.zeros(1, tokens, H // 2, dtype=torch.bfloat16, device=gpu)
+    y[0, -1] = 3
+    back = taot.combine_rows(y, pos, top_k=1)
+    assert torch.equal(back[0, -2:], y[0, -2:])
+
+
+def test_odd_addresses(gpu):
+    pos = torch.from_numpy(_positions(1, 12, seed=2)).to(gpu)
+    g = torch.Generator().manual_seed(2)
+    room = torch.randn(1 + 12 * 40, generator=g).half().to(gpu)
+    y = room[1:].view(1, 12, 40)
+    w = torch.rand(13, generator=g).to(gpu)[1:].view(1, 12)
+    assert torch.equal(taot.combine_rows(y, pos, weights=w, top_k=4),
+                       taot.combine_rows(y.clone(), pos, weights=w.clone(), top_k=4))
+    b = torch.arange(1 + 3 * 37, device=gpu).byte()[1:].view(1, 3, 37)
+    assert torch.equal(taot.dispatch_rows(b, pos), taot.dispatch_rows(b.clone(), pos))
+
+
+def test_empty_and_refusals(gpu):
+    ids, home, slot, X = (torch.from_numpy(a).to(gpu) for a in _instance(1, 4, 2, 12, 2, 30, seed=0))
+    for rank0 in (-1, 3):
+        with pytest.raises(taot.TaotError) as e:
+            taot.dispatch_map(ids, home, slot, X, 2, rank0=rank0)
+        assert e.value.code == 1
+    with pytest.raises(ValueError):
+        taot.dispatch_map(ids, home, slot, X, 3)
+    with pytest.raises(ValueError):
+        taot.dispatch_map(ids, home, slot[:, :-1], X, 2)
+    with pytest.raises(TypeError):
+        taot.dispatch_map(ids.long(), home, slot, X, 2)
+    with pytest.raises(ValueError):
+        taot.dispatch_map(ids.transpose(1, 2), home, slot, X, 2)
+    m = taot.dispatch_map(ids[:0], home, slot[:0], X[:0], 2)
+    assert m.pos.shape == (0, 2, 30)
+    x, pos = torch.zeros(1, 4, 8, device=gpu), torch.zeros(1, 12, dtype=torch.int32, device=gpu)
+    with pytest.raises(ValueError):
+        taot.dispatch_rows(x[:, :3].transpose(1, 2), pos)
+    with pytest.raises(ValueError):
+        taot.dispatch_rows(x, pos[:, :11].contiguous())
+    with pytest.raises(TypeError):
+        taot.dispatch_rows(x, pos.long())
+    y = torch.zeros(1, 12, 8, device=gpu)
+    with pytest.raises(ValueError):
+        taot.combine_rows(y, pos, top_k=5)
+    with pytest.raises(TypeError):
+        taot.combine_rows(y.double(), pos, top_k=3)
+    with pytest.raises(ValueError):
+        taot.combine_rows(y, pos, weights=torch.zeros(1, 11, device=gpu), top_k=3)
+    with pytest.raises(ValueError):
+        taot.combine_rows_backward(x[..., :7].contiguous(), y, pos, torch.zeros(1, 12, device=gpu))
+    with pytest.raises(taot.TaotError) as e:
+        taot.combine_rows(torch.zeros(1, 65, 8, device=gpu), torch.zeros(1, 65, dtype=torch.int32, device=gpu), top_k=65)
+    assert e.value.code == 2
+    none = torch.zeros(1, 0, dtype=torch.int32, device=gpu)
+    assert taot.dispatch_rows(x[:, :0], none).shape == (1, 0, 8)
+    assert taot.combine_rows(y[:, :0], none, top_k=4).shape == (1, 0, 8)

@@ -1,0 +1,308 @@
+"""route and its gradient against the definition in 64 bits.
+
+Choices are compared exactly.  Logits and biases lie on grids, so that ties are
+exact and common; tokens on which two different keys come closer than 1e-6 of
+each other in 64 bits (where 32 bits may order them otherwise) are left out, and
+are few.  Weights: exp and the division are within 3 units of 2^-24, the
+exponent's rounding is at most 2^-24 times the spread of the logits (below 32
+here), and a sum of up to 32768 positive terms passes through at most 128 + 70
+additions a term: 1.5e-5 in all; 3e-6 where only the chosen enter."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2608_03676_amd as taot
+
+pytestmark = pytest.mark.gpu
+
+TYPES = [torch.bfloat16, torch.float16, torch.float32]
+U = {torch.bfloat16: 2.0 ** -8, torch.float16: 2.0 ** -11, torch.float32: 2.0 ** -24}
+SIG, REN, TWO = taot.ROUTE_SIGMOID, taot.ROUTE_RENORM, taot.ROUTE_GROUP_TWO
+
+
+def oracle(x, k, bias, groups, top_groups, scale, flags):
+    """ids [T][k], weights [T][k], margin [T]: how near the closest two different keys that decide come."""
+    x = np.asarray(x, np.float64)
+    T, E = x.shape
+    ids, weights, margin = np.full((T, k), -1), np.zeros((T, k)), np.full(T, np.inf)
+    for t in range(T):
+        z = np.where(x[t] > -np.inf, np.minimum(x[t], 3.402823466e38), -np.inf)
+        ok = z > -np.inf
+        if not ok.any():
+            continue
+        if flags & SIG:
+            s = np.where(ok, 1 / (1 + np.exp(-np.where(ok, z, 0))), 0)
+        else:
+            s = np.where(ok, np.exp(z - z[ok].max()), 0)
+            s = s / s.sum()
+        key = z if bias is None else s + bias
+        key = np.where(ok & (key > -np.inf), key, -np.inf)
+        if groups > 1:
+            g = -np.sort(-key.reshape(groups, -1), axis=1)
+            value = g[:, 0].copy()
+            if flags & TWO and g.shape[1] > 1:
+                value = value + np.where(g[:, 1] > -np.inf, g[:, 1], 0)
+            order = np.lexsort((np.arange(groups), -value))
+            drop = order[top_groups:]
+            if len(drop) and value[drop].max() > -np.inf:  # the last that stays against the first that does not
+                near = value[order[top_groups - 1]] - value[drop].max()
+                margin[t] = near if near > 0 else margin[t]
+            key.reshape(groups, -1)[drop] = -np.inf
+        order = np.lexsort((np.arange(E), -key))[:min(E, k + 1)]
+        gaps = -np.diff(key[order][key[order] > -np.inf])
+        gaps = gaps[gaps > 0]
+        if gaps.size:
+            margin[t] = min(margin[t], gaps.min())
+        pick = [e for e in order[:k] if key[e] > -np.inf]
+        w = s[pick]
+        if flags & REN and len(pick):
+            if flags & SIG:
+                w = w / (w.sum() + 1e-20)
+            else:
+                w = np.exp(z[pick] - z[pick].max())
+                w = w / w.sum()
+        ids[t, :len(pick)], weights[t, :len(pick)] = pick, scale * w
+    return ids, weights, margin
+
+
+def _logits(T, E, dtype, seed, step=1 / 16):
+    g = torch.Generator().manual_seed(seed)
+    x = torch.randn(T, E, generator=g) * 1.5
+    return ((x / step).round() * step).to(dtype)  # exact in every type
+
+
+def _bias(E, seed):
+    return torch.randint(-20, 21, (E,), generator=torch.Generator().manual_seed(seed)).float() / 256
+
+
+def _check(gpu, x, k, bias=None, groups=1, top_groups=1, scale=1.0, flags=0, tol=1.5e-5):
+    r = taot.route(x.to(gpu), k, bias=None if bias is None else bias.to(gpu), groups=groups, top_groups=top_groups,
+                   scale=scale, flags=flags)
+    ids, weights, margin = oracle(x.double().numpy(), k, None if bias is None else bias.double().numpy(), groups,
+                                  top_groups, scale, flags)
+    sure = margin > 1e-6
+    assert sure.mean() > 0.8 or len(sure) < 20, sure.mean()
+    got_ids, got_w = r.ids.cpu().numpy(), r.weights.double().cpu().numpy()
+    assert np.array_equal(got_ids[sure], ids[sure])
+    assert (np.abs(got_w - weights)[sure] <= tol * np.abs(weights[sure]) + 1e-30).all()
+    return r
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("E,k", [(1, 1), (2, 2), (8, 8), (16, 3), (60, 6), (64, 1), (100, 17), (128, 8), (129, 8),
+                                 (256, 8), (257, 16), (384, 8), (512, 8), (513, 4), (1000, 64), (1024, 8), (1030, 8),
+                                 (2048, 2), (4096, 8), (4104, 8)])
+def test_experts_and_choices(gpu, dtype, E, k):
+    print(f"[route] {dtype} E = {E}, k = {k}", flush=True)
+    for T in (1, 5, 67):
+        x = _logits(T, E, dtype, seed=E + T)
+        _check(gpu, x, k, flags=0, scale=1.0)
+        _check(gpu, x, k, flags=REN, scale=2.5, tol=3e-6)
+        _check(gpu, x, k, flags=SIG | REN, scale=1.5, tol=3e-6)
+        _check(gpu, x, k, flags=SIG, bias=_bias(E, E), tol=3e-6)
+        _check(gpu, x, k, flags=0, bias=_bias(E, E + 1))
+
+
+@pytest.mark.parametrize("E,k", [(9000, 8), (32768, 64)])
+def test_more_experts_than_registers(gpu, E, k):
+    x = _logits(3, E, torch.float32, seed=E, step=1 / 64)
+    _check(gpu, x, k, flags=0)
+    _check(gpu, x, k, flags=SIG | REN, tol=3e-6)
+    _check(gpu, x, k, groups=8, top_groups=3, flags=REN, tol=3e-6)
+    _check(gpu, x, k, groups=8, top_groups=3, flags=REN | TWO, tol=3e-6)
+    x = _logits(3, E, torch.bfloat16, seed=E)
+    _check(gpu, x, k, flags=SIG, bias=_bias(E, E), groups=4, top_groups=1, tol=3e-6)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("E,groups,top_groups,k", [(16, 8, 4, 8), (64, 8, 3, 4), (160, 8, 4, 6), (256, 8, 4, 8),
+                                                   (256, 4, 1, 8), (256, 16, 5, 8), (60, 3, 2, 6), (500, 5, 2, 8),
+                                                   (512, 32, 7, 8), (4096, 8, 4, 8), (1000, 8, 4, 8), (64, 64, 20, 8),
+                                                   (256, 128, 9, 8), (4096, 256, 20, 8), (512, 2, 1, 20), (96, 6, 6, 8)])
+def test_groups(gpu, dtype, E, groups, top_groups, k):
+    print(f"[route groups] {dtype} E = {E}, {top_groups} of {groups}, k = {k}", flush=True)
+    x = _logits(37, E, dtype, seed=E + groups, step=1 / 64)
+    bias = _bias(E, groups)
+    a = dict(groups=groups, top_groups=top_groups)
+    _check(gpu, x, k, bias=bias, flags=SIG | REN, tol=3e-6, **a)
+    _check(gpu, x, k, flags=REN, tol=3e-6, **a)
+    _check(gpu, x, k, flags=0, **a)
+
+
+@pytest.mark.parametrize("E,groups,k", [(64, 4, 6), (256, 8, 8), (1000, 8, 8), (4096, 16, 8)])
+def test_groups_by_two(gpu, E, groups, k):
+    # a coarse grid of keys: sums of two are exact in 32 bits, so group ties are true ties
+    x = _logits(41, E, torch.float32, seed=E, step=1 / 8)
+    _check(gpu, x, k, groups=groups, top_groups=groups // 2, flags=REN | TWO, tol=3e-6)
+
+
+def test_ties_go_to_the_lower_expert(gpu):
+    for E in (64, 300, 2000, 5000):
+        r = taot.route(torch.zeros(3, E, device=gpu), 8)
+        assert (r.ids.cpu() == torch.arange(8)).all()
+        r = taot.route(torch.zeros(3, E, device=gpu), 8, bias=torch.zeros(E, device=gpu), flags=SIG)
+        assert (r.ids.cpu() == torch.arange(8)).all()
+        x = torch.full((2, E), -0.0, device=gpu)
+        x[:, ::2] = 0.0
+        assert (taot.route(x, 5).ids.cpu() == torch.arange(5)).all()
+    r = taot.route(torch.zeros(3, 64, device=gpu), 8, groups=8, top_groups=2)
+    assert (r.ids.cpu() == torch.arange(8)).all()
+
+
+@pytest.mark.parametrize("E,groups", [(64, 1), (256, 8), (1024, 1), (4096, 16), (6000, 4)])
+@pytest.mark.parametrize("flags", [0, REN, SIG, SIG | REN | TWO])
+def test_masked_experts(gpu, E, groups, flags):
+    x = _logits(8, E, torch.float32, seed=E, step=1 / 8)
+    x[0] = -np.inf                      # a row that is masked altogether
+    x[1, 3:] = -np.inf                  # fewer experts than choices
+    x[2] = torch.finfo(torch.float32).min
+    x[2, 5] = 0.0                       # the lowest value is a value
+    x[3, ::2] = float("nan")
+    x[4, 7] = float("inf")
+    x[5] = float("nan")
+    x[6, 1:] = torch.finfo(torch.float32).min
+    x[7, : E // 2] = -np.inf
+    bias = None
+    if flags & SIG:
+        bias = _bias(E, 3)
+        bias[11] = -np.inf
+    r = _check(gpu, x, 8, bias=bias, groups=groups, top_groups=max(1, groups // 2), flags=flags)
+    assert (r.ids[0] == -1).all() and not r.weights[0].any() and not torch.isnan(r.weights).any()
+    d = taot.route_backward(torch.ones_like(r.weights), x.to(gpu), r.ids, flags=flags)
+    assert torch.isfinite(d).all() and not d[0].any() and not d[5].any()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_odd_addresses(gpu, dtype):
+    x = _logits(9, 256, dtype, seed=1)
+    room = torch.empty(9 * 256 + 1, dtype=dtype, device=gpu)
+    room[1:] = x.reshape(-1).to(gpu)
+    y = room[1:].view(9, 256)
+    for a in (dict(), dict(groups=8, top_groups=4)):
+        r, s = taot.route(x.to(gpu), 8, **a), taot.route(y, 8, **a)
+        assert torch.equal(r.ids, s.ids) and torch.equal(r.weights, s.weights)
+    d = torch.ones_like(r.weights)
+    assert torch.equal(taot.route_backward(d, x.to(gpu), r.ids), taot.route_backward(d, y, r.ids))
+
+
+def test_ids_are_what_the_planner_reads(gpu):
+    B, R, tokens, E, k = 2, 3, 50, 24, 4
+    x = _logits(B * R * tokens, E, torch.bfloat16, seed=9).view(B, R, tokens, E)
+    r = taot.route(x.to(gpu), k, flags=REN)
+    assert r.ids.shape == (B, R, tokens, k)
+    home = (torch.arange(E, dtype=torch.int32, device=gpu) % R).int()
+    loads = taot.plan_loads(r.ids.view(B, R, tokens * k), home, E)
+    n = torch.zeros(B, R, E, dtype=torch.int32)
+    for b in range(B):
+        for q in range(R):
+            n[b, q] = torch.bincount(r.ids[b, q].cpu().long().reshape(-1), minlength=E).int()
+    assert torch.equal(loads.n.cpu(), n) and not loads.bad_ids.any()
+
+
+def _weights64(x, ids, scale, flags):
+    ok = x > -np.inf
+    x = torch.where(ok, x, torch.full_like(x, -np.inf))
+    if flags & REN and not flags & SIG:  # over the chosen alone, so that the others' gradient is 0 and not what 64 bits leave
+        return scale * torch.softmax(x.gather(1, ids), 1)
+    s = torch.sigmoid(x) if flags & SIG else torch.softmax(x, -1)
+    w = s.gather(1, ids)
+    if flags & REN:
+        w = w / (w.sum(1, keepdim=True) + 1e-20)
+    return scale * w
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("T,E,k", [(1, 1, 1), (3, 8, 8), (5, 60, 6), (7, 128, 8), (9, 257, 1), (33, 384, 8),
+                                   (5, 4096, 64), (3, 4104, 8), (2, 32768, 8)])
+@pytest.mark.parametrize("flags", [0, REN, SIG, SIG | REN])
+def test_backward(gpu, dtype, T, E, k, flags):
+    """Each entry: u of the type, and 2e-5 of the terms that make it up (the weights' tolerance)."""
+    x = _logits(T, E, dtype, seed=E + T)
+    r = taot.route(x.to(gpu), k, scale=1.7, flags=flags)
+    dw = torch.randn(T, k, generator=torch.Generator().manual_seed(k))
+    d = taot.route_backward(dw.to(gpu), x.to(gpu), r.ids, scale=1.7, flags=flags)
+    ids = r.ids.cpu().long()
+    z = x.double().requires_grad_()
+    w = _weights64(z, ids, 1.7, flags)
+    want = torch.autograd.grad((w * dw.double()).sum(), z)[0]
+    w = w.detach()
+    # size of the terms of the sum over the choices, for each expert
+    reach = (dw.double().abs() * 1.7).sum(1, keepdim=True)
+    at = torch.zeros(T, E, dtype=torch.float64).scatter_(1, ids, w / 1.7)
+    if flags == 0:
+        at = torch.softmax(x.double(), 1)
+    if flags == SIG:
+        reach = torch.zeros(T, E, dtype=torch.float64).scatter_(1, ids, dw.double().abs() * 1.7)
+    lim = (U[dtype] + 2e-5) * want.abs() + 2e-5 * at * reach + (2.0 ** -25 if dtype == torch.float16 else 0)
+    err = (d.double().cpu() - want).abs()
+    assert (err <= lim).all(), float((err - lim).max())
+    if flags:
+        zero = torch.ones(T, E, dtype=torch.bool).scatter_(1, ids, False)
+        assert not d.cpu()[zero].any()
+
+
+@pytest.mark.parametrize("flags", [0, REN, SIG, SIG | REN])
+def test_backward_against_differences(gpu, flags):
+    T, E, k = 6, 40, 5
+    x = _logits(T, E, torch.float32, seed=4)
+    r = taot.route(x.to(gpu), k, scale=1.3, flags=flags)
+    g = torch.Generator().manual_seed(1)
+    dw, v = torch.randn(T, k, generator=g), torch.randn(T, E, generator=g)
+    d = taot.route_backward(dw.to(gpu), x.to(gpu), r.ids, scale=1.3, flags=flags).double().cpu()
+    ids = r.ids.cpu().long()
+
+    def value(step):
+        return (_weights64(x.double() + step * v.double(), ids, 1.3, flags) * dw.double()).sum()
+
+    want = (value(1e-5) - value(-1e-5)) / 2e-5
+    assert abs(want - (d * v.double()).sum()) <= 2e-5 * (d * v.double()).abs().sum() + 1e-8
+
+
+def test_backward_skips_what_was_not_chosen(gpu):
+    x = _logits(4, 32, torch.float32, seed=2)
+    ids = torch.tensor([[0, 1, -1], [-1, -1, -1], [31, 5, 40], [2, 3, 4]], dtype=torch.int32)
+    for flags in (0, REN, SIG, SIG | REN):
+        d = taot.route_backward(torch.ones(4, 3, device=gpu), x.to(gpu), ids.to(gpu), flags=flags).cpu()
+        assert torch.isfinite(d).all() and not d[1].any()
+        if flags:
+            assert set(d[2].nonzero().flatten().tolist()) <= {31, 5}
+
+
+def test_many_tokens(gpu):
+    """More tokens than one launch has waves: every token once."""
+    x = _logits(70001, 64, torch.bfloat16, seed=11).to(gpu)
+    r = taot.route(x, 4, flags=REN)
+    want = x.float().sort(dim=1, descending=True, stable=True).indices[:, :4].int()
+    assert torch.equal(r.ids, want)
+    d = taot.route_backward(r.weights, x, r.ids, flags=REN)
+    few = torch.cat([taot.route_backward(r.weights[lo:lo + 7000], x[lo:lo + 7000], r.ids[lo:lo + 7000], flags=REN)
+                     for lo in range(0, 70001, 7000)])
+    assert torch.equal(d, few)
+
+
+def test_empty_and_refusals(gpu):
+    x = torch.zeros(4, 16, device=gpu)
+    assert taot.route(x[:0], 4).ids.shape == (0, 4)
+    assert taot.route_backward(torch.zeros(0, 4, device=gpu), x[:0], torch.zeros(0, 4, dtype=torch.int32, device=gpu)).shape == (0, 16)
+    for bad in (dict(top_k=0), dict(top_k=17), dict(top_k=4, groups=3), dict(top_k=4, groups=4, top_groups=5),
+                dict(top_k=5, groups=4, top_groups=1), dict(top_k=4, flags=0x8), dict(top_k=4, scale=float("nan"))):
+        with pytest.raises(taot.TaotError) as e:
+            taot.route(x, **bad)
+        assert e.value.code == 1
+    with pytest.raises(taot.TaotError) as e:
+        taot.route(torch.zeros(1, 100, device=gpu), 65)
+    assert e.value.code == 2
+    with pytest.raises(taot.TaotError) as e:
+        taot.route(torch.zeros(1, 32769, device=gpu), 8)
+    assert e.value.code == 2
+    with pytest.raises(TypeError):
+        taot.route(x.double(), 4)
+    with pytest.raises(TypeError):
+        taot.route(x, 4, bias=torch.zeros(16, dtype=torch.float64, device=gpu))
+    with pytest.raises(ValueError):
+        taot.route(x, 4, bias=torch.zeros(15, device=gpu))
+    with pytest.raises(ValueError):
+        taot.route(x.t(), 4)
+    ids = torch.zeros(4, 2, dtype=torch.int32, device=gpu)
+    with pytest.raises(ValueError):
+        taot.route_backward(torch.zeros(4, 3, device=gpu), x, ids)
