@@ -17,7 +17,8 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 SOURCES = ["csrc/api.hip", "csrc/loads.hip", "csrc/sinkhorn.hip", "csrc/sk_reg_w4g4.hip", "csrc/sk_reg_w2g8.hip",
            "csrc/sk_reg_w2g2.hip", "csrc/sk_dense.hip", "csrc/sk_tier.hip", "csrc/schedule.hip",
-           "csrc/norm.hip", "csrc/route.hip", "csrc/dispatch.hip"]
+           "csrc/norm.hip", "csrc/route.hip", "csrc/route_bf16.hip", "csrc/route_f16.hip",
+           "csrc/route_f32.hip", "csrc/dispatch.hip"]
 LIB = os.path.join(HERE, "libtaot.so")
 PROBES_LIB = os.path.join(HERE, "libtaot_probes.so")
 OBJ_DIR = os.path.join(HERE, "_build")

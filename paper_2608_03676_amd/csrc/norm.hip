@@ -16,7 +16,7 @@ namespace {
 
 constexpr float kF8Max = 448.f;       // largest finite e4m3 value
 constexpr float kF8Floor = 1e-30f;    // a group of smaller values (all zero) has floor / 448 as its scale
-constexpr int kManyRows = 4096;
+constexpr int kRowsOfBlock = 4;       // where a wave holds a row
 
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef __attribute__((aligned(1))) u32x2 u32x2_at;
@@ -43,44 +43,40 @@ __device__ __forceinline__ void store_f8(uint8_t* p, u32x2 v, int n) {
     if (u < n) p[u] = (uint8_t)(v[u / 4] >> (8 * (u % 4)));
 }
 
-// Sum (or maximum) over the WAVES waves of a row.  `slot` alternates between
+// Sum (or maximum) over the `waves` waves of a row.  `slot` alternates between
 // two sets of words from call to call, so one barrier a call is enough.
-template <int WAVES, typename Op>
-__device__ __forceinline__ float row_reduce(float v, Op op, float (*part)[16], int slot) {
+template <typename Op>
+__device__ __forceinline__ float row_reduce(float v, Op op, float (*part)[16], int slot, int waves) {
   v = block_reduce<kWave>(v, op);
-  if constexpr (WAVES > 1) {
-    const int wid = threadIdx.x / kWave;
-    if ((threadIdx.x & (kWave - 1)) == 0) part[slot][wid] = v;
+  if (waves > 1) {
+    if ((threadIdx.x & (kWave - 1)) == 0) part[slot][threadIdx.x / kWave] = v;
     __syncthreads();
     v = part[slot][0];
-#pragma unroll
-    for (int w = 1; w < WAVES; ++w) v = op(v, part[slot][w]);
+    for (int w = 1; w < waves; ++w) v = op(v, part[slot][w]);
   }
   return v;
 }
 
-constexpr int rows_of_block(int waves) { return waves == 1 ? 4 : 1; }
-
-// WAVES waves hold a row; lane l has columns 8 (i LANES + l) .. + 7 for i < CPL,
-// so a wave's accesses are contiguous and a group of 8 m columns is m
-// neighbouring lanes at one i.
-template <typename T, int WAVES, int CPL>
-__global__ void __launch_bounds__(kWave* WAVES* rows_of_block(WAVES))
+// `waves` waves hold a row (one: four rows a block); of their lanes, lane l has
+// columns 8 (i lanes + l) .. + 7 for i < CPL, so a wave's accesses are contiguous
+// and a group of 8 m columns is m neighbouring lanes at one i.
+template <typename T, int CPL>
+__global__ void __launch_bounds__(1024)
 add_rms_norm_kernel(const T* __restrict__ x, const T* __restrict__ residual, const void* __restrict__ weight,
                     bool w_f32, int64_t rows, int32_t H, float eps, int32_t group, T* __restrict__ h,
                     T* __restrict__ y, uint8_t* __restrict__ q, float* __restrict__ scale,
-                    float* __restrict__ rstd) {
-  constexpr int kLanes = WAVES * kWave;
+                    float* __restrict__ rstd, int waves) {
   __shared__ float part[2][16];
-  const int lane = threadIdx.x % kLanes;
-  const int64_t row = (int64_t)blockIdx.x * rows_of_block(WAVES) + threadIdx.x / kLanes;
+  const int lanes = waves * kWave;
+  const int lane = waves == 1 ? threadIdx.x & (kWave - 1) : threadIdx.x;
+  const int64_t row = waves == 1 ? (int64_t)blockIdx.x * kRowsOfBlock + threadIdx.x / kWave : blockIdx.x;
   if (row >= rows) return;  // whole waves, and only where no wave waits for another
   const int64_t at = row * H;
   f32x8 v[CPL];
   float ss = 0.f;
 #pragma unroll
   for (int i = 0; i < CPL; ++i) {
-    const int col = 8 * (i * kLanes + lane), n = H - col;
+    const int col = 8 * (i * lanes + lane), n = H - col;
     v[i] = load_row(x + at + col, n);
     if (residual) v[i] += load_row(residual + at + col, n);
   }
@@ -91,17 +87,17 @@ add_rms_norm_kernel(const T* __restrict__ x, const T* __restrict__ residual, con
   if (h) {
 #pragma unroll
     for (int i = 0; i < CPL; ++i) {
-      const int col = 8 * (i * kLanes + lane);
+      const int col = 8 * (i * lanes + lane);
       store_row(h + at + col, v[i], H - col);
     }
   }
-  const float s = 1.f / sqrtf(row_reduce<WAVES>(ss, SumOp(), part, 0) / (float)H + eps);
+  const float s = 1.f / sqrtf(row_reduce(ss, SumOp(), part, 0, waves) / (float)H + eps);
   if (lane == 0 && rstd) rstd[row] = s;
   float amax = 0.f;
   const int32_t groups = group > 0 ? (H + group - 1) / group : 1;
 #pragma unroll
   for (int i = 0; i < CPL; ++i) {
-    const int col = 8 * (i * kLanes + lane), n = H - col;
+    const int col = 8 * (i * lanes + lane), n = H - col;
     v[i] = v[i] * s * load_row_either<T>(weight, w_f32, col, n);
     if (y) store_row(y + at + col, v[i], n);
     if (q) {
@@ -118,69 +114,92 @@ add_rms_norm_kernel(const T* __restrict__ x, const T* __restrict__ residual, con
     }
   }
   if (q && group == 0) {
-    amax = fmaxf(row_reduce<WAVES>(amax, MaxOp(), part, 1), kF8Floor);
+    amax = fmaxf(row_reduce(amax, MaxOp(), part, 1, waves), kF8Floor);
     const float inv = kF8Max / amax;
     if (lane == 0) scale[row] = amax / kF8Max;
 #pragma unroll
     for (int i = 0; i < CPL; ++i) {
-      const int col = 8 * (i * kLanes + lane);
+      const int col = 8 * (i * lanes + lane);
       store_f8(q + at + col, to_f8(v[i], inv), H - col);
     }
   }
 }
 
-// A worker (WAVES waves) takes rows worker, worker + workers, ... and keeps its
-// share of dw in registers until it writes it as one row of `partial`.
-template <typename T, int WAVES, int CPL>
-__global__ void __launch_bounds__(kWave* WAVES* rows_of_block(WAVES))
+// A worker (`waves` waves) takes rows worker, worker + workers, ... and keeps its
+// share of dw in registers until it writes it as one row of `partial`.  The
+// next row is on its way while the present one is worked on, as long as the
+// registers of 16 waves hold both (CPL <= 2).
+template <typename T, int CPL>
+__global__ void __launch_bounds__(1024)
 add_rms_norm_backward_kernel(const T* __restrict__ dy, const T* __restrict__ dh, const T* __restrict__ h,
                              const float* __restrict__ rstd, const void* __restrict__ weight, bool w_f32,
                              int64_t rows, int32_t H, T* __restrict__ dx, float* __restrict__ partial,
-                             int32_t workers) {
-  constexpr int kLanes = WAVES * kWave;
+                             int32_t workers, int waves) {
+  using Raw = typename Row8<T>::vec;
+  constexpr bool kAhead = CPL <= 2;
   __shared__ float part[2][16];
-  const int lane = threadIdx.x % kLanes;
-  const int32_t worker = blockIdx.x * rows_of_block(WAVES) + threadIdx.x / kLanes;
+  const int lanes = waves * kWave;
+  const int lane = waves == 1 ? threadIdx.x & (kWave - 1) : threadIdx.x;
+  const int32_t worker = waves == 1 ? blockIdx.x * kRowsOfBlock + threadIdx.x / kWave : blockIdx.x;
   if (worker >= workers) return;
   f32x8 dw[CPL];
+  Raw a[CPL], g[CPL], d[CPL], next_a[CPL], next_g[CPL], next_d[CPL];
+  float s = rstd[worker], next_s = 0.f;
+  auto fetch = [&](int64_t row, Raw* to_a, Raw* to_g, Raw* to_d) {
+#pragma unroll
+    for (int i = 0; i < CPL; ++i) {
+      const int col = 8 * (i * lanes + lane), n = H - col;
+      to_a[i] = load_raw(h + row * H + col, n);
+      to_g[i] = load_raw(dy + row * H + col, n);
+      if (dh && kAhead) to_d[i] = load_raw(dh + row * H + col, n);
+    }
+  };
 #pragma unroll
   for (int i = 0; i < CPL; ++i) dw[i] = 0.f;
+  fetch(worker, a, g, d);
   int slot = 0;
   for (int64_t row = worker; row < rows; row += workers) {
-    const int64_t at = row * H;
-    const float s = rstd[row];
-    f32x8 a[CPL], g[CPL];
+    const int64_t then = row + workers < rows ? row + workers : row;
+    if constexpr (kAhead) {
+      next_s = rstd[then];
+      fetch(then, next_a, next_g, next_d);
+    }
     float dot = 0.f;
 #pragma unroll
     for (int i = 0; i < CPL; ++i) {
-      const int col = 8 * (i * kLanes + lane), n = H - col;
-      a[i] = load_row(h + at + col, n);
-      g[i] = load_row(dy + at + col, n);
-    }
-#pragma unroll
-    for (int i = 0; i < CPL; ++i) {
-      const int col = 8 * (i * kLanes + lane), n = H - col;
-      const f32x8 w = load_row_either<T>(weight, w_f32, col, n);
+      const int col = 8 * (i * lanes + lane), n = H - col;
+      const f32x8 w = load_row_either<T>(weight, w_f32, col, n), A = widen(a[i]), G = widen(g[i]);
 #pragma unroll
       for (int u = 0; u < 8; ++u) {
-        dw[i][u] = fmaf(g[i][u], a[i][u] * s, dw[i][u]);
-        g[i][u] *= w[u];
-        dot = fmaf(g[i][u], a[i][u], dot);
+        dw[i][u] = fmaf(G[u], A[u] * s, dw[i][u]);
+        dot = fmaf(G[u] * w[u], A[u], dot);
       }
     }
-    const float c = s * s * (row_reduce<WAVES>(dot, SumOp(), part, slot) / (float)H);
+    const float c = s * s * (row_reduce(dot, SumOp(), part, slot, waves) / (float)H);
     slot ^= 1;
 #pragma unroll
     for (int i = 0; i < CPL; ++i) {
-      const int col = 8 * (i * kLanes + lane), n = H - col;
-      f32x8 r = s * (g[i] - a[i] * c);
-      if (dh) r += load_row(dh + at + col, n);
-      store_row(dx + at + col, r, n);
+      const int col = 8 * (i * lanes + lane), n = H - col;
+      f32x8 r = s * (widen(g[i]) * load_row_either<T>(weight, w_f32, col, n) - widen(a[i]) * c);
+      if (dh) r += kAhead ? widen(d[i]) : load_row(dh + row * H + col, n);
+      store_row(dx + row * H + col, r, n);
+    }
+    if constexpr (kAhead) {
+      s = next_s;
+#pragma unroll
+      for (int i = 0; i < CPL; ++i) {
+        a[i] = next_a[i];
+        g[i] = next_g[i];
+        d[i] = next_d[i];
+      }
+    } else {
+      s = rstd[then];
+      fetch(then, a, g, d);
     }
   }
 #pragma unroll
   for (int i = 0; i < CPL; ++i) {
-    const int col = 8 * (i * kLanes + lane);
+    const int col = 8 * (i * lanes + lane);
     store_row(partial + (int64_t)worker * H + col, dw[i], H - col);
   }
 }
@@ -205,33 +224,32 @@ dweight_kernel(const float* __restrict__ partial, int32_t workers, int32_t H, fl
   }
 }
 
-int32_t backward_workers(int64_t rows) { return (int32_t)(rows < 512 ? rows : 512); }
-
 struct Shape {
   int waves, cpl;
 };
-// Waves and chunks of eight columns per lane that hold a row of H.
-Shape shape_of(int64_t rows, int32_t H) {
+// Waves, and chunks of eight columns per lane, that hold a row of H: as few
+// chunks as 16 waves allow (a row of 4096 in 16 bits, 16384 rows: 116 us with
+// one chunk in 8 waves, 120 with four in two; backward, 98 and 124 with two).
+Shape shape_of(int32_t H) {
   const int chunks = (H + 7) / 8;
-  int waves = 1;
-  if (rows >= kManyRows) {
-    if (chunks > 64 * 8) waves = chunks > 256 * 8 ? 16 : 4;
-  } else {
-    if (chunks > 64) waves = chunks > 256 ? 16 : 4;
-  }
   int cpl = 1;
-  while (cpl * waves * kWave < chunks) cpl *= 2;
-  return {waves, cpl};
+  while (cpl * 16 * kWave < chunks) cpl *= 2;
+  return {(chunks + cpl * kWave - 1) / (cpl * kWave), cpl};
+}
+
+// Workers of the gradient: 16 waves a compute unit.  More would write and read
+// more partial sums, fewer leave loads unissued (32768 rows of 1024: 53 us with
+// half the waves, 48 us; 4096 rows of 8192: 54 us, 62 with twice as many).
+int32_t backward_workers(int64_t rows, int32_t H) {
+  const int64_t most = 4096 / shape_of(H).waves;
+  return (int32_t)(rows < most ? rows : most);
 }
 
 template <typename F>
-bool with_shape(Shape s, F f) {
-#define TAOT_SHAPE(W, C) \
-  if (s.waves == W && s.cpl == C) return f(std::integral_constant<int, W>(), std::integral_constant<int, C>())
-  TAOT_SHAPE(1, 1); TAOT_SHAPE(1, 2); TAOT_SHAPE(1, 4); TAOT_SHAPE(1, 8);
-  TAOT_SHAPE(4, 1); TAOT_SHAPE(4, 2); TAOT_SHAPE(4, 4); TAOT_SHAPE(4, 8);
-  TAOT_SHAPE(16, 1); TAOT_SHAPE(16, 2); TAOT_SHAPE(16, 4);
-#undef TAOT_SHAPE
+bool with_chunks(int cpl, F f) {
+  if (cpl == 1) return f(std::integral_constant<int, 1>());
+  if (cpl == 2) return f(std::integral_constant<int, 2>());
+  if (cpl == 4) return f(std::integral_constant<int, 4>());
   return false;
 }
 
@@ -239,11 +257,12 @@ template <typename T>
 taot_status forward(const void* x, const void* residual, const void* weight, bool w_f32, int64_t rows, int32_t H,
                     float eps, int32_t group, void* h, void* y, uint8_t* q, float* scale, float* rstd,
                     hipStream_t stream) {
-  const bool ok = with_shape(shape_of(rows, H), [&](auto W, auto C) {
-    constexpr int w = W.value, c = C.value, per = rows_of_block(w);
-    add_rms_norm_kernel<T, w, c><<<(unsigned)((rows + per - 1) / per), kWave * w * per, 0, stream>>>(
+  const Shape s = shape_of(H);
+  const int per = s.waves == 1 ? kRowsOfBlock : 1;
+  const bool ok = with_chunks(s.cpl, [&](auto C) {
+    add_rms_norm_kernel<T, C.value><<<(unsigned)((rows + per - 1) / per), kWave * s.waves * per, 0, stream>>>(
         static_cast<const T*>(x), static_cast<const T*>(residual), weight, w_f32, rows, H, eps, group,
-        static_cast<T*>(h), static_cast<T*>(y), q, scale, rstd);
+        static_cast<T*>(h), static_cast<T*>(y), q, scale, rstd, s.waves);
     return true;
   });
   return ok && hipGetLastError() == hipSuccess ? TAOT_OK : TAOT_ERR_LAUNCH;
@@ -252,14 +271,16 @@ taot_status forward(const void* x, const void* residual, const void* weight, boo
 template <typename T>
 taot_status backward(const void* dy, const void* dh, const void* h, const float* rstd, const void* weight, bool w_f32,
                      int64_t rows, int32_t H, void* dx, float* dweight, float* partial, hipStream_t stream) {
-  const int32_t workers = backward_workers(rows);
+  const int32_t workers = backward_workers(rows, H);
   bool ok = true;
   if (rows > 0) {
-    ok = with_shape(shape_of(rows, H), [&](auto W, auto C) {
-      constexpr int w = W.value, c = C.value, per = rows_of_block(w);
-      add_rms_norm_backward_kernel<T, w, c><<<(unsigned)((workers + per - 1) / per), kWave * w * per, 0, stream>>>(
-          static_cast<const T*>(dy), static_cast<const T*>(dh), static_cast<const T*>(h), rstd, weight, w_f32, rows,
-          H, static_cast<T*>(dx), partial, workers);
+    const Shape s = shape_of(H);
+    const int per = s.waves == 1 ? kRowsOfBlock : 1;
+    ok = with_chunks(s.cpl, [&](auto C) {
+      add_rms_norm_backward_kernel<T, C.value>
+          <<<(unsigned)((workers + per - 1) / per), kWave * s.waves * per, 0, stream>>>(
+              static_cast<const T*>(dy), static_cast<const T*>(dh), static_cast<const T*>(h), rstd, weight, w_f32,
+              rows, H, static_cast<T*>(dx), partial, workers, s.waves);
       return true;
     });
   }
@@ -271,7 +292,7 @@ taot_status backward(const void* dy, const void* dh, const void* h, const float*
 
 size_t add_rms_norm_backward_ws(int64_t rows, int32_t H) {
   Carver c{nullptr};
-  c.take<float>((size_t)backward_workers(rows) * (size_t)H);
+  c.take<float>((size_t)backward_workers(rows, H) * (size_t)H);
   return c.off;
 }
 
@@ -292,7 +313,7 @@ taot_status launch_add_rms_norm_backward(const void* dy, const void* dh, const v
                                          hipStream_t stream) {
   const bool f32 = weight_dtype == TAOT_F32;
   Carver c{static_cast<char*>(ws)};
-  float* partial = c.take<float>((size_t)backward_workers(rows) * (size_t)H);
+  float* partial = c.take<float>((size_t)backward_workers(rows, H) * (size_t)H);
   if (dtype == TAOT_BF16)
     return backward<__bf16>(dy, dh, h, rstd, weight, f32, rows, H, dx, dweight, partial, stream);
   if (dtype == TAOT_F16)

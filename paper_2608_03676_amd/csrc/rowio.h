@@ -17,25 +17,22 @@ struct Row8 {
   typedef __attribute__((aligned(sizeof(T)))) vec at;
 };
 
+// n values from p, as they are (n of 8 and more: eight; 0 and less: none), zeros behind them.
 template <typename T>
-__device__ __forceinline__ f32x8 load8(const T* p) {
-  return __builtin_convertvector(*reinterpret_cast<const typename Row8<T>::at*>(p), f32x8);
-}
-
-// The first n of eight values (n < 8), zeros behind them.
-template <typename T>
-__device__ __forceinline__ f32x8 load_head(const T* p, int n) {
-  f32x8 v;
+__device__ __forceinline__ typename Row8<T>::vec load_raw(const T* p, int n) {
+  if (n >= 8) return *reinterpret_cast<const typename Row8<T>::at*>(p);
+  typename Row8<T>::vec v;
 #pragma unroll
-  for (int u = 0; u < 8; ++u) v[u] = u < n ? (float)p[u] : 0.f;
+  for (int u = 0; u < 8; ++u) v[u] = u < n ? p[u] : (T)0.f;
   return v;
 }
-
-// n values from p (0 and less: none), zeros behind them.
+template <typename V>
+__device__ __forceinline__ f32x8 widen(V v) {
+  return __builtin_convertvector(v, f32x8);
+}
 template <typename T>
 __device__ __forceinline__ f32x8 load_row(const T* p, int n) {
-  if (n >= 8) return load8(p);
-  return load_head(p, n);
+  return widen(load_raw(p, n));
 }
 
 // Rounds to nearest even.
@@ -66,23 +63,30 @@ template <int S>
 __device__ __forceinline__ int lane_step(int v) {
   static_assert(S >= 0 && S < 4, "steps within a row of 16 lanes");
   constexpr int ctrl = S == 0 ? 0xB1 : S == 1 ? 0x4E : S == 2 ? 0x141 : 0x140;
-  return __builtin_amdgcn_mov_dpp(v, ctrl, 0xF, 0xF, false);
+  return __builtin_amdgcn_mov_dpp(v, ctrl, 0xF, 0xF, true);
 }
 template <int S>
 __device__ __forceinline__ float lane_step(float v) {
   return __int_as_float(lane_step<S>(__float_as_int(v)));
 }
 
+// The value of one lane, the same for all.
+__device__ __forceinline__ int lane_value(int v, int lane) { return __builtin_amdgcn_readlane(v, lane); }
+__device__ __forceinline__ float lane_value(float v, int lane) {
+  return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), lane));
+}
+
 // Result of `op` over blocks of L neighbouring lanes (L a power of two), in
-// every lane of the block; op has to commute.  The order is fixed.
+// every lane of the block; op has to commute.  The order is fixed.  A whole
+// wave's four rows of 16 lanes meet in scalar registers.
 template <int L, typename V, typename Op>
 __device__ __forceinline__ V block_reduce(V v, Op op) {
   if constexpr (L >= 2) v = op(v, lane_step<0>(v));
   if constexpr (L >= 4) v = op(v, lane_step<1>(v));
   if constexpr (L >= 8) v = op(v, lane_step<2>(v));
   if constexpr (L >= 16) v = op(v, lane_step<3>(v));
-  if constexpr (L >= 32) v = op(v, __shfl_xor(v, 16, kWave));
-  if constexpr (L >= 64) v = op(v, __shfl_xor(v, 32, kWave));
+  if constexpr (L == 32) v = op(v, __shfl_xor(v, 16, kWave));
+  if constexpr (L == 64) v = op(op(lane_value(v, 0), lane_value(v, 16)), op(lane_value(v, 32), lane_value(v, 48)));
   return v;
 }
 
