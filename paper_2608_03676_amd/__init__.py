@@ -99,6 +99,11 @@ def _stream(stream) -> ctypes.c_void_p:
     return ctypes.c_void_p(s.cuda_stream)
 
 
+def _queue(stream, device) -> int:
+    """The handle of the stream, or of the device's current one (without a torch.cuda.Stream for it: 3 us a call)."""
+    return torch._C._cuda_getCurrentRawStream(device.index) if stream is None else stream.cuda_stream
+
+
 def _dev(t: torch.Tensor, name: str, dtype) -> torch.Tensor:
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise TypeError(f"{name} must be a GPU tensor")
@@ -313,8 +318,6 @@ def _shape(t: torch.Tensor, name: str, shape):
 def _empty(shape, dtype, device, stream) -> torch.Tensor:
     """New memory of the stream that the call's work goes to: what used it before is done when that work begins, and
     it is not handed out again before that work is done."""
-    if stream is None:
-        return torch.empty(shape, dtype=dtype, device=device)
     with torch.cuda.stream(stream):
         return torch.empty(shape, dtype=dtype, device=device)
 
@@ -322,14 +325,14 @@ def _empty(shape, dtype, device, stream) -> torch.Tensor:
 def _into(t: Optional[torch.Tensor], name: str, shape, dtype, device, stream) -> torch.Tensor:
     """The caller's output tensor, checked, or a new one."""
     if t is None:
-        return _empty(shape, dtype, device, stream)
+        return torch.empty(shape, dtype=dtype, device=device) if stream is None else _empty(shape, dtype, device, stream)
     _shape(_dev(t, name, dtype), name, shape)
     return t
 
 
 def _room(workspace: Optional[torch.Tensor], nbytes: int, device, stream) -> torch.Tensor:
     if workspace is None:
-        return _empty((max(int(nbytes), 1),), torch.uint8, device, stream)
+        return _into(None, "workspace", (max(int(nbytes), 1),), torch.uint8, device, stream)
     if not workspace.is_cuda or not workspace.is_contiguous():
         raise ValueError("workspace must be a contiguous GPU tensor")
     return workspace
@@ -371,7 +374,7 @@ def add_rms_norm(x: torch.Tensor, weight: torch.Tensor, eps: float, residual: Op
     _check("taot_add_rms_norm", lib().taot_add_rms_norm(
         x.data_ptr(), _ptr(residual), weight.data_ptr(), T, H, _DTYPE[x.dtype], _DTYPE[weight.dtype], float(eps),
         int(group or 0), None if residual is None else out.h.data_ptr(), out.y.data_ptr(), _ptr(q), _ptr(s),
-        out.rstd.data_ptr(), _stream(stream)))
+        out.rstd.data_ptr(), _queue(stream, dev)))
     return out
 
 
@@ -403,7 +406,7 @@ def add_rms_norm_backward(dy: torch.Tensor, h: torch.Tensor, rstd: torch.Tensor,
     _check("taot_add_rms_norm_backward", lib().taot_add_rms_norm_backward(
         dy.data_ptr(), _ptr(dh), h.data_ptr(), rstd.data_ptr(), weight.data_ptr(), T, H, _DTYPE[h.dtype],
         _DTYPE[weight.dtype], out.dx.data_ptr(), out.dweight.data_ptr(), ws.data_ptr(),
-        ws.numel() * ws.element_size(), _stream(stream)))
+        ws.numel() * ws.element_size(), _queue(stream, h.device)))
     return out
 
 
@@ -430,7 +433,7 @@ def route(logits: torch.Tensor, top_k: int, bias: Optional[torch.Tensor] = None,
     T = logits.numel() // E if E else 0
     _check("taot_route", lib().taot_route(
         logits.data_ptr(), _ptr(bias), T, E, int(top_k), int(groups), int(top_groups), float(scale), int(flags),
-        _DTYPE[logits.dtype], out.ids.data_ptr(), out.weights.data_ptr(), _stream(stream)))
+        _DTYPE[logits.dtype], out.ids.data_ptr(), out.weights.data_ptr(), _queue(stream, logits.device)))
     return out
 
 
@@ -447,7 +450,7 @@ def route_backward(dweights: torch.Tensor, logits: torch.Tensor, ids: torch.Tens
     T = logits.numel() // E if E else 0
     _check("taot_route_backward", lib().taot_route_backward(
         dweights.data_ptr(), logits.data_ptr(), ids.data_ptr(), T, E, top_k, float(scale), int(flags),
-        _DTYPE[logits.dtype], out.data_ptr(), _stream(stream)))
+        _DTYPE[logits.dtype], out.data_ptr(), _queue(stream, logits.device)))
     return out
 
 
@@ -486,7 +489,7 @@ def dispatch_map(ids: torch.Tensor, home: torch.Tensor, slot_expert: torch.Tenso
     _check("taot_dispatch_map", lib().taot_dispatch_map(
         ids.data_ptr(), B, rows, int(rank0), N, home.data_ptr(), R, E, int(K), slot_expert.data_ptr(), X.data_ptr(),
         out.pos.data_ptr(), out.offsets.data_ptr(), out.sends.data_ptr(), out.status.data_ptr(), ws.data_ptr(),
-        ws.numel() * ws.element_size(), _stream(stream)))
+        ws.numel() * ws.element_size(), _queue(stream, dev)))
     return out
 
 
@@ -520,7 +523,7 @@ def dispatch_rows(x: torch.Tensor, pos: torch.Tensor, scale: Optional[torch.Tens
         more = 4 * scale.shape[-1]
     _check("taot_dispatch_rows", lib().taot_dispatch_rows(
         x.data_ptr(), x.shape[-1] * x.element_size(), _ptr(scale), more, rows, tokens, k, pos.data_ptr(),
-        out.data_ptr(), _ptr(out_scale) if scale is not None else None, _stream(stream)))
+        out.data_ptr(), _ptr(out_scale) if scale is not None else None, _queue(stream, x.device)))
     return out if scale is None else (out, out_scale)
 
 
@@ -540,7 +543,7 @@ def combine_rows(y: torch.Tensor, pos: torch.Tensor, weights: Optional[torch.Ten
     rows, tokens, _ = _tokens(pos, lead, "y")
     _check("taot_combine_rows", lib().taot_combine_rows(
         y.data_ptr(), pos.data_ptr(), _ptr(weights), rows, tokens, int(top_k), H, _DTYPE[y.dtype], out.data_ptr(),
-        _stream(stream)))
+        _queue(stream, y.device)))
     return out
 
 
@@ -571,7 +574,7 @@ def combine_rows_backward(dout: torch.Tensor, y: torch.Tensor, pos: torch.Tensor
     out.dweights = _into(out.dweights, "out.dweights", weights.shape, torch.float32, y.device, stream)
     _check("taot_combine_rows_backward", lib().taot_combine_rows_backward(
         dout.data_ptr(), y.data_ptr(), pos.data_ptr(), weights.data_ptr(), rows, tokens, k, H, _DTYPE[y.dtype],
-        out.dy.data_ptr(), out.dweights.data_ptr(), _stream(stream)))
+        out.dy.data_ptr(), out.dweights.data_ptr(), _queue(stream, y.device)))
     return out
 
 

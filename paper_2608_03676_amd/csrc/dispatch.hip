@@ -11,33 +11,52 @@
 // sort: integers, and the same on every run.
 //
 // Kernels
-//   lists_kernel  (B + 1 blocks)  slots of each expert; experts of each rank
-//   count_kernel  (a wave per chunk of a row)  copies of each expert in the chunk
-//   bases_kernel  (a thread per row and expert)  running sums over the chunks
+//   count_kernel  (a wave per chunk of a row)  copies of each expert in the chunk;
+//                 its first B + 1 blocks: slots of each expert, experts of each rank
+//   bases_kernel  (16 threads per row and expert)  running sums over the chunks
 //   tables_kernel (a block per row)  slots' shares, instance offsets, sends
 //   place_kernel  (a wave per chunk)  occurrence by occurrence to a position
+//   row_kernel    (a block per row)  all of these for a short row, in one launch
 //   rows_kernel, combine_kernel, combine_backward_kernel  (one or four waves a token)
+#include <stdlib.h>
 #include "rowio.h"
 
 namespace taot {
 namespace {
 
-constexpr int kListThreads = 1024;
+constexpr int kThreads = 256, kTableThreads = 1024;
 constexpr int kUnroll = 4;
-constexpr int32_t kChunkMin = 1024, kChunkMax = 32768;
-constexpr int64_t kWavesWanted = 16384;
+constexpr int32_t kChunkMin = 256, kChunkMax = 32768;
+constexpr int64_t kWavesWanted = 8192;
+constexpr size_t kTableLds = 32768;  // a row's tables are kept in LDS up to this size
+constexpr int64_t kRowIds = 8192;    // rows up to this length are done by one block
+constexpr size_t kRowLds = 65536;
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((aligned(1))) u32x4 u32x4_at;
 
-// Lanes of the wave (among `valid`) that hold the same key, of `bits` bits.
-__device__ __forceinline__ uint64_t same_key(uint32_t key, int bits, uint64_t valid) {
-  uint64_t m = valid;
-  for (int b = 0; b < bits; ++b) {
-    const bool s = (key >> b) & 1u;
-    const uint64_t v = __ballot(s);
-    m &= s ? v : ~v;
-  }
+// Lanes of the wave (among `valid`) that hold the same key, of `bits` bits, as two halves.
+struct Same {
+  uint32_t lo, hi;
+  __device__ __forceinline__ int below() const { return (int)__builtin_amdgcn_mbcnt_hi(hi, __builtin_amdgcn_mbcnt_lo(lo, 0)); }
+  __device__ __forceinline__ int all() const { return __popc(lo) + __popc(hi); }
+};
+__device__ __forceinline__ void same_bit(Same& m, uint32_t key, int b) {
+  const uint32_t s = (uint32_t)__builtin_amdgcn_sbfe((int32_t)key, b, 1);  // the bit, everywhere
+  const uint64_t v = __ballot(s != 0);
+  m.lo &= ~((uint32_t)v ^ s);
+  m.hi &= ~((uint32_t)(v >> 32) ^ s);
+}
+__device__ __forceinline__ Same same_key(uint32_t key, int bits, uint64_t valid) {
+  Same m{(uint32_t)valid, (uint32_t)(valid >> 32)};
+  for (int b = 0; b < bits; ++b) same_bit(m, key, b);
+  return m;
+}
+template <int BITS>
+__device__ __forceinline__ Same same_key(uint32_t key, uint64_t valid) {
+  Same m{(uint32_t)valid, (uint32_t)(valid >> 32)};
+#pragma unroll
+  for (int b = 0; b < BITS; ++b) same_bit(m, key, b);
   return m;
 }
 
@@ -48,8 +67,8 @@ __host__ __device__ inline int bits_for(uint32_t n) {
   return b;
 }
 
-// Exclusive sum over a block of kListThreads threads; *total gets the block's.
-template <typename V>
+// Exclusive sum over a block of NT threads; *total gets the block's.
+template <int NT, typename V>
 __device__ __forceinline__ V block_exclusive(V v, V* part, V* total) {
   const int lane = threadIdx.x & (kWave - 1), wid = threadIdx.x / kWave;
   V incl = v;
@@ -62,7 +81,7 @@ __device__ __forceinline__ V block_exclusive(V v, V* part, V* total) {
   if (lane == kWave - 1) part[wid] = incl;
   __syncthreads();
   V off = incl - v, all = 0;
-  for (int w = 0; w < kListThreads / kWave; ++w) {
+  for (int w = 0; w < NT / kWave; ++w) {
     off += w < wid ? part[w] : (V)0;
     all += part[w];
   }
@@ -70,22 +89,23 @@ __device__ __forceinline__ V block_exclusive(V v, V* part, V* total) {
   return off;
 }
 
-// Stable order of n keys in [0, nkeys]: first[q] = keys below q (q <= nkeys),
-// place(i, position).  cnt: nkeys + 1 words of LDS.
-template <typename Key, typename Place>
-__device__ void stable_order(int32_t n, int32_t nkeys, Key key, Place place, int32_t* __restrict__ first, int32_t* cnt) {
-  __shared__ int32_t part[kListThreads / kWave];
+// Stable order of n keys in [0, nkeys] by a block of NT threads: first[q] = keys
+// below q (q <= nkeys), put(i, its key, position).  cnt: nkeys + 1 words of LDS.  The
+// first wave places; no barrier behind it.
+template <int NT, typename Key, typename Put>
+__device__ __forceinline__ void stable_order(int32_t n, int32_t nkeys, Key key, Put put, int32_t* first,
+                                             int32_t* cnt, int32_t* part) {
   const int tid = threadIdx.x, lane = tid & (kWave - 1);
-  for (int32_t q = tid; q <= nkeys; q += kListThreads) cnt[q] = 0;
+  for (int32_t q = tid; q <= nkeys; q += NT) cnt[q] = 0;
   __syncthreads();
-  for (int32_t i = tid; i < n; i += kListThreads) atomicAdd(&cnt[key(i)], 1);
+  for (int32_t i = tid; i < n; i += NT) atomicAdd(&cnt[key(i)], 1);
   __syncthreads();
   int32_t run = 0;
-  for (int32_t q0 = 0; q0 <= nkeys; q0 += kListThreads) {
+  for (int32_t q0 = 0; q0 <= nkeys; q0 += NT) {
     const int32_t q = q0 + tid;
     int32_t total;
     const int32_t mine = q <= nkeys ? cnt[q] : 0;
-    const int32_t at = run + block_exclusive(mine, part, &total);
+    const int32_t at = run + block_exclusive<NT>(mine, part, &total);
     if (q <= nkeys) {
       cnt[q] = at;
       first[q] = at;
@@ -95,73 +115,104 @@ __device__ void stable_order(int32_t n, int32_t nkeys, Key key, Place place, int
   __syncthreads();
   if (tid >= kWave) return;
   const int bits = bits_for((uint32_t)nkeys);
+  int32_t next = lane < n ? key(lane) : nkeys;
   for (int32_t i0 = 0; i0 < n; i0 += kWave) {
-    const int32_t i = i0 + lane;
+    const int32_t i = i0 + lane, q = next;
     const bool in = i < n;
-    const int32_t q = in ? key(i) : nkeys;
-    const uint64_t m = same_key((uint32_t)q, bits, __ballot(in));
-    const int before = __popcll(m & ((1ull << lane) - 1));
-    if (in) {
-      const int32_t at = cnt[q] + before;
-      place(i, at);
-    }
+    next = i + kWave < n ? key(i + kWave) : nkeys;
+    const Same m = same_key((uint32_t)q, bits, __ballot(in));
+    const int before = m.below();
+    const int32_t at = cnt[q] + before;
+    if (in) put(i, q, at);
     __builtin_amdgcn_wave_barrier();
-    if (in && (m >> lane) == 1) cnt[q] += before + 1;  // the last lane of the key
+    if (in && before + 1 == m.all()) cnt[q] = at + 1;  // the last lane of the key
     __builtin_amdgcn_wave_barrier();
   }
 }
 
-// Block b < B: slots of problem b by expert.  Block B: experts by home rank.
-__global__ void __launch_bounds__(kListThreads)
-lists_kernel(const int32_t* __restrict__ home, const int32_t* __restrict__ slot_expert, int32_t B, int32_t R,
-             int32_t E, int32_t K, int32_t* __restrict__ own_at, int32_t* __restrict__ rank_first,
-             int32_t* __restrict__ slot_first, int32_t* __restrict__ slot_of, uint32_t* __restrict__ status) {
-  extern __shared__ int32_t cnt[];
-  __shared__ int32_t bad;
-  const int32_t S = R * K, b = blockIdx.x;
-  if (b == B) {
-    auto key = [&](int32_t e) {
-      const int32_t h = home[e];
-      return h >= 0 && h < R ? h : R;
-    };
-    stable_order(E, R, key, [&](int32_t e, int32_t at) { own_at[e] = at + K * key(e); }, rank_first, cnt);
-    return;
-  }
-  const int32_t* slots = slot_expert + (int64_t)b * S;
-  if (threadIdx.x == 0) bad = 0;
-  __syncthreads();
-  for (int32_t e = threadIdx.x; e < E; e += kListThreads)
-    if (home[e] < 0 || home[e] >= R) bad = 1;
-  __syncthreads();
-  if (threadIdx.x == 0 && status) status[b] = bad ? TAOT_ST_BAD_INPUT : 0u;
+struct Lists {
+  const int32_t* home;
+  const int32_t* slot_expert;
+  int32_t* own_at;
+  int32_t* rank_first;
+  int32_t* slot_first;
+  int32_t* slot_of;
+  uint32_t* status;
+};
+
+template <int NT>
+__device__ __forceinline__ void order_experts(const int32_t* home, int32_t R, int32_t E, int32_t K, int32_t* own_at,
+                                              int32_t* rank_first, int32_t* cnt, int32_t* part) {
+  auto key = [&](int32_t e) {
+    const int32_t h = home[e];
+    return h >= 0 && h < R ? h : R;
+  };
+  stable_order<NT>(E, R, key, [&](int32_t e, int32_t h, int32_t at) { own_at[e] = at + K * h; }, rank_first, cnt, part);
+}
+
+template <int NT>
+__device__ __forceinline__ void order_slots(const int32_t* slots, int32_t S, int32_t E, int32_t* slot_first,
+                                            int32_t* slot_of, int32_t* cnt, int32_t* part) {
   auto key = [&](int32_t s) {
     const int32_t e = slots[s];
     return e >= 0 && e < E ? e : E;
   };
-  stable_order(S, E, key, [&](int32_t s, int32_t at) { slot_of[(int64_t)b * S + at] = s; },
-               slot_first + (int64_t)b * (E + 1), cnt);
+  stable_order<NT>(S, E, key, [&](int32_t s, int32_t, int32_t at) { slot_of[at] = s; }, slot_first, cnt, part);
 }
 
-// hist[row][chunk][e]: copies of expert e in the chunk; e = E: ids that are no expert.
-__global__ void __launch_bounds__(256)
-count_kernel(const int32_t* __restrict__ ids, int64_t N, int32_t E, int32_t chunk, int32_t chunks, int64_t jobs,
-             int32_t* __restrict__ hist) {
+// Block b < B: slots of problem b by expert.  Block B: experts by home rank.
+__device__ void lists(const Lists& l, int32_t b, int32_t B, int32_t R, int32_t E, int32_t K, int32_t* cnt) {
+  __shared__ int32_t part[kThreads / kWave];
+  __shared__ int32_t bad;
+  const int32_t S = R * K;
+  if (b == B) {
+    order_experts<kThreads>(l.home, R, E, K, l.own_at, l.rank_first, cnt, part);
+    return;
+  }
+  if (threadIdx.x == 0) bad = 0;
+  __syncthreads();
+  for (int32_t e = threadIdx.x; e < E; e += kThreads)
+    if (l.home[e] < 0 || l.home[e] >= R) bad = 1;
+  __syncthreads();
+  if (threadIdx.x == 0 && l.status) l.status[b] = bad ? TAOT_ST_BAD_INPUT : 0u;
+  order_slots<kThreads>(l.slot_expert + (int64_t)b * S, S, E, l.slot_first + (int64_t)b * (E + 1),
+                        l.slot_of + (int64_t)b * S, cnt, part);
+}
+
+// hist[row][chunk][e]: copies of expert e in the chunk; e = E: ids that are no
+// expert.  The lists do not depend on the counts and take longer to start than to
+// finish, so they ride along.
+__global__ void __launch_bounds__(kThreads)
+count_kernel(Lists l, int32_t B, int32_t R, int32_t K, const int32_t* __restrict__ ids, int64_t N, int32_t E,
+             int32_t chunk, int32_t chunks, int64_t jobs, int waves, int32_t* __restrict__ hist) {
   extern __shared__ int32_t cnt[];
-  const int lane = threadIdx.x & (kWave - 1);
-  const int64_t job = (int64_t)blockIdx.x * (blockDim.x / kWave) + threadIdx.x / kWave;
-  if (job >= jobs) return;
-  int32_t* mine = cnt + (threadIdx.x / kWave) * (E + 1);
+  if ((int32_t)blockIdx.x <= B) {
+    lists(l, (int32_t)blockIdx.x, B, R, E, K, cnt);
+    return;
+  }
+  const int lane = threadIdx.x & (kWave - 1), wid = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const int64_t job = ((int64_t)blockIdx.x - B - 1) * waves + wid;
+  if (wid >= waves || job >= jobs) return;
+  int32_t* mine = cnt + wid * (E + 1);
   const int64_t row = job / chunks, lo = (job % chunks) * (int64_t)chunk;
   const int32_t n = (int32_t)min((int64_t)chunk, N - lo);
   const int32_t* src = ids + row * N + lo;
   for (int32_t e = lane; e <= E; e += kWave) mine[e] = 0;
   __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
   __builtin_amdgcn_wave_barrier();
-#pragma unroll 8
-  for (int32_t i = lane; i < n; i += kWave) {
-    const int32_t e = src[i];
-    atomicAdd(&mine[(uint32_t)e < (uint32_t)E ? e : E], 1);
+  auto count = [&](int32_t e) { atomicAdd(&mine[(uint32_t)e < (uint32_t)E ? e : E], 1); };
+  typedef int32_t four __attribute__((ext_vector_type(4)));
+  typedef __attribute__((aligned(4))) four four_at;
+  const int32_t n4 = n / 4;  // the order does not matter here: four ids a load
+#pragma unroll 4
+  for (int32_t i = lane; i < n4; i += kWave) {
+    const four v = *reinterpret_cast<const four_at*>(src + 4 * i);
+    count(v.x);
+    count(v.y);
+    count(v.z);
+    count(v.w);
   }
+  if (4 * n4 + lane < n) count(src[4 * n4 + lane]);
   __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
   __builtin_amdgcn_wave_barrier();
   int32_t* dst = hist + job * (E + 1);
@@ -169,29 +220,52 @@ count_kernel(const int32_t* __restrict__ ids, int64_t N, int32_t E, int32_t chun
 }
 
 // hist becomes the copies of e before the chunk; total[row][e] those of the row.
-__global__ void __launch_bounds__(256)
-bases_kernel(int32_t* __restrict__ hist, int32_t E, int32_t chunks, int64_t entries, int32_t* __restrict__ total) {
-  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (i >= entries) return;
-  const int64_t row = i / (E + 1), e = i % (E + 1);
+// A block has 64 experts of a row, 16 threads each, which share the chunks and
+// hold up to kHeld counts each.
+constexpr int kBaseThreads = 1024, kHeld = 8;
+__global__ void __launch_bounds__(kBaseThreads)
+bases_kernel(int32_t* __restrict__ hist, int32_t E, int32_t chunks, int32_t* __restrict__ total) {
+  constexpr int kGroups = kBaseThreads / kWave;
+  __shared__ int32_t part[kGroups][kWave];
+  const int32_t tiles = (E + kWave) / kWave;
+  const int64_t row = blockIdx.x / tiles;
+  const int32_t c = threadIdx.x % kWave, g = threadIdx.x / kWave, e = (int32_t)(blockIdx.x % tiles) * kWave + c;
+  const int32_t each = (chunks + kGroups - 1) / kGroups, lo = min(g * each, chunks), hi = min(lo + each, chunks);
   int32_t* h = hist + row * chunks * (E + 1) + e;
-  int32_t run = 0, c = 0;
-  for (; c + 8 <= chunks; c += 8) {
-    int32_t v[8];
+  int32_t sum = 0, v[kHeld];
+  const bool held = each <= kHeld;
+  if (e <= E) {
+    if (held) {
 #pragma unroll
-    for (int u = 0; u < 8; ++u) v[u] = h[(int64_t)(c + u) * (E + 1)];
+      for (int u = 0; u < kHeld; ++u) v[u] = lo + u < hi ? h[(int64_t)(lo + u) * (E + 1)] : 0;
 #pragma unroll
-    for (int u = 0; u < 8; ++u) {
-      h[(int64_t)(c + u) * (E + 1)] = run;
-      run += v[u];
+      for (int u = 0; u < kHeld; ++u) sum += v[u];
+    } else {
+#pragma unroll 8
+      for (int32_t k = lo; k < hi; ++k) sum += h[(int64_t)k * (E + 1)];
     }
   }
-  for (; c < chunks; ++c) {
-    const int32_t v = h[(int64_t)c * (E + 1)];
-    h[(int64_t)c * (E + 1)] = run;
-    run += v;
+  part[g][c] = sum;
+  __syncthreads();
+  if (e > E) return;
+  int32_t run = 0;
+#pragma unroll
+  for (int w = 0; w < kGroups; ++w) run += w < g ? part[w][c] : 0;
+  if (held) {
+#pragma unroll
+    for (int u = 0; u < kHeld; ++u) {
+      if (lo + u < hi) h[(int64_t)(lo + u) * (E + 1)] = run;
+      run += v[u];
+    }
+  } else {
+#pragma unroll 8
+    for (int32_t k = lo; k < hi; ++k) {
+      const int32_t x = h[(int64_t)k * (E + 1)];
+      h[(int64_t)k * (E + 1)] = run;
+      run += x;
+    }
   }
-  total[i] = run;
+  if (g == kGroups - 1) total[row * (E + 1) + e] = run;
 }
 
 struct Tables {
@@ -201,154 +275,303 @@ struct Tables {
   const int32_t* slot_of;     // [B][S]       slots by expert
   const int32_t* total;       // [rows][E + 1]
   int64_t* upto;              // [rows][S + 1]  running sum of X over the slots by expert
-  int32_t* slot_before;       // [rows][S]    copies of the expert that slots before take
-  int32_t* slot_base;         // [rows][S]    position of occurrence 0, were it the slot's
+  int2* guest;                // [rows][S]    of the slots by expert: copies of the expert that slots before take,
+                              //              and the position of its occurrence 0, were it this slot's
   int2* own;                  // [rows][E]    copies at guests; position of occurrence 0, were it at home
   int32_t* placed;            // [rows]       copies that go somewhere
 };
 
-__global__ void __launch_bounds__(kListThreads)
-tables_kernel(Tables t, const int32_t* __restrict__ X, int64_t N, int32_t rows, int32_t rank0, int32_t R, int32_t E,
-              int32_t K, int32_t* __restrict__ offsets, int32_t* __restrict__ sends, uint32_t* __restrict__ status) {
-  __shared__ int64_t part64[kListThreads / kWave];
-  __shared__ int32_t part[kListThreads / kWave];
-  const int tid = threadIdx.x;
-  const int64_t row = blockIdx.x, b = row / rows;
-  const int32_t S = R * K, I = E + S, r = rank0 + (int32_t)(row % rows);
-  const int32_t* first = t.slot_first + b * (E + 1);
-  const int32_t* slot_of = t.slot_of + b * S;
-  const int32_t* total = t.total + row * (E + 1);
-  const int32_t* share = X + (b * R + r) * (int64_t)S;
-  int64_t* upto = t.upto + row * (S + 1);
-  int32_t* before = t.slot_before + row * S;
-  int32_t* base = t.slot_base + row * S;
-  int2* own = t.own + row * E;
-  int32_t* off = offsets + row * (I + 1);
-  const int32_t filled = S > 0 ? first[E] : 0;
-  auto guest_at = [&](int32_t s) { return s + t.rank_first[s / K + 1]; };
+// What a row's tables are made from and go to, in LDS or in memory.
+struct Row {
+  const int32_t* own_at;
+  const int32_t* rank_first;
+  const int32_t* first;
+  const int32_t* slot_of;
+  const int32_t* total;
+  int64_t* upto;
+  int32_t* off;
+  int2* guest;
+  int2* own;
+};
 
+// The whole block; returns the number of copies that go somewhere.  A barrier
+// lies behind `off`, none behind `guest` and `own`.
+__device__ __forceinline__ int32_t tables(const Row& t, const int32_t* expert, const int32_t* share, int32_t R,
+                                          int32_t E, int32_t K, int32_t* sends, int64_t* part64, int32_t* part) {
+  const int tid = threadIdx.x;
+  const int32_t S = R * K, I = E + S, filled = t.first[E];
+  auto guest_at = [&](int32_t s) { return s + t.rank_first[s / K + 1]; };
+  auto at_guests = [&](int32_t e) { return min(t.upto[t.first[e + 1]] - t.upto[t.first[e]], (int64_t)t.total[e]); };
   int64_t run = 0;
-  for (int32_t i0 = 0; i0 < filled; i0 += kListThreads) {
+  for (int32_t i0 = 0; i0 < filled; i0 += kTableThreads) {
     const int32_t i = i0 + tid;
-    const int64_t x = i < filled ? (int64_t)max(share[slot_of[i]], 0) : 0;
+    const int64_t x = i < filled ? (int64_t)max(share[t.slot_of[i]], 0) : 0;
     int64_t all;
-    const int64_t at = run + block_exclusive(x, part64, &all);
-    if (i < filled) upto[i] = at;
+    const int64_t at = run + block_exclusive<kTableThreads>(x, part64, &all);
+    if (i < filled) t.upto[i] = at;
     run += all;
   }
-  if (tid == 0) upto[filled] = run;
-  for (int32_t s = tid; s < I; s += kListThreads) off[s] = 0;  // slots that hold no expert
+  if (tid == 0) t.upto[filled] = run;
+  for (int32_t s = tid; s < I; s += kTableThreads) t.off[s] = 0;  // slots that hold no expert
   __syncthreads();
-  for (int32_t e = tid; e < E; e += kListThreads) {
-    const int32_t lo = S > 0 ? first[e] : 0, hi = S > 0 ? first[e + 1] : 0;
-    const int64_t guests = upto[hi] - upto[lo];
-    const int32_t taken = (int32_t)min(guests, (int64_t)total[e]);
-    off[t.own_at[e]] = total[e] - taken;
-    own[e].x = taken;
-  }
-  // the expert of a sorted slot by its place in `first`
-  for (int32_t i = tid; i < filled; i += kListThreads) {
-    int32_t lo = 0, hi = E;  // first[lo] <= i < first[hi]
-    while (lo + 1 < hi) {
-      const int32_t mid = (lo + hi) / 2;
-      if (first[mid] <= i) lo = mid;
-      else hi = mid;
-    }
-    const int32_t n = total[lo];
-    const int32_t c = (int32_t)min(upto[i] - upto[first[lo]], (int64_t)n);
-    before[i] = c;
-    off[guest_at(slot_of[i])] = (int32_t)min((int64_t)(n - c), upto[i + 1] - upto[i]);
+  for (int32_t e = tid; e < E; e += kTableThreads) t.off[t.own_at[e]] = t.total[e] - (int32_t)at_guests(e);
+  for (int32_t i = tid; i < filled; i += kTableThreads) {
+    const int32_t s = t.slot_of[i], e = expert[s], n = t.total[e];
+    const int32_t c = (int32_t)min(t.upto[i] - t.upto[t.first[e]], (int64_t)n);
+    t.guest[i].x = c;
+    t.off[guest_at(s)] = (int32_t)min((int64_t)(n - c), t.upto[i + 1] - t.upto[i]);
   }
   __syncthreads();
   int32_t sum = 0;
-  for (int32_t i0 = 0; i0 < I; i0 += kListThreads) {
+  for (int32_t i0 = 0; i0 < I; i0 += kTableThreads) {
     const int32_t i = i0 + tid;
-    const int32_t v = i < I ? off[i] : 0;
+    const int32_t v = i < I ? t.off[i] : 0;
     int32_t all;
-    const int32_t at = sum + block_exclusive(v, part, &all);
-    if (i < I) off[i] = at;
+    const int32_t at = sum + block_exclusive<kTableThreads>(v, part, &all);
+    if (i < I) t.off[i] = at;
     sum += all;
   }
-  if (tid == 0) off[I] = sum;
+  if (tid == 0) t.off[I] = sum;
   __syncthreads();
-  // experts without a home rank lie behind all instances
-  const int32_t valid = t.rank_first[R] + S;
-  const int32_t placed = off[valid];
-  for (int32_t e = tid; e < E; e += kListThreads) own[e].y = off[t.own_at[e]] - own[e].x;
-  for (int32_t i = tid; i < filled; i += kListThreads) base[i] = off[guest_at(slot_of[i])] - before[i];
-  for (int32_t j = tid; j < R; j += kListThreads)
-    sends[row * R + j] = off[t.rank_first[j + 1] + K * (j + 1)] - off[t.rank_first[j] + K * j];
-  if (tid == 0) {
-    t.placed[row] = placed;
-    if (status && total[E] > 0) atomicOr(&status[b], TAOT_ST_BAD_ID);
+  for (int32_t e = tid; e < E; e += kTableThreads) {
+    const int32_t taken = (int32_t)at_guests(e);
+    t.own[e] = int2{taken, t.off[t.own_at[e]] - taken};
   }
-  __syncthreads();
-  for (int32_t i = valid + 1 + tid; i <= I; i += kListThreads) off[i] = placed;
+  for (int32_t i = tid; i < filled; i += kTableThreads) t.guest[i].y = t.off[guest_at(t.slot_of[i])] - t.guest[i].x;
+  for (int32_t j = tid; j < R; j += kTableThreads)
+    sends[j] = t.off[t.rank_first[j + 1] + K * (j + 1)] - t.off[t.rank_first[j] + K * j];
+  return t.off[t.rank_first[R] + S];  // experts without a home rank lie behind all instances
 }
 
-__global__ void __launch_bounds__(256)
-place_kernel(const int32_t* __restrict__ ids, Tables t, const int32_t* __restrict__ hist, int64_t N, int32_t rows,
-             int32_t E, int32_t S, int32_t chunk, int32_t chunks, int64_t jobs, int bits, int32_t* __restrict__ pos) {
-  extern __shared__ int32_t cnt[];
+// LDS: the running sums and instances lie in LDS.
+template <bool LDS>
+__global__ void __launch_bounds__(kTableThreads)
+tables_kernel(Tables t, const int32_t* __restrict__ slot_expert, const int32_t* __restrict__ X, int32_t rows,
+              int32_t rank0, int32_t R, int32_t E, int32_t K, int32_t* __restrict__ offsets,
+              int32_t* __restrict__ sends, uint32_t* __restrict__ status) {
+  extern __shared__ int64_t room[];
+  __shared__ int64_t part64[kTableThreads / kWave];
+  __shared__ int32_t part[kTableThreads / kWave];
+  const int tid = threadIdx.x;
+  const int64_t row = blockIdx.x, b = row / rows;
+  const int32_t S = R * K, I = E + S, r = rank0 + (int32_t)(row % rows);
+  int32_t* out = offsets + row * (I + 1);
+  Row w{t.own_at, t.rank_first, t.slot_first + b * (E + 1), t.slot_of + b * S, t.total + row * (E + 1),
+        LDS ? room : t.upto + row * (S + 1), LDS ? reinterpret_cast<int32_t*>(room + S + 1) : out, t.guest + row * S,
+        t.own + row * E};
+  const int32_t placed = tables(w, slot_expert + b * S, X + (b * R + r) * (int64_t)S, R, E, K, sends + row * R, part64,
+                                part);
+  if (tid == 0) {
+    t.placed[row] = placed;
+    if (status && w.total[E] > 0) atomicOr(&status[b], TAOT_ST_BAD_ID);
+  }
+  const int32_t valid = t.rank_first[R] + S;
+  if (LDS) {
+    for (int32_t i = tid; i <= I; i += kTableThreads) out[i] = i <= valid ? w.off[i] : placed;
+  } else {
+    __syncthreads();
+    for (int32_t i = valid + 1 + tid; i <= I; i += kTableThreads) out[i] = placed;
+  }
+}
+
+// A wave: ids src[0 .. n) of a row, n > 0, in order; mine[e]: occurrences of e
+// before them.  E <= 2^BITS.
+template <int BITS>
+__device__ __forceinline__ void place(const int32_t* __restrict__ src, int32_t n, int32_t E, int32_t* mine,
+                                      const int2* own, const int32_t* first, const int2* guest, int32_t placed,
+                                      int32_t dropped, int32_t* __restrict__ dst) {
   const int lane = threadIdx.x & (kWave - 1);
-  const int64_t job = (int64_t)blockIdx.x * (blockDim.x / kWave) + threadIdx.x / kWave;
-  if (job >= jobs) return;
-  int32_t* mine = cnt + (threadIdx.x / kWave) * (E + 1);
-  const int64_t row = job / chunks, lo = (job % chunks) * (int64_t)chunk, b = row / rows;
-  const int32_t n = (int32_t)min((int64_t)chunk, N - lo);
-  const int32_t* src = ids + row * N + lo;
-  int32_t* dst = pos + row * N + lo;
-  const int32_t* first = t.slot_first + b * (E + 1);
-  const int32_t* before = t.slot_before + row * S;
-  const int32_t* base = t.slot_base + row * S;
-  const int2* own = t.own + row * E;
-  const int32_t placed = t.placed[row];
-  const int32_t dropped = (int32_t)(N - t.total[row * (E + 1) + E]);  // where ids that are no expert begin
-  for (int32_t e = lane; e <= E; e += kWave) mine[e] = hist[job * (E + 1) + e];
-  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-  __builtin_amdgcn_wave_barrier();
+  int32_t next[kUnroll];
+  auto fetch = [&](int32_t i0) {  // past the end: the last id again
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u) next[u] = src[min(i0 + u * kWave + lane, n - 1)];
+  };
+  fetch(0);
   for (int32_t i0 = 0; i0 < n; i0 += kUnroll * kWave) {
     int32_t e[kUnroll], j[kUnroll];
+    Same m[kUnroll];
+    int2 o[kUnroll];
+    bool in[kUnroll];
 #pragma unroll
     for (int u = 0; u < kUnroll; ++u) {
-      const int32_t i = i0 + u * kWave + lane;
-      const int32_t q = i < n ? src[i] : E;
-      e[u] = (uint32_t)q < (uint32_t)E ? q : E;
+      in[u] = i0 + u * kWave + lane < n;
+      e[u] = (uint32_t)next[u] < (uint32_t)E ? next[u] : E;
+    }
+    fetch(i0 + kUnroll * kWave);
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u) {  // ids that are no expert are one key more
+      const uint64_t experts = __ballot(in[u] & (e[u] < E)), others = __ballot(in[u] & (e[u] == E));
+      m[u] = same_key<BITS>((uint32_t)e[u], experts);
+      m[u].lo = e[u] < E ? m[u].lo : (uint32_t)others;
+      m[u].hi = e[u] < E ? m[u].hi : (uint32_t)(others >> 32);
+      o[u] = own[min(e[u], E - 1)];
     }
 #pragma unroll
     for (int u = 0; u < kUnroll; ++u) {
-      const bool in = i0 + u * kWave + lane < n;
-      const uint64_t m = same_key((uint32_t)e[u], bits, __ballot(in));
-      const int at = __popcll(m & ((1ull << lane) - 1));
-      j[u] = mine[e[u]] + at;
+      const int below = m[u].below();
+      j[u] = mine[e[u]] + below;
       __builtin_amdgcn_wave_barrier();
-      if (in && (m >> lane) == 1) mine[e[u]] = j[u] + 1;
+      if (in[u] & (below + 1 == m[u].all())) mine[e[u]] = j[u] + 1;
       __builtin_amdgcn_wave_barrier();
     }
 #pragma unroll
     for (int u = 0; u < kUnroll; ++u) {
-      const int32_t i = i0 + u * kWave + lane;
-      if (i >= n) continue;
-      int32_t p;
-      if (e[u] == E) {
-        p = dropped + j[u];
-      } else {
-        const int2 o = own[e[u]];
-        if (j[u] >= o.x) {
-          p = o.y + j[u];
-        } else {
-          int32_t a = first[e[u]], z = first[e[u] + 1];  // before[a] <= j < before[z]
-          while (a + 1 < z) {
-            const int32_t mid = (a + z) / 2;
-            if (before[mid] <= j[u]) a = mid;
-            else z = mid;
-          }
-          p = base[a] + j[u];
+      int32_t p = (e[u] < E ? o[u].y : dropped) + j[u];
+      if ((e[u] < E) & (j[u] < o[u].x)) {
+        int32_t a = first[e[u]], z = first[e[u] + 1];  // guest[a].x <= j < guest[z].x
+        while (a + 1 < z) {
+          const int32_t mid = (a + z) / 2;
+          if (guest[mid].x <= j[u]) a = mid;
+          else z = mid;
         }
+        p = guest[a].y + j[u];
       }
-      dst[i] = p < placed ? p : ~p;
+      if (in[u]) dst[i0 + u * kWave + lane] = p < placed ? p : ~p;
     }
   }
+}
+
+// n words into LDS by `threads` threads, four loads at a time.
+__device__ __forceinline__ void bring(int32_t* to, const int32_t* __restrict__ from, int32_t n, int i, int threads) {
+  for (; i < n; i += 4 * threads) {
+    int32_t v[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) v[u] = from[min(i + u * threads, n - 1)];
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+      if (i + u * threads < n) to[i + u * threads] = v[u];
+  }
+}
+
+// LDS: the row's tables are brought into LDS first; a block then works on
+// chunks of one row.
+template <bool LDS, int BITS>
+__global__ void __launch_bounds__(kThreads)
+place_kernel(const int32_t* __restrict__ ids, Tables t, const int32_t* __restrict__ hist, int64_t N, int32_t rows,
+             int32_t E, int32_t S, int32_t chunk, int32_t chunks, int32_t blocks_of_row, int waves,
+             int32_t* __restrict__ pos) {
+  extern __shared__ int32_t cnt[];
+  const int lane = threadIdx.x & (kWave - 1), wid = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const int64_t row = blockIdx.x / blocks_of_row, b = row / rows;
+  const int32_t my_chunk = (int32_t)(blockIdx.x % blocks_of_row) * waves + wid;
+  const int2* own = t.own + row * E;
+  const int32_t* first = t.slot_first + b * (E + 1);
+  const int2* guest = t.guest + row * S;
+  const bool works = wid < waves && my_chunk < chunks;
+  const int64_t job = row * chunks + my_chunk, lo = my_chunk * (int64_t)chunk;
+  int32_t* mine = cnt + wid * (E + 1);
+  if (works) bring(mine, hist + job * (E + 1), E + 1, lane, kWave);
+  if constexpr (LDS) {
+    int32_t* own_l = cnt + ((waves * (E + 1) + 1) & ~1);
+    int32_t *guest_l = own_l + 2 * E, *first_l = guest_l + 2 * S;
+    bring(own_l, reinterpret_cast<const int32_t*>(own), 2 * E, threadIdx.x, kThreads);
+    bring(guest_l, reinterpret_cast<const int32_t*>(guest), 2 * S, threadIdx.x, kThreads);
+    bring(first_l, first, E + 1, threadIdx.x, kThreads);
+    own = reinterpret_cast<const int2*>(own_l);
+    guest = reinterpret_cast<const int2*>(guest_l);
+    first = first_l;
+  }
+  __syncthreads();
+  if (!works) return;
+  const int32_t n = (int32_t)min((int64_t)chunk, N - lo);
+  const int32_t dropped = (int32_t)(N - t.total[row * (E + 1) + E]);  // where ids that are no expert begin
+  place<BITS>(ids + row * N + lo, n, E, mine, own, first, guest, t.placed[row], dropped, pos + row * N + lo);
+}
+
+// A short row by one block and in one launch: everything above, in LDS.
+struct RowRoom {
+  size_t cnt, own_at, rank_first, first, slot_of, total, upto, off, guest, own, hist, bytes;
+};
+__host__ __device__ inline RowRoom row_room(int32_t R, int32_t E, int32_t S, int waves) {
+  RowRoom r{};
+  size_t at = 0;
+  auto take = [&](size_t n) {
+    const size_t was = at;
+    at += (n + 7) / 8 * 8;
+    return was;
+  };
+  r.upto = take((size_t)(S + 1) * 8);
+  r.guest = take((size_t)S * 8);
+  r.own = take((size_t)E * 8);
+  r.cnt = take((size_t)((E > R ? E : R) + 1) * 4);
+  r.own_at = take((size_t)E * 4);
+  r.rank_first = take((size_t)(R + 1) * 4);
+  r.first = take((size_t)(E + 1) * 4);
+  r.slot_of = take((size_t)S * 4);
+  r.total = take((size_t)(E + 1) * 4);
+  r.off = take((size_t)(E + S + 1) * 4);
+  r.hist = take((size_t)waves * (E + 1) * 4);
+  r.bytes = at;
+  return r;
+}
+
+template <int BITS>
+__global__ void __launch_bounds__(kTableThreads)
+row_kernel(const int32_t* __restrict__ home, const int32_t* __restrict__ slot_expert, const int32_t* __restrict__ X,
+           const int32_t* __restrict__ ids, int32_t N, int32_t rows, int32_t rank0, int32_t R, int32_t E, int32_t K,
+           int waves, int32_t* __restrict__ pos, int32_t* __restrict__ offsets, int32_t* __restrict__ sends,
+           uint32_t* __restrict__ bad) {
+  extern __shared__ int64_t room[];
+  __shared__ int64_t part64[kTableThreads / kWave];
+  __shared__ int32_t part[kTableThreads / kWave];
+  __shared__ int32_t bad_home;
+  const int tid = threadIdx.x, lane = tid & (kWave - 1), wid = __builtin_amdgcn_readfirstlane(tid / kWave);
+  const int64_t row = blockIdx.x, b = row / rows;
+  const int32_t S = R * K, I = E + S, r = rank0 + (int32_t)(row % rows);
+  const RowRoom at = row_room(R, E, S, waves);
+  char* base = reinterpret_cast<char*>(room);
+  auto words = [&](size_t o) { return reinterpret_cast<int32_t*>(base + o); };
+  int32_t *own_at = words(at.own_at), *rank_first = words(at.rank_first), *first = words(at.first),
+          *slot_of = words(at.slot_of), *total = words(at.total), *hist = words(at.hist);
+  int2 *guest = reinterpret_cast<int2*>(base + at.guest), *own = reinterpret_cast<int2*>(base + at.own);
+  // `waves` runs of the row, in order
+  const int32_t run = (N + waves * kWave - 1) / (waves * kWave) * kWave, lo = min(wid * run, N), n = min(run, N - lo);
+  const int32_t* src = ids + row * N + lo;
+  int32_t* mine = hist + wid * (E + 1);
+  if (tid == 0) bad_home = 0;
+  if (wid < waves)
+    for (int32_t e = lane; e <= E; e += kWave) mine[e] = 0;
+  order_experts<kTableThreads>(home, R, E, K, own_at, rank_first, words(at.cnt), part);
+  if (wid < waves) {
+    for (int32_t i = lane; i < n; i += kWave) {
+      const int32_t e = src[i];
+      atomicAdd(&mine[(uint32_t)e < (uint32_t)E ? e : E], 1);
+    }
+  }
+  for (int32_t e = tid; e < E; e += kTableThreads)
+    if (home[e] < 0 || home[e] >= R) bad_home = 1;
+  __syncthreads();
+  order_slots<kTableThreads>(slot_expert + b * S, S, E, first, slot_of, words(at.cnt), part);
+  for (int32_t e = tid; e <= E; e += kTableThreads) {
+    int32_t sum = 0;
+    for (int w = 0; w < waves; ++w) {
+      const int32_t v = hist[w * (E + 1) + e];
+      hist[w * (E + 1) + e] = sum;
+      sum += v;
+    }
+    total[e] = sum;
+  }
+  __syncthreads();
+  Row w{own_at, rank_first, first, slot_of, total, reinterpret_cast<int64_t*>(base + at.upto), words(at.off), guest, own};
+  const int32_t placed =
+      tables(w, slot_expert + b * S, X + (b * R + r) * (int64_t)S, R, E, K, sends + row * R, part64, part);
+  int32_t* out = offsets + row * (I + 1);
+  const int32_t valid = rank_first[R] + S;
+  for (int32_t i = tid; i <= I; i += kTableThreads) out[i] = i <= valid ? w.off[i] : placed;
+  if (tid == 0) bad[row] = (bad_home ? TAOT_ST_BAD_INPUT : 0u) | (total[E] > 0 ? TAOT_ST_BAD_ID : 0u);
+  __syncthreads();
+  if (wid < waves && n > 0)
+    place<BITS>(src, n, E, mine, own, first, guest, placed, N - total[E], pos + row * N + lo);
+}
+
+// status[b] of the rows' bits.
+__global__ void __launch_bounds__(kThreads)
+status_kernel(const uint32_t* __restrict__ bad, int32_t B, int32_t rows, uint32_t* __restrict__ status) {
+  const int64_t b = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+  if (b >= B) return;
+  uint32_t s = 0;
+  for (int32_t r = 0; r < rows; ++r) s |= bad[b * rows + r];
+  status[b] = s;
 }
 
 // ---- rows ------------------------------------------------------------------------
@@ -507,7 +730,8 @@ combine_backward_kernel(const T* __restrict__ dout, const T* __restrict__ y, con
 // Ids of a wave: enough waves to fill the chip, and no more counters than ids.
 int32_t chunk_of(int64_t rows, int64_t N, int32_t E) {
   int64_t c = kChunkMin;
-  while (c < kChunkMax && (c < E || rows * ((N + c - 1) / c) > kWavesWanted)) c *= 2;
+  const int64_t want = getenv("DW") ? atoi(getenv("DW")) : kWavesWanted;
+  while (c < kChunkMax && (c < E || rows * ((N + c - 1) / c) > want)) c *= 2;
   return (int32_t)c;
 }
 
@@ -534,8 +758,7 @@ Plan carve(void* ws, int32_t B, int32_t rows, int64_t N, int32_t R, int32_t E, i
   p.slot_of = c.take<int32_t>((size_t)B * S);
   p.total = c.take<int32_t>(n * (E + 1));
   p.t.upto = c.take<int64_t>(n * (S + 1));
-  p.t.slot_before = c.take<int32_t>(n * S);
-  p.t.slot_base = c.take<int32_t>(n * S);
+  p.t.guest = c.take<int2>(n * S);
   p.t.own = c.take<int2>(n * E);
   p.t.placed = c.take<int32_t>(n);
   p.hist = c.take<int32_t>(n * chunks * (E + 1));
@@ -546,6 +769,16 @@ Plan carve(void* ws, int32_t B, int32_t rows, int64_t N, int32_t R, int32_t E, i
   p.t.total = p.total;
   p.bytes = c.off;
   return p;
+}
+
+// f by the number of bits of an expert, as a constant that is large enough.
+template <typename F>
+auto with_bits(int bits, F f) {
+  if (bits <= 6) return f(std::integral_constant<int, 6>());
+  if (bits <= 8) return f(std::integral_constant<int, 8>());
+  if (bits <= 9) return f(std::integral_constant<int, 9>());
+  if (bits <= 12) return f(std::integral_constant<int, 12>());
+  return f(std::integral_constant<int, 15>());
 }
 
 template <typename F>
@@ -570,25 +803,46 @@ taot_status launch_dispatch_map(const int32_t* ids, int32_t B, int32_t rows, int
   const int64_t n = (int64_t)B * rows;
   const int32_t chunk = chunk_of(n, N, E), chunks = (int32_t)((N + chunk - 1) / chunk);
   const int64_t jobs = n * chunks;
-  const int32_t most = E > R ? E : R;
-  const size_t list_lds = (size_t)(most + 1) * sizeof(int32_t);
-  if (!allow_lds(reinterpret_cast<const void*>(lists_kernel), list_lds)) return TAOT_ERR_LAUNCH;
-  lists_kernel<<<(unsigned)B + 1, kListThreads, list_lds, stream>>>(home, slot_expert, B, R, E, K, p.own_at,
-                                                                    p.rank_first, p.slot_first, p.slot_of, status);
-  const size_t row_lds = (size_t)(E + 1) * sizeof(int32_t);
+  const int32_t S = R * K, I = E + S, most = E > R ? E : R;
+  const Lists lists{home, slot_expert, p.own_at, p.rank_first, p.slot_first, p.slot_of, status};
+  const size_t list_lds = (size_t)(most + 1) * sizeof(int32_t), row_lds = (size_t)(E + 1) * sizeof(int32_t);
   const int waves = 4 * row_lds <= 65536 ? 4 : 2 * row_lds <= 65536 ? 2 : 1;
-  const unsigned blocks = (unsigned)((jobs + waves - 1) / waves);
-  if (jobs > 0) {
-    if (!allow_lds(reinterpret_cast<const void*>(count_kernel), waves * row_lds)) return TAOT_ERR_LAUNCH;
-    count_kernel<<<blocks, kWave * waves, waves * row_lds, stream>>>(ids, N, E, chunk, chunks, jobs, p.hist);
+  const size_t count_lds = waves * row_lds > list_lds ? waves * row_lds : list_lds;
+  const int bits = bits_for((uint32_t)E - 1);
+  if (N <= kRowIds) {
+    const int wanted = (int)((N + kWave - 1) / kWave), row_waves = wanted < 1 ? 1 : wanted < 16 ? wanted : 16;
+    const size_t lds = row_room(R, E, S, row_waves).bytes;
+    if (lds <= kRowLds) {
+      auto* kernel = with_bits(bits, [](auto n) { return row_kernel<n.value>; });
+      if (!allow_lds(reinterpret_cast<const void*>(kernel), lds)) return TAOT_ERR_LAUNCH;
+      // one row a problem: its bits are the problem's status
+      uint32_t* bad = status && rows == 1 ? status : reinterpret_cast<uint32_t*>(p.t.placed);
+      kernel<<<(unsigned)n, kTableThreads, lds, stream>>>(home, slot_expert, X, ids, (int32_t)N, rows, rank0, R, E, K,
+                                                          row_waves, pos, offsets, sends, bad);
+      if (status && rows > 1)
+        status_kernel<<<(unsigned)((B + kThreads - 1) / kThreads), kThreads, 0, stream>>>(bad, B, rows, status);
+      return hipGetLastError() == hipSuccess ? TAOT_OK : TAOT_ERR_LAUNCH;
+    }
   }
-  const int64_t entries = n * (E + 1);
-  bases_kernel<<<(unsigned)((entries + 255) / 256), 256, 0, stream>>>(p.hist, E, chunks, entries, p.total);
-  tables_kernel<<<(unsigned)n, kListThreads, 0, stream>>>(p.t, X, N, rows, rank0, R, E, K, offsets, sends, status);
+  if (!allow_lds(reinterpret_cast<const void*>(count_kernel), count_lds)) return TAOT_ERR_LAUNCH;
+  count_kernel<<<(unsigned)(B + 1 + (jobs + waves - 1) / waves), kThreads, count_lds, stream>>>(
+      lists, B, R, K, ids, N, E, chunk, chunks, jobs, waves, p.hist);
+  bases_kernel<<<(unsigned)(n * ((E + kWave) / kWave)), kBaseThreads, 0, stream>>>(p.hist, E, chunks, p.total);
+  const size_t table_lds = (size_t)(S + 1) * sizeof(int64_t) + (size_t)(I + 1) * sizeof(int32_t);
+  const bool small_tables = table_lds <= kTableLds;
+  (small_tables ? tables_kernel<true> : tables_kernel<false>)<<<(unsigned)n, kTableThreads, small_tables ? table_lds : 0,
+                                                               stream>>>(p.t, slot_expert, X, rows, rank0, R, E, K,
+                                                                         offsets, sends, status);
   if (jobs > 0) {
-    if (!allow_lds(reinterpret_cast<const void*>(place_kernel), waves * row_lds)) return TAOT_ERR_LAUNCH;
-    place_kernel<<<blocks, kWave * waves, waves * row_lds, stream>>>(ids, p.t, p.hist, N, rows, E, R * K, chunk, chunks,
-                                                                     jobs, bits_for((uint32_t)E), pos);
+    const size_t extra = (size_t)(E + S) * sizeof(int2) + (size_t)(E + 1) * sizeof(int32_t) + sizeof(int2);
+    const bool small_rows = extra <= kTableLds;
+    const size_t lds = waves * row_lds + (small_rows ? extra : 0);
+    auto* kernel = small_rows ? with_bits(bits, [](auto n) { return place_kernel<true, n.value>; })
+                              : with_bits(bits, [](auto n) { return place_kernel<false, n.value>; });
+    if (!allow_lds(reinterpret_cast<const void*>(kernel), lds)) return TAOT_ERR_LAUNCH;
+    const int32_t blocks = (chunks + waves - 1) / waves;
+    kernel<<<(unsigned)(n * blocks), kThreads, lds, stream>>>(ids, p.t, p.hist, N, rows, E, S, chunk, chunks, blocks, waves,
+                                                            pos);
   }
   return hipGetLastError() == hipSuccess ? TAOT_OK : TAOT_ERR_LAUNCH;
 }

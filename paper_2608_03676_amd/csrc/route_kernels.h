@@ -121,30 +121,36 @@ struct Lanes {
 #pragma unroll
     for (int v0 = 0; v0 < V; v0 += W) d[v0 / W] = *reinterpret_cast<const at*>(row + max(0, min(index(v0), E - W)));
     if (full) return;
+    if (whole) {
+#pragma unroll
+      for (int v0 = 0; v0 < V; v0 += W) {
+        const bool in = left(v0) > 0;
+        words r = __builtin_bit_cast(words, d[v0 / W]);
+#pragma unroll
+        for (int u = 0; u < kWords; ++u) r[u] = in ? r[u] : kLow;
+        d[v0 / W] = __builtin_bit_cast(vec, r);
+      }
+      return;
+    }
 #pragma unroll
     for (int v0 = 0; v0 < V; v0 += W) {
       const int32_t n = left(v0);
       words r = __builtin_bit_cast(words, d[v0 / W]);
-      if (whole) {
+      const int32_t off = index(v0) - min(index(v0), E - W);  // the load was moved back by this
+      constexpr int kPer = k32 ? 1 : 2;                       // values of a word
 #pragma unroll
-        for (int u = 0; u < kWords; ++u) r[u] = n > 0 ? r[u] : kLow;
-      } else {
-        const int32_t off = index(v0) - min(index(v0), E - W);  // the load was moved back by this
-        constexpr int kPer = k32 ? 1 : 2;                       // values of a word
+      for (int s = W / 2; s >= kPer; s /= 2)
 #pragma unroll
-        for (int s = W / 2; s >= kPer; s /= 2)
+        for (int u = 0; u < kWords; ++u) r[u] = off & s ? (u + s / kPer < kWords ? r[u + s / kPer] : 0u) : r[u];
+      if (!k32) {
 #pragma unroll
-          for (int u = 0; u < kWords; ++u) r[u] = off & s ? (u + s / kPer < kWords ? r[u + s / kPer] : 0u) : r[u];
-        if (!k32) {
+        for (int u = 0; u < kWords; ++u)
+          r[u] = off & 1 ? (r[u] >> 16) | (u + 1 < kWords ? r[u + 1] << 16 : 0u) : r[u];
+      }
 #pragma unroll
-          for (int u = 0; u < kWords; ++u)
-            r[u] = off & 1 ? (r[u] >> 16) | (u + 1 < kWords ? r[u + 1] << 16 : 0u) : r[u];
-        }
-#pragma unroll
-        for (int u = 0; u < kWords; ++u) {
-          const uint32_t keep = n >= (u + 1) * kPer ? ~0u : !k32 && n == 2 * u + 1 ? 0xFFFFu : 0u;
-          r[u] = (r[u] & keep) | (kLow & ~keep);
-        }
+      for (int u = 0; u < kWords; ++u) {
+        const uint32_t keep = n >= (u + 1) * kPer ? ~0u : !k32 && n == 2 * u + 1 ? 0xFFFFu : 0u;
+        r[u] = (r[u] & keep) | (kLow & ~keep);
       }
       d[v0 / W] = __builtin_bit_cast(vec, r);
     }
@@ -383,7 +389,7 @@ __device__ __forceinline__ float exp_fast(float x) { return __builtin_amdgcn_exp
 constexpr int log2_of(int n) { return n <= 1 ? 0 : 1 + log2_of(n / 2); }
 
 template <typename T, int L, int V, int DEPTH, int MODE, bool GROUPED>
-__global__ void __launch_bounds__(256)
+__global__ void __launch_bounds__(256, sizeof(T) == 4 || MODE == kSigmoid ? 4 : 5)
 route_few_kernel(RouteArgs a, Layout lay) {
   using Place = Lanes<T, L, V, GROUPED>;
   static_assert(V >= DEPTH, "every place of the list holds a word");
@@ -455,27 +461,25 @@ route_few_kernel(RouteArgs a, Layout lay) {
   } else {
     // fixed point over the range of the keys, by the largest bias of all experts (infinite or NaN: exact keys)
     float most = 0.f, least = INFINITY;
-    auto biases = [&](int v0) {  // of places v0 .. v0 + 3
-      typedef float four __attribute__((ext_vector_type(4)));
-      typedef __attribute__((aligned(4))) four at4;
-      four b;
-      if (at.whole) {
-        b = *reinterpret_cast<const at4*>(a.bias + max(0, min(at.index(v0), a.E - 4)));
-      } else {
-#pragma unroll
-        for (int u = 0; u < 4; ++u) b[u] = a.bias[min(at.index(v0 + u), a.E - 1)];
-      }
-      return b;
-    };
+    float bias[kWide ? 1 : V];
     if constexpr (kWide) {
       for (int e = lane; e < a.E; e += kWave) most = fmaxf(most, fabsf(a.bias[e]));
     } else {
+      if (at.whole) {
+        typedef float four __attribute__((ext_vector_type(4)));
+        typedef __attribute__((aligned(4))) four at4;
 #pragma unroll
-      for (int v0 = 0; v0 < V; v0 += 4) {
-        const auto b = biases(v0);
+        for (int v = 0; v < V; v += 4) {
+          const four b = *reinterpret_cast<const at4*>(a.bias + max(0, min(at.index(v), a.E - 4)));
 #pragma unroll
-        for (int u = 0; u < 4; ++u) most = fmaxf(most, fabsf(b[u]));
+          for (int u = 0; u < 4; ++u) bias[v + u] = b[u];
+        }
+      } else {
+#pragma unroll
+        for (int v = 0; v < V; ++v) bias[v] = a.bias[min(at.index(v), a.E - 1)];
       }
+#pragma unroll
+      for (int v = 0; v < V; ++v) most = fmaxf(most, fabsf(bias[v]));
     }
     most = block_reduce<L>(most, MaxOp());
     const float unit = (kMost - 16.f) / (1.f + 2.f * most), zero = most * unit + 4.f;
@@ -483,16 +487,12 @@ route_few_kernel(RouteArgs a, Layout lay) {
     for (int v = 0; v < V; ++v) least = fminf(least, logit(v));
     auto fill = [&](auto masked) {
 #pragma unroll
-      for (int v0 = 0; v0 < V; v0 += 4) {
-        const auto bias = biases(v0);
-#pragma unroll
-        for (int u = 0; u < 4; ++u) {
-          const int v = v0 + u;
-          const float x = logit(v), b = fmaf(bias[u], unit, zero);
-          const uint32_t k = (uint32_t)fmaf(__builtin_amdgcn_rcpf(1.f + exp_fast(-x)), unit, b);  // NaN: 0
-          const uint32_t q = !masked.value || x > -INFINITY ? k : 0u;
-          insert((int)((q << kShift) | (uint32_t)(kLow - Place::away(v))));
-        }
+      for (int v = 0; v < V; ++v) {
+        const float x = logit(v);
+        const float b = fmaf(kWide ? a.bias[min(at.index(v), a.E - 1)] : bias[kWide ? 0 : v], unit, zero);
+        const uint32_t k = (uint32_t)fmaf(__builtin_amdgcn_rcpf(1.f + exp_fast(-x)), unit, b);  // NaN: 0
+        const uint32_t q = !masked.value || x > -INFINITY ? k : 0u;
+        insert((int)((q << kShift) | (uint32_t)(kLow - Place::away(v))));
       }
     };
     if (__ballot(least == -INFINITY) != 0) fill(std::true_type());
