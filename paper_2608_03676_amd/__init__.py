@@ -325,9 +325,17 @@ def _empty(shape, dtype, device, stream) -> torch.Tensor:
 def _into(t: Optional[torch.Tensor], name: str, shape, dtype, device, stream) -> torch.Tensor:
     """The caller's output tensor, checked, or a new one."""
     if t is None:
-        return torch.empty(shape, dtype=dtype, device=device) if stream is None else _empty(shape, dtype, device, stream)
+        return (torch.empty(tuple(shape), dtype=dtype, device=device) if stream is None else
+                _empty(shape, dtype, device, stream))
     _shape(_dev(t, name, dtype), name, shape)
     return t
+
+
+def _like(t: Optional[torch.Tensor], name: str, x: torch.Tensor, stream) -> torch.Tensor:
+    """The caller's output tensor of the shape and type of x, checked, or a new one."""
+    if t is None and stream is None:
+        return torch.empty_like(x)
+    return _into(t, name, x.shape, x.dtype, x.device, stream)
 
 
 def _room(workspace: Optional[torch.Tensor], nbytes: int, device, stream) -> torch.Tensor:
@@ -354,17 +362,15 @@ def add_rms_norm(x: torch.Tensor, weight: torch.Tensor, eps: float, residual: Op
     of two from 8 to 512), 0: one scale a row; None: no 8-bit output."""
     _rows(x, "x")
     H = x.shape[-1] if x.dim() else 0
-    if weight.dtype != torch.float32:
-        _rows(weight, "weight", x)
-    _shape(_rows(weight, "weight"), "weight", (H,))
+    _shape(_rows(weight, "weight", None if weight.dtype == torch.float32 else x), "weight", (H,))
     if residual is not None:
         _shape(_rows(residual, "residual", x), "residual", x.shape)
     lead, dev = x.shape[:-1], x.device
     if out is None:
         out = Norm()
-    out.y = _into(out.y, "out.y", x.shape, x.dtype, dev, stream)
+    out.y = _like(out.y, "out.y", x, stream)
     out.rstd = _into(out.rstd, "out.rstd", lead, torch.float32, dev, stream)
-    out.h = x if residual is None else _into(out.h, "out.h", x.shape, x.dtype, dev, stream)
+    out.h = x if residual is None else _like(out.h, "out.h", x, stream)
     q = s = None
     if group is not None:
         q = out.q = _into(out.q, "out.q", x.shape, torch.float8_e4m3fn, dev, stream)
@@ -393,13 +399,11 @@ def add_rms_norm_backward(dy: torch.Tensor, h: torch.Tensor, rstd: torch.Tensor,
     _shape(_rows(dy, "dy", h), "dy", h.shape)
     if dh is not None:
         _shape(_rows(dh, "dh", h), "dh", h.shape)
-    if weight.dtype != torch.float32:
-        _rows(weight, "weight", h)
-    _shape(_rows(weight, "weight"), "weight", (H,))
+    _shape(_rows(weight, "weight", None if weight.dtype == torch.float32 else h), "weight", (H,))
     _shape(_dev(rstd, "rstd", torch.float32), "rstd", h.shape[:-1])
     if out is None:
         out = NormGrad()
-    out.dx = _into(out.dx, "out.dx", h.shape, h.dtype, h.device, stream)
+    out.dx = _like(out.dx, "out.dx", h, stream)
     out.dweight = _into(out.dweight, "out.dweight", (H,), torch.float32, h.device, stream)
     T = h.numel() // H if H else 0
     ws = _room(workspace, lib().taot_add_rms_norm_backward_workspace_size(T, H), h.device, stream)
@@ -446,7 +450,7 @@ def route_backward(dweights: torch.Tensor, logits: torch.Tensor, ids: torch.Tens
     shape = (*logits.shape[:-1], top_k)
     _shape(_dev(ids, "ids", torch.int32), "ids", shape)
     _shape(_dev(dweights, "dweights", torch.float32), "dweights", shape)
-    out = _into(out, "out", logits.shape, logits.dtype, logits.device, stream)
+    out = _like(out, "out", logits, stream)
     T = logits.numel() // E if E else 0
     _check("taot_route_backward", lib().taot_route_backward(
         dweights.data_ptr(), logits.data_ptr(), ids.data_ptr(), T, E, top_k, float(scale), int(flags),
@@ -481,7 +485,7 @@ def dispatch_map(ids: torch.Tensor, home: torch.Tensor, slot_expert: torch.Tenso
     dev = ids.device
     if out is None:
         out = Dispatch()
-    out.pos = _into(out.pos, "out.pos", (B, rows, N), torch.int32, dev, stream)
+    out.pos = _like(out.pos, "out.pos", ids, stream)
     out.offsets = _into(out.offsets, "out.offsets", (B, rows, E + S + 1), torch.int32, dev, stream)
     out.sends = _into(out.sends, "out.sends", (B, rows, R), torch.int32, dev, stream)
     out.status = _into(out.status, "out.status", (B,), torch.int32, dev, stream)
@@ -570,8 +574,8 @@ def combine_rows_backward(dout: torch.Tensor, y: torch.Tensor, pos: torch.Tensor
         raise ValueError("weights must have a value for each copy")
     if out is None:
         out = CombineGrad()
-    out.dy = _into(out.dy, "out.dy", y.shape, y.dtype, y.device, stream)
-    out.dweights = _into(out.dweights, "out.dweights", weights.shape, torch.float32, y.device, stream)
+    out.dy = _like(out.dy, "out.dy", y, stream)
+    out.dweights = _like(out.dweights, "out.dweights", weights, stream)
     _check("taot_combine_rows_backward", lib().taot_combine_rows_backward(
         dout.data_ptr(), y.data_ptr(), pos.data_ptr(), weights.data_ptr(), rows, tokens, k, H, _DTYPE[y.dtype],
         out.dy.data_ptr(), out.dweights.data_ptr(), _queue(stream, y.device)))

@@ -18,7 +18,6 @@
 //   place_kernel  (a wave per chunk)  occurrence by occurrence to a position
 //   row_kernel    (a block per row)  all of these for a short row, in one launch
 //   rows_kernel, combine_kernel, combine_backward_kernel  (one or four waves a token)
-#include <stdlib.h>
 #include "rowio.h"
 
 namespace taot {
@@ -27,8 +26,9 @@ namespace {
 constexpr int kThreads = 256, kTableThreads = 1024;
 constexpr int kUnroll = 4;
 constexpr int32_t kChunkMin = 256, kChunkMax = 32768;
-constexpr int64_t kWavesWanted = 8192;
+constexpr int64_t kWavesWanted = 4096;  // 64 rows of 131072: 54 us, 58 with twice as many (more counts), 58 with half
 constexpr size_t kTableLds = 32768;  // a row's tables are kept in LDS up to this size
+constexpr size_t kKeepLds = 65536;   // and beside its waves' stretches up to this one
 constexpr int64_t kRowIds = 8192;    // rows up to this length are done by one block
 constexpr size_t kRowLds = 65536;
 
@@ -46,11 +46,6 @@ __device__ __forceinline__ void same_bit(Same& m, uint32_t key, int b) {
   const uint64_t v = __ballot(s != 0);
   m.lo &= ~((uint32_t)v ^ s);
   m.hi &= ~((uint32_t)(v >> 32) ^ s);
-}
-__device__ __forceinline__ Same same_key(uint32_t key, int bits, uint64_t valid) {
-  Same m{(uint32_t)valid, (uint32_t)(valid >> 32)};
-  for (int b = 0; b < bits; ++b) same_bit(m, key, b);
-  return m;
 }
 template <int BITS>
 __device__ __forceinline__ Same same_key(uint32_t key, uint64_t valid) {
@@ -89,20 +84,19 @@ __device__ __forceinline__ V block_exclusive(V v, V* part, V* total) {
   return off;
 }
 
-// Stable order of n keys in [0, nkeys] by a block of NT threads: first[q] = keys
-// below q (q <= nkeys), put(i, its key, position).  cnt: nkeys + 1 words of LDS.  The
-// first wave places; no barrier behind it.
-template <int NT, typename Key, typename Put>
-__device__ __forceinline__ void stable_order(int32_t n, int32_t nkeys, Key key, Put put, int32_t* first,
-                                             int32_t* cnt, int32_t* part) {
-  const int tid = threadIdx.x, lane = tid & (kWave - 1);
-  for (int32_t q = tid; q <= nkeys; q += NT) cnt[q] = 0;
-  __syncthreads();
-  for (int32_t i = tid; i < n; i += NT) atomicAdd(&cnt[key(i)], 1);
-  __syncthreads();
+// Stable order of n keys in [0, nkeys], in three steps: their counts, running
+// sums of those (first[q] = keys below q, q <= nkeys), and positions, by one wave:
+// put(i, its key, position) for keys up to `last`.  cnt: nkeys + 1 words of LDS.
+template <int NT, typename Key>
+__device__ __forceinline__ void order_counts(int32_t n, Key key, int32_t* cnt) {
+  for (int32_t i = threadIdx.x; i < n; i += NT) atomicAdd(&cnt[key(i)], 1);
+}
+
+template <int NT>
+__device__ __forceinline__ void order_sums(int32_t nkeys, int32_t* first, int32_t* cnt, int32_t* part) {
   int32_t run = 0;
   for (int32_t q0 = 0; q0 <= nkeys; q0 += NT) {
-    const int32_t q = q0 + tid;
+    const int32_t q = q0 + threadIdx.x;
     int32_t total;
     const int32_t mine = q <= nkeys ? cnt[q] : 0;
     const int32_t at = run + block_exclusive<NT>(mine, part, &total);
@@ -112,23 +106,43 @@ __device__ __forceinline__ void stable_order(int32_t n, int32_t nkeys, Key key, 
     }
     run += total;
   }
-  __syncthreads();
-  if (tid >= kWave) return;
-  const int bits = bits_for((uint32_t)nkeys);
-  int32_t next = lane < n ? key(lane) : nkeys;
+}
+
+// last < 2^BITS
+template <int BITS, typename Key, typename Put>
+__device__ __forceinline__ void order_positions(int32_t n, int32_t last, Key key, Put put, int32_t* cnt) {
+  const int lane = threadIdx.x & (kWave - 1);
+  int32_t next = key(min(lane, n - 1));
   for (int32_t i0 = 0; i0 < n; i0 += kWave) {
     const int32_t i = i0 + lane, q = next;
-    const bool in = i < n;
-    next = i + kWave < n ? key(i + kWave) : nkeys;
-    const Same m = same_key((uint32_t)q, bits, __ballot(in));
+    const bool in = (i < n) & (q <= last);
+    next = key(min(i + kWave, n - 1));
+    const Same m = same_key<BITS>((uint32_t)q, __ballot(in));
     const int before = m.below();
-    const int32_t at = cnt[q] + before;
+    const int32_t at = cnt[min(q, last)] + before;
     if (in) put(i, q, at);
     __builtin_amdgcn_wave_barrier();
-    if (in && before + 1 == m.all()) cnt[q] = at + 1;  // the last lane of the key
+    if (in & (before + 1 == m.all())) cnt[q] = at + 1;  // the last lane of the key
     __builtin_amdgcn_wave_barrier();
   }
 }
+
+constexpr int kRankBits = 12;  // holds 0 .. TAOT_MAX_RANKS
+static_assert(TAOT_MAX_RANKS < 1 << kRankBits, "bits of a rank");
+constexpr int kExpertBits = 15;
+static_assert(TAOT_MAX_EXPERTS <= 1 << kExpertBits, "bits of an expert");
+
+// Ranks of experts (R: none) and experts of slots (E: none).
+struct HomeKey {
+  const int32_t* home;
+  int32_t R;
+  __device__ __forceinline__ int32_t operator()(int32_t e) const { return (uint32_t)home[e] < (uint32_t)R ? home[e] : R; }
+};
+struct SlotKey {
+  const int32_t* slots;
+  int32_t E;
+  __device__ __forceinline__ int32_t operator()(int32_t s) const { return (uint32_t)slots[s] < (uint32_t)E ? slots[s] : E; }
+};
 
 struct Lists {
   const int32_t* home;
@@ -140,43 +154,33 @@ struct Lists {
   uint32_t* status;
 };
 
-template <int NT>
-__device__ __forceinline__ void order_experts(const int32_t* home, int32_t R, int32_t E, int32_t K, int32_t* own_at,
-                                              int32_t* rank_first, int32_t* cnt, int32_t* part) {
-  auto key = [&](int32_t e) {
-    const int32_t h = home[e];
-    return h >= 0 && h < R ? h : R;
-  };
-  stable_order<NT>(E, R, key, [&](int32_t e, int32_t h, int32_t at) { own_at[e] = at + K * h; }, rank_first, cnt, part);
-}
-
-template <int NT>
-__device__ __forceinline__ void order_slots(const int32_t* slots, int32_t S, int32_t E, int32_t* slot_first,
-                                            int32_t* slot_of, int32_t* cnt, int32_t* part) {
-  auto key = [&](int32_t s) {
-    const int32_t e = slots[s];
-    return e >= 0 && e < E ? e : E;
-  };
-  stable_order<NT>(S, E, key, [&](int32_t s, int32_t, int32_t at) { slot_of[at] = s; }, slot_first, cnt, part);
-}
-
 // Block b < B: slots of problem b by expert.  Block B: experts by home rank.
 __device__ void lists(const Lists& l, int32_t b, int32_t B, int32_t R, int32_t E, int32_t K, int32_t* cnt) {
   __shared__ int32_t part[kThreads / kWave];
   __shared__ int32_t bad;
-  const int32_t S = R * K;
-  if (b == B) {
-    order_experts<kThreads>(l.home, R, E, K, l.own_at, l.rank_first, cnt, part);
-    return;
-  }
+  const int32_t S = R * K, n = b == B ? E : S, nkeys = b == B ? R : E;
+  const HomeKey home{l.home, R};
+  const SlotKey slot{l.slot_expert + (int64_t)b * S, E};
   if (threadIdx.x == 0) bad = 0;
+  for (int32_t q = threadIdx.x; q <= nkeys; q += kThreads) cnt[q] = 0;
   __syncthreads();
-  for (int32_t e = threadIdx.x; e < E; e += kThreads)
-    if (l.home[e] < 0 || l.home[e] >= R) bad = 1;
+  if (b == B) {
+    order_counts<kThreads>(n, home, cnt);
+  } else {
+    order_counts<kThreads>(n, slot, cnt);
+    for (int32_t e = threadIdx.x; e < E; e += kThreads)
+      if (home(e) == R) bad = 1;
+  }
   __syncthreads();
-  if (threadIdx.x == 0 && l.status) l.status[b] = bad ? TAOT_ST_BAD_INPUT : 0u;
-  order_slots<kThreads>(l.slot_expert + (int64_t)b * S, S, E, l.slot_first + (int64_t)b * (E + 1),
-                        l.slot_of + (int64_t)b * S, cnt, part);
+  order_sums<kThreads>(nkeys, b == B ? l.rank_first : l.slot_first + (int64_t)b * (E + 1), cnt, part);
+  if (b < B && threadIdx.x == 0 && l.status) l.status[b] = bad ? TAOT_ST_BAD_INPUT : 0u;
+  __syncthreads();
+  if (threadIdx.x >= kWave || n == 0) return;
+  if (b == B)
+    order_positions<kRankBits>(n, R, home, [&](int32_t e, int32_t h, int32_t at) { l.own_at[e] = at + K * h; }, cnt);
+  else
+    order_positions<kExpertBits>(n, E - 1, slot, [&](int32_t s, int32_t, int32_t at) { l.slot_of[(int64_t)b * S + at] = s; },
+                                 cnt);
 }
 
 // hist[row][chunk][e]: copies of expert e in the chunk; e = E: ids that are no
@@ -184,17 +188,18 @@ __device__ void lists(const Lists& l, int32_t b, int32_t B, int32_t R, int32_t E
 // finish, so they ride along.
 __global__ void __launch_bounds__(kThreads)
 count_kernel(Lists l, int32_t B, int32_t R, int32_t K, const int32_t* __restrict__ ids, int64_t N, int32_t E,
-             int32_t chunk, int32_t chunks, int64_t jobs, int waves, int32_t* __restrict__ hist) {
+             int32_t chunk, int32_t chunks, int32_t blocks_of_row, int waves, int32_t* __restrict__ hist) {
   extern __shared__ int32_t cnt[];
   if ((int32_t)blockIdx.x <= B) {
     lists(l, (int32_t)blockIdx.x, B, R, E, K, cnt);
     return;
   }
   const int lane = threadIdx.x & (kWave - 1), wid = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-  const int64_t job = ((int64_t)blockIdx.x - B - 1) * waves + wid;
-  if (wid >= waves || job >= jobs) return;
+  const uint32_t block = blockIdx.x - (uint32_t)B - 1, in_row = block % (uint32_t)blocks_of_row;
+  const int32_t my_chunk = (int32_t)in_row * waves + wid;
+  if (wid >= waves || my_chunk >= chunks) return;
   int32_t* mine = cnt + wid * (E + 1);
-  const int64_t row = job / chunks, lo = (job % chunks) * (int64_t)chunk;
+  const int64_t row = block / (uint32_t)blocks_of_row, job = row * chunks + my_chunk, lo = my_chunk * (int64_t)chunk;
   const int32_t n = (int32_t)min((int64_t)chunk, N - lo);
   const int32_t* src = ids + row * N + lo;
   for (int32_t e = lane; e <= E; e += kWave) mine[e] = 0;
@@ -228,8 +233,8 @@ bases_kernel(int32_t* __restrict__ hist, int32_t E, int32_t chunks, int32_t* __r
   constexpr int kGroups = kBaseThreads / kWave;
   __shared__ int32_t part[kGroups][kWave];
   const int32_t tiles = (E + kWave) / kWave;
-  const int64_t row = blockIdx.x / tiles;
-  const int32_t c = threadIdx.x % kWave, g = threadIdx.x / kWave, e = (int32_t)(blockIdx.x % tiles) * kWave + c;
+  const int64_t row = blockIdx.x / (uint32_t)tiles;
+  const int32_t c = threadIdx.x % kWave, g = threadIdx.x / kWave, e = (int32_t)(blockIdx.x % (uint32_t)tiles) * kWave + c;
   const int32_t each = (chunks + kGroups - 1) / kGroups, lo = min(g * each, chunks), hi = min(lo + each, chunks);
   int32_t* h = hist + row * chunks * (E + 1) + e;
   int32_t sum = 0, v[kHeld];
@@ -275,9 +280,10 @@ struct Tables {
   const int32_t* slot_of;     // [B][S]       slots by expert
   const int32_t* total;       // [rows][E + 1]
   int64_t* upto;              // [rows][S + 1]  running sum of X over the slots by expert
-  int2* guest;                // [rows][S]    of the slots by expert: copies of the expert that slots before take,
-                              //              and the position of its occurrence 0, were it this slot's
-  int2* own;                  // [rows][E]    copies at guests; position of occurrence 0, were it at home
+  // [rows][E + S], of a row first its experts: copies at guests, and the position of occurrence 0, were it at home;
+  // then its slots by expert: copies of the expert that slots before take, and the position of its occurrence 0, were
+  // it this slot's
+  int2* shares;
   int32_t* placed;            // [rows]       copies that go somewhere
 };
 
@@ -353,12 +359,12 @@ tables_kernel(Tables t, const int32_t* __restrict__ slot_expert, const int32_t* 
   __shared__ int64_t part64[kTableThreads / kWave];
   __shared__ int32_t part[kTableThreads / kWave];
   const int tid = threadIdx.x;
-  const int64_t row = blockIdx.x, b = row / rows;
-  const int32_t S = R * K, I = E + S, r = rank0 + (int32_t)(row % rows);
+  const int64_t row = blockIdx.x, b = blockIdx.x / (uint32_t)rows;
+  const int32_t S = R * K, I = E + S, r = rank0 + (int32_t)(blockIdx.x % (uint32_t)rows);
   int32_t* out = offsets + row * (I + 1);
   Row w{t.own_at, t.rank_first, t.slot_first + b * (E + 1), t.slot_of + b * S, t.total + row * (E + 1),
-        LDS ? room : t.upto + row * (S + 1), LDS ? reinterpret_cast<int32_t*>(room + S + 1) : out, t.guest + row * S,
-        t.own + row * E};
+        LDS ? room : t.upto + row * (S + 1), LDS ? reinterpret_cast<int32_t*>(room + S + 1) : out,
+        t.shares + row * (E + S) + E, t.shares + row * (E + S)};
   const int32_t placed = tables(w, slot_expert + b * S, X + (b * R + r) * (int64_t)S, R, E, K, sends + row * R, part64,
                                 part);
   if (tid == 0) {
@@ -374,13 +380,40 @@ tables_kernel(Tables t, const int32_t* __restrict__ slot_expert, const int32_t* 
   }
 }
 
+// What the copies of an expert in a row go to, in LDS or in memory.
+struct Shares {
+  const int2* own;
+  const int32_t* first;
+  const int2* guest;
+};
+
+// A run of an expert's occurrences that go to one place: position = base + occurrence, below `end`.
+struct Stretch {
+  int32_t base, end;
+};
+__device__ __forceinline__ Stretch stretch(const Shares& s, int32_t e, int32_t j) {
+  const int2 o = s.own[e];
+  if (j >= o.x) return Stretch{o.y, INT32_MAX};
+  int32_t a = s.first[e], z = s.first[e + 1];
+  const int32_t last = z;
+  while (a + 1 < z) {  // guest[a].x <= j < guest[z].x
+    const int32_t mid = (a + z) / 2;
+    if (s.guest[mid].x <= j) a = mid;
+    else z = mid;
+  }
+  return Stretch{s.guest[a].y, a + 1 < last ? s.guest[a + 1].x : o.x};
+}
+
 // A wave: ids src[0 .. n) of a row, n > 0, in order; mine[e]: occurrences of e
-// before them.  E <= 2^BITS.
-template <int BITS>
+// before them.  E <= 2^BITS.  KEEP: mine[e] holds the stretch of the next
+// occurrence too (j, base, end), which most copies fall into; else every copy
+// looks its own up.
+template <int BITS, bool KEEP>
 __device__ __forceinline__ void place(const int32_t* __restrict__ src, int32_t n, int32_t E, int32_t* mine,
-                                      const int2* own, const int32_t* first, const int2* guest, int32_t placed,
-                                      int32_t dropped, int32_t* __restrict__ dst) {
+                                      const Shares& shares, int32_t placed, int32_t dropped,
+                                      int32_t* __restrict__ dst) {
   const int lane = threadIdx.x & (kWave - 1);
+  int4* kept = reinterpret_cast<int4*>(mine);
   int32_t next[kUnroll];
   auto fetch = [&](int32_t i0) {  // past the end: the last id again
 #pragma unroll
@@ -388,9 +421,8 @@ __device__ __forceinline__ void place(const int32_t* __restrict__ src, int32_t n
   };
   fetch(0);
   for (int32_t i0 = 0; i0 < n; i0 += kUnroll * kWave) {
-    int32_t e[kUnroll], j[kUnroll];
+    int32_t e[kUnroll], j[kUnroll], p[kUnroll];
     Same m[kUnroll];
-    int2 o[kUnroll];
     bool in[kUnroll];
 #pragma unroll
     for (int u = 0; u < kUnroll; ++u) {
@@ -402,85 +434,111 @@ __device__ __forceinline__ void place(const int32_t* __restrict__ src, int32_t n
     for (int u = 0; u < kUnroll; ++u) {  // ids that are no expert are one key more
       const uint64_t experts = __ballot(in[u] & (e[u] < E)), others = __ballot(in[u] & (e[u] == E));
       m[u] = same_key<BITS>((uint32_t)e[u], experts);
-      m[u].lo = e[u] < E ? m[u].lo : (uint32_t)others;
-      m[u].hi = e[u] < E ? m[u].hi : (uint32_t)(others >> 32);
-      o[u] = own[min(e[u], E - 1)];
+      if (others != 0) {
+        m[u].lo = e[u] < E ? m[u].lo : (uint32_t)others;
+        m[u].hi = e[u] < E ? m[u].hi : (uint32_t)(others >> 32);
+      }
     }
 #pragma unroll
     for (int u = 0; u < kUnroll; ++u) {
       const int below = m[u].below();
-      j[u] = mine[e[u]] + below;
-      __builtin_amdgcn_wave_barrier();
-      if (in[u] & (below + 1 == m[u].all())) mine[e[u]] = j[u] + 1;
+      const bool last = in[u] & (below + 1 == m[u].all());
+      if constexpr (KEEP) {
+        const int4 k = kept[e[u]];
+        Stretch s{k.y, k.z};
+        j[u] = k.x + below;
+        if (j[u] >= s.end) s = stretch(shares, e[u], j[u]);
+        p[u] = s.base + j[u];
+        __builtin_amdgcn_wave_barrier();
+        if (last) kept[e[u]] = int4{j[u] + 1, s.base, s.end, 0};
+      } else {
+        j[u] = mine[e[u]] + below;
+        __builtin_amdgcn_wave_barrier();
+        if (last) mine[e[u]] = j[u] + 1;
+      }
       __builtin_amdgcn_wave_barrier();
     }
 #pragma unroll
     for (int u = 0; u < kUnroll; ++u) {
-      int32_t p = (e[u] < E ? o[u].y : dropped) + j[u];
-      if ((e[u] < E) & (j[u] < o[u].x)) {
-        int32_t a = first[e[u]], z = first[e[u] + 1];  // guest[a].x <= j < guest[z].x
-        while (a + 1 < z) {
-          const int32_t mid = (a + z) / 2;
-          if (guest[mid].x <= j[u]) a = mid;
-          else z = mid;
-        }
-        p = guest[a].y + j[u];
-      }
-      if (in[u]) dst[i0 + u * kWave + lane] = p < placed ? p : ~p;
+      if (!KEEP) p[u] = (e[u] < E ? stretch(shares, e[u], j[u]).base : dropped) + j[u];
+      if (in[u]) dst[i0 + u * kWave + lane] = p[u] < placed ? p[u] : ~p[u];
     }
   }
 }
 
-// n words into LDS by `threads` threads, four loads at a time.
+// n words into LDS by `threads` threads, eight loads at a time.
 __device__ __forceinline__ void bring(int32_t* to, const int32_t* __restrict__ from, int32_t n, int i, int threads) {
-  for (; i < n; i += 4 * threads) {
-    int32_t v[4];
+  for (; i < n; i += 8 * threads) {
+    int32_t v[8];
 #pragma unroll
-    for (int u = 0; u < 4; ++u) v[u] = from[min(i + u * threads, n - 1)];
+    for (int u = 0; u < 8; ++u) v[u] = from[min(i + u * threads, n - 1)];
 #pragma unroll
-    for (int u = 0; u < 4; ++u)
+    for (int u = 0; u < 8; ++u)
       if (i + u * threads < n) to[i + u * threads] = v[u];
   }
 }
 
-// LDS: the row's tables are brought into LDS first; a block then works on
-// chunks of one row.
-template <bool LDS, int BITS>
+// KEEP as in place(), four words of LDS an expert and wave instead of one; the
+// row's tables are brought into LDS then, which the waves' first stretches come
+// from.  A block works on chunks of one row.
+template <bool KEEP, int BITS>
 __global__ void __launch_bounds__(kThreads)
 place_kernel(const int32_t* __restrict__ ids, Tables t, const int32_t* __restrict__ hist, int64_t N, int32_t rows,
              int32_t E, int32_t S, int32_t chunk, int32_t chunks, int32_t blocks_of_row, int waves,
              int32_t* __restrict__ pos) {
-  extern __shared__ int32_t cnt[];
+  extern __shared__ int4 stretches[];
   const int lane = threadIdx.x & (kWave - 1), wid = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-  const int64_t row = blockIdx.x / blocks_of_row, b = row / rows;
-  const int32_t my_chunk = (int32_t)(blockIdx.x % blocks_of_row) * waves + wid;
-  const int2* own = t.own + row * E;
-  const int32_t* first = t.slot_first + b * (E + 1);
-  const int2* guest = t.guest + row * S;
+  const uint32_t at_row = blockIdx.x / (uint32_t)blocks_of_row;
+  const int64_t row = at_row, b = at_row / (uint32_t)rows;
+  const int32_t my_chunk = (int32_t)(blockIdx.x % (uint32_t)blocks_of_row) * waves + wid;
   const bool works = wid < waves && my_chunk < chunks;
-  const int64_t job = row * chunks + my_chunk, lo = my_chunk * (int64_t)chunk;
-  int32_t* mine = cnt + wid * (E + 1);
-  if (works) bring(mine, hist + job * (E + 1), E + 1, lane, kWave);
-  if constexpr (LDS) {
-    int32_t* own_l = cnt + ((waves * (E + 1) + 1) & ~1);
-    int32_t *guest_l = own_l + 2 * E, *first_l = guest_l + 2 * S;
-    bring(own_l, reinterpret_cast<const int32_t*>(own), 2 * E, threadIdx.x, kThreads);
-    bring(guest_l, reinterpret_cast<const int32_t*>(guest), 2 * S, threadIdx.x, kThreads);
-    bring(first_l, first, E + 1, threadIdx.x, kThreads);
-    own = reinterpret_cast<const int2*>(own_l);
-    guest = reinterpret_cast<const int2*>(guest_l);
-    first = first_l;
-  }
-  __syncthreads();
-  if (!works) return;
-  const int32_t n = (int32_t)min((int64_t)chunk, N - lo);
+  const int64_t job = row * chunks + (works ? my_chunk : 0), lo = my_chunk * (int64_t)chunk;
+  Shares shares{t.shares + row * (E + S), t.slot_first + b * (E + 1), t.shares + row * (E + S) + E};
   const int32_t dropped = (int32_t)(N - t.total[row * (E + 1) + E]);  // where ids that are no expert begin
-  place<BITS>(ids + row * N + lo, n, E, mine, own, first, guest, t.placed[row], dropped, pos + row * N + lo);
+  int32_t* mine = reinterpret_cast<int32_t*>(stretches) + (KEEP ? 4 : 1) * wid * (E + 1);
+  if constexpr (KEEP) {
+    int32_t *own = reinterpret_cast<int32_t*>(stretches + waves * (E + 1)), *first = own + 2 * (E + S);
+    int32_t j[4], f[4];
+    const int32_t* base = hist + job * (E + 1);
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      j[u] = base[min(lane + u * kWave, E)];
+      f[u] = shares.first[min((int)threadIdx.x + u * kThreads, E)];
+    }
+    bring(own, reinterpret_cast<const int32_t*>(shares.own), 2 * (E + S), threadIdx.x, kThreads);
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+      if ((int)threadIdx.x + u * kThreads <= E) first[threadIdx.x + u * kThreads] = f[u];
+    if (E >= 4 * kThreads) bring(first, shares.first, E + 1, threadIdx.x + 4 * kThreads, kThreads);
+    shares = Shares{reinterpret_cast<const int2*>(own), first, reinterpret_cast<const int2*>(own) + E};
+    __syncthreads();
+    if (!works) return;
+    int4* kept = reinterpret_cast<int4*>(mine);
+    for (int32_t e0 = lane; e0 <= E; e0 += 4 * kWave) {
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const int32_t e = e0 + u * kWave;
+        if (e > E) continue;
+        Stretch s{dropped, INT32_MAX};
+        if (e < E) s = stretch(shares, e, j[u]);
+        kept[e] = int4{j[u], s.base, s.end, 0};
+      }
+#pragma unroll
+      for (int u = 0; u < 4; ++u) j[u] = base[min(e0 + (u + 4) * kWave, E)];
+    }
+  } else {
+    if (!works) return;
+    bring(mine, hist + job * (E + 1), E + 1, lane, kWave);
+  }
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  const int32_t n = (int32_t)min((int64_t)chunk, N - lo);
+  place<BITS, KEEP>(ids + row * N + lo, n, E, mine, shares, t.placed[row], dropped, pos + row * N + lo);
 }
 
 // A short row by one block and in one launch: everything above, in LDS.
 struct RowRoom {
-  size_t cnt, own_at, rank_first, first, slot_of, total, upto, off, guest, own, hist, bytes;
+  size_t rank_cnt, slot_cnt, own_at, rank_first, first, slot_of, total, upto, off, guest, own, hist, bytes;
 };
 __host__ __device__ inline RowRoom row_room(int32_t R, int32_t E, int32_t S, int waves) {
   RowRoom r{};
@@ -493,7 +551,8 @@ __host__ __device__ inline RowRoom row_room(int32_t R, int32_t E, int32_t S, int
   r.upto = take((size_t)(S + 1) * 8);
   r.guest = take((size_t)S * 8);
   r.own = take((size_t)E * 8);
-  r.cnt = take((size_t)((E > R ? E : R) + 1) * 4);
+  r.rank_cnt = take((size_t)(R + 1) * 4);
+  r.slot_cnt = take((size_t)(E + 1) * 4);
   r.own_at = take((size_t)E * 4);
   r.rank_first = take((size_t)(R + 1) * 4);
   r.first = take((size_t)(E + 1) * 4);
@@ -516,32 +575,47 @@ row_kernel(const int32_t* __restrict__ home, const int32_t* __restrict__ slot_ex
   __shared__ int32_t part[kTableThreads / kWave];
   __shared__ int32_t bad_home;
   const int tid = threadIdx.x, lane = tid & (kWave - 1), wid = __builtin_amdgcn_readfirstlane(tid / kWave);
-  const int64_t row = blockIdx.x, b = row / rows;
-  const int32_t S = R * K, I = E + S, r = rank0 + (int32_t)(row % rows);
+  const int64_t row = blockIdx.x, b = blockIdx.x / (uint32_t)rows;
+  const int32_t S = R * K, I = E + S, r = rank0 + (int32_t)(blockIdx.x % (uint32_t)rows);
   const RowRoom at = row_room(R, E, S, waves);
   char* base = reinterpret_cast<char*>(room);
   auto words = [&](size_t o) { return reinterpret_cast<int32_t*>(base + o); };
   int32_t *own_at = words(at.own_at), *rank_first = words(at.rank_first), *first = words(at.first),
-          *slot_of = words(at.slot_of), *total = words(at.total), *hist = words(at.hist);
+          *slot_of = words(at.slot_of), *total = words(at.total), *hist = words(at.hist), *rank_cnt = words(at.rank_cnt),
+          *slot_cnt = words(at.slot_cnt);
   int2 *guest = reinterpret_cast<int2*>(base + at.guest), *own = reinterpret_cast<int2*>(base + at.own);
   // `waves` runs of the row, in order
   const int32_t run = (N + waves * kWave - 1) / (waves * kWave) * kWave, lo = min(wid * run, N), n = min(run, N - lo);
   const int32_t* src = ids + row * N + lo;
   int32_t* mine = hist + wid * (E + 1);
   if (tid == 0) bad_home = 0;
+  for (int32_t q = tid; q <= R; q += kTableThreads) rank_cnt[q] = 0;
+  for (int32_t q = tid; q <= E; q += kTableThreads) slot_cnt[q] = 0;
   if (wid < waves)
     for (int32_t e = lane; e <= E; e += kWave) mine[e] = 0;
-  order_experts<kTableThreads>(home, R, E, K, own_at, rank_first, words(at.cnt), part);
+  const HomeKey home_key{home, R};
+  const SlotKey slot_key{slot_expert + b * S, E};
+  __syncthreads();
+  order_counts<kTableThreads>(E, home_key, rank_cnt);
+  order_counts<kTableThreads>(S, slot_key, slot_cnt);
+  for (int32_t e = tid; e < E; e += kTableThreads)
+    if (home_key(e) == R) bad_home = 1;
+  __syncthreads();
+  order_sums<kTableThreads>(R, rank_first, rank_cnt, part);
+  order_sums<kTableThreads>(E, first, slot_cnt, part);
+  __syncthreads();
+  // the last two waves order the experts and the slots, the ids' runs begin with the first
+  if (wid == kTableThreads / kWave - 1)
+    order_positions<kRankBits>(E, R, home_key, [&](int32_t e, int32_t h, int32_t at) { own_at[e] = at + K * h; }, rank_cnt);
+  if (wid == kTableThreads / kWave - 2 && S > 0)
+    order_positions<BITS>(S, E - 1, slot_key, [&](int32_t s, int32_t, int32_t at) { slot_of[at] = s; }, slot_cnt);
   if (wid < waves) {
     for (int32_t i = lane; i < n; i += kWave) {
       const int32_t e = src[i];
       atomicAdd(&mine[(uint32_t)e < (uint32_t)E ? e : E], 1);
     }
   }
-  for (int32_t e = tid; e < E; e += kTableThreads)
-    if (home[e] < 0 || home[e] >= R) bad_home = 1;
   __syncthreads();
-  order_slots<kTableThreads>(slot_expert + b * S, S, E, first, slot_of, words(at.cnt), part);
   for (int32_t e = tid; e <= E; e += kTableThreads) {
     int32_t sum = 0;
     for (int w = 0; w < waves; ++w) {
@@ -561,7 +635,7 @@ row_kernel(const int32_t* __restrict__ home, const int32_t* __restrict__ slot_ex
   if (tid == 0) bad[row] = (bad_home ? TAOT_ST_BAD_INPUT : 0u) | (total[E] > 0 ? TAOT_ST_BAD_ID : 0u);
   __syncthreads();
   if (wid < waves && n > 0)
-    place<BITS>(src, n, E, mine, own, first, guest, placed, N - total[E], pos + row * N + lo);
+    place<BITS, false>(src, n, E, mine, Shares{own, first, guest}, placed, N - total[E], pos + row * N + lo);
 }
 
 // status[b] of the rows' bits.
@@ -572,6 +646,16 @@ status_kernel(const uint32_t* __restrict__ bad, int32_t B, int32_t rows, uint32_
   uint32_t s = 0;
   for (int32_t r = 0; r < rows; ++r) s |= bad[b * rows + r];
   status[b] = s;
+}
+
+// The token of a group of WAVES waves, among `all`, and the first row of its row of copies.
+struct Token {
+  int64_t t, row0;
+};
+template <int WAVES>
+__device__ __forceinline__ Token token_of(int64_t tokens, int32_t k) {
+  const uint32_t t = blockIdx.x * (4 / WAVES) + __builtin_amdgcn_readfirstlane(threadIdx.x / (WAVES * kWave));
+  return Token{t, (int64_t)(t / (uint32_t)tokens) * tokens * k};
 }
 
 // ---- rows ------------------------------------------------------------------------
@@ -618,10 +702,10 @@ template <int WAVES>
 __global__ void __launch_bounds__(256)
 rows_kernel(Payload a, Payload b, int64_t all, int64_t tokens, int32_t k, const int32_t* __restrict__ pos) {
   constexpr int kLanes = WAVES * kWave;
-  const int64_t t = (int64_t)blockIdx.x * (256 / kLanes) + threadIdx.x / kLanes;
+  const auto [t, row0] = token_of<WAVES>(tokens, k);
   if (t >= all) return;
   const int lane = threadIdx.x % kLanes;
-  const int64_t N = tokens * k, row0 = t / tokens * N;
+  const int64_t N = tokens * k;
   spread<WAVES>(a, t, row0, N, k, pos + t * k, lane);
   if (b.in) spread<WAVES>(b, t, row0, N, k, pos + t * k, lane);
 }
@@ -632,11 +716,11 @@ combine_kernel(const T* __restrict__ y, const int32_t* __restrict__ pos, const f
                int64_t all, int64_t tokens, int32_t k, int32_t H, T* __restrict__ out) {
   constexpr int kLanes = WAVES * kWave;
   constexpr int kAhead = 4;
-  const int64_t t = (int64_t)blockIdx.x * (256 / kLanes) + threadIdx.x / kLanes;
+  const auto [t, row0] = token_of<WAVES>(tokens, k);
   if (t >= all) return;
   const int lane = threadIdx.x % kLanes;
   const int64_t N = tokens * k;
-  const T* base = y + t / tokens * N * H;
+  const T* base = y + row0 * H;
   for (int32_t c = 8 * lane; c < H; c += 8 * kLanes) {
     f32x8 acc = 0.f;
     for (int32_t j0 = 0; j0 < k; j0 += kAhead) {
@@ -669,10 +753,10 @@ combine_backward_kernel(const T* __restrict__ dout, const T* __restrict__ y, con
   using Raw = typename Row8<T>::vec;
   constexpr int kLanes = WAVES * kWave, kAhead = 4;
   __shared__ float part[2][kAhead][4];
-  const int64_t t = (int64_t)blockIdx.x * (256 / kLanes) + threadIdx.x / kLanes;
+  const auto [t, row0] = token_of<WAVES>(tokens, k);
   if (t >= all) return;  // whole waves, and whole blocks where waves share a token
   const int lane = threadIdx.x % kLanes;
-  const int64_t N = tokens * k, row0 = t / tokens * N;
+  const int64_t N = tokens * k;
   int slot = 0;
   for (int32_t j0 = 0; j0 < k; j0 += kAhead, slot ^= 1) {
     float dot[kAhead], w[kAhead];
@@ -730,8 +814,7 @@ combine_backward_kernel(const T* __restrict__ dout, const T* __restrict__ y, con
 // Ids of a wave: enough waves to fill the chip, and no more counters than ids.
 int32_t chunk_of(int64_t rows, int64_t N, int32_t E) {
   int64_t c = kChunkMin;
-  const int64_t want = getenv("DW") ? atoi(getenv("DW")) : kWavesWanted;
-  while (c < kChunkMax && (c < E || rows * ((N + c - 1) / c) > want)) c *= 2;
+  while (c < kChunkMax && (c < E || rows * ((N + c - 1) / c) > kWavesWanted)) c *= 2;
   return (int32_t)c;
 }
 
@@ -758,8 +841,7 @@ Plan carve(void* ws, int32_t B, int32_t rows, int64_t N, int32_t R, int32_t E, i
   p.slot_of = c.take<int32_t>((size_t)B * S);
   p.total = c.take<int32_t>(n * (E + 1));
   p.t.upto = c.take<int64_t>(n * (S + 1));
-  p.t.guest = c.take<int2>(n * S);
-  p.t.own = c.take<int2>(n * E);
+  p.t.shares = c.take<int2>(n * (E + S));
   p.t.placed = c.take<int32_t>(n);
   p.hist = c.take<int32_t>(n * chunks * (E + 1));
   p.t.own_at = p.own_at;
@@ -802,7 +884,6 @@ taot_status launch_dispatch_map(const int32_t* ids, int32_t B, int32_t rows, int
   const Plan p = carve(ws, B, rows, N, R, E, K);
   const int64_t n = (int64_t)B * rows;
   const int32_t chunk = chunk_of(n, N, E), chunks = (int32_t)((N + chunk - 1) / chunk);
-  const int64_t jobs = n * chunks;
   const int32_t S = R * K, I = E + S, most = E > R ? E : R;
   const Lists lists{home, slot_expert, p.own_at, p.rank_first, p.slot_first, p.slot_of, status};
   const size_t list_lds = (size_t)(most + 1) * sizeof(int32_t), row_lds = (size_t)(E + 1) * sizeof(int32_t);
@@ -825,22 +906,22 @@ taot_status launch_dispatch_map(const int32_t* ids, int32_t B, int32_t rows, int
     }
   }
   if (!allow_lds(reinterpret_cast<const void*>(count_kernel), count_lds)) return TAOT_ERR_LAUNCH;
-  count_kernel<<<(unsigned)(B + 1 + (jobs + waves - 1) / waves), kThreads, count_lds, stream>>>(
-      lists, B, R, K, ids, N, E, chunk, chunks, jobs, waves, p.hist);
+  const int32_t blocks = chunks > 0 ? (chunks + waves - 1) / waves : 1;  // of a row
+  count_kernel<<<(unsigned)(B + 1 + (chunks > 0 ? n * blocks : 0)), kThreads, count_lds, stream>>>(
+      lists, B, R, K, ids, N, E, chunk, chunks, blocks, waves, p.hist);
   bases_kernel<<<(unsigned)(n * ((E + kWave) / kWave)), kBaseThreads, 0, stream>>>(p.hist, E, chunks, p.total);
   const size_t table_lds = (size_t)(S + 1) * sizeof(int64_t) + (size_t)(I + 1) * sizeof(int32_t);
   const bool small_tables = table_lds <= kTableLds;
   (small_tables ? tables_kernel<true> : tables_kernel<false>)<<<(unsigned)n, kTableThreads, small_tables ? table_lds : 0,
                                                                stream>>>(p.t, slot_expert, X, rows, rank0, R, E, K,
                                                                          offsets, sends, status);
-  if (jobs > 0) {
-    const size_t extra = (size_t)(E + S) * sizeof(int2) + (size_t)(E + 1) * sizeof(int32_t) + sizeof(int2);
-    const bool small_rows = extra <= kTableLds;
-    const size_t lds = waves * row_lds + (small_rows ? extra : 0);
-    auto* kernel = small_rows ? with_bits(bits, [](auto n) { return place_kernel<true, n.value>; })
-                              : with_bits(bits, [](auto n) { return place_kernel<false, n.value>; });
+  if (chunks > 0) {
+    const size_t kept = 4 * waves * row_lds + (size_t)(E + S) * sizeof(int2) + row_lds;
+    const bool keep = kept <= kKeepLds;
+    const size_t lds = keep ? kept : waves * row_lds;
+    auto* kernel = keep ? with_bits(bits, [](auto n) { return place_kernel<true, n.value>; })
+                        : with_bits(bits, [](auto n) { return place_kernel<false, n.value>; });
     if (!allow_lds(reinterpret_cast<const void*>(kernel), lds)) return TAOT_ERR_LAUNCH;
-    const int32_t blocks = (chunks + waves - 1) / waves;
     kernel<<<(unsigned)(n * blocks), kThreads, lds, stream>>>(ids, p.t, p.hist, N, rows, E, S, chunk, chunks, blocks, waves,
                                                             pos);
   }
