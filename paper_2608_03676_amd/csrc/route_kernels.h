@@ -263,7 +263,7 @@ route_kernel(RouteArgs a, Layout lay) {
 template <typename T>
 __device__ void route_block(const RouteArgs& a, int64_t t, int* keys) {
   __shared__ int value[TAOT_MAX_ROUTE_GROUPS];
-  __shared__ unsigned long long found[4];
+  __shared__ int found[2][2][4];
   __shared__ float part[2][4];
   __shared__ int chosen[kWave];
   const int tid = threadIdx.x, lane = tid & (kWave - 1), wid = tid / kWave;
@@ -289,6 +289,7 @@ __device__ void route_block(const RouteArgs& a, int64_t t, int* keys) {
     __syncthreads();
     sum = part[1][0] + part[1][1] + part[1][2] + part[1][3];
   }
+#pragma unroll 4
   for (int e = tid; e < a.E; e += 256) {
     const float x = logit(e);
     if (!a.bias) keys[e] = key_of(x);
@@ -324,32 +325,41 @@ __device__ void route_block(const RouteArgs& a, int64_t t, int* keys) {
     }
     __syncthreads();
   }
-  for (int j = 0; j < a.k; ++j) {
-    int best = kNone, at = INT32_MAX;
+  // each thread's best key; after a round only the winner's thread looks again
+  int best, at;
+  auto look = [&] {
+    best = kNone;
+    at = INT32_MAX;
+#pragma unroll 4
     for (int e = tid; e < a.E; e += 256) {
       const int x = keys[e];
       at = x > best ? e : at;
       best = max(best, x);
     }
-    // larger key first, then the lower expert
-    unsigned long long p = ((unsigned long long)((uint32_t)best ^ 0x80000000u) << 32) | (0x7fffffffu - (uint32_t)at);
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) {
-      const unsigned long long q = __shfl_xor(p, o, kWave);
-      p = q > p ? q : p;
-    }
-    if (lane == 0) found[wid] = p;
-    __syncthreads();
-#pragma unroll
-    for (int w = 0; w < 4; ++w) p = found[w] > p ? found[w] : p;
-    const bool none = (p >> 32) == 0;
-    const int win = (int)(0x7fffffffu - (uint32_t)p);
-    if (tid == 0) {
-      chosen[j] = none ? -1 : win;
-      if (!none) keys[win] = kNone;
+  };
+  look();
+  for (int j = 0; j < a.k; ++j) {
+    const int most = block_reduce<kWave>(best, MaxOp()), first = block_reduce<kWave>(best == most ? at : INT32_MAX, MinOp());
+    int(*turn)[4] = found[j & 1];  // two sets of words take turns: one barrier a round
+    if (lane == 0) {
+      turn[0][wid] = most;
+      turn[1][wid] = first;
     }
     __syncthreads();
+    int top = turn[0][0], win = turn[1][0];
+#pragma unroll
+    for (int w = 1; w < 4; ++w) {
+      const int x = turn[0][w], e = turn[1][w];
+      win = x > top ? e : x == top ? min(win, e) : win;
+      top = max(top, x);
+    }
+    if (tid == 0) chosen[j] = top == kNone ? -1 : win;
+    if (top != kNone && tid == win % 256) {
+      keys[win] = kNone;
+      look();
+    }
   }
+  __syncthreads();
   if (wid == 0) finish<kWave, T>(a, t, lane < a.k, lane, lane < a.k ? chosen[lane] : -1, m, sum);
 }
 
@@ -395,10 +405,14 @@ route_few_kernel(RouteArgs a, Layout lay) {
   static_assert(V >= DEPTH, "every place of the list holds a word");
   constexpr int W = Place::W;
   constexpr int kInf16 = std::is_same<T, __bf16>::value ? 0x7F80 : 0x7C00;
-  constexpr int kShift = MODE == kExact16 ? 16 : log2_of(L * V), kLow = (1 << kShift) - 1;
+  constexpr bool kWide = L == 64 && V > 16;
+  // Words of a wide row's keys in fixed point hold the place alone, which leaves more bits to the key: two lanes'
+  // words may then be equal, and are undecided.
+  constexpr bool kByLane = kWide && MODE != kExact16;
+  constexpr int kShift = MODE == kExact16 ? 16 : log2_of(kByLane ? V : L * V), kLow = (1 << kShift) - 1;
   constexpr float kMost = (float)((1 << (31 - kShift < 24 ? 31 - kShift : 24)) - 1);  // largest key in fixed point
   constexpr int kRanOut = INT32_MIN + 1;  // behind a lane's last word
-  constexpr bool kWide = L == 64 && V > 16;
+  auto low = [](int v) { return (uint32_t)(kLow - (kByLane ? v : Place::away(v))); };
   const int lane = threadIdx.x & (kWave - 1), sl = lane % L, base = lane - sl;
   const int64_t t = ((int64_t)blockIdx.x * 256 + threadIdx.x) / L;
   const bool live = t < a.T;
@@ -447,37 +461,41 @@ route_few_kernel(RouteArgs a, Layout lay) {
       const pair size = x & (short)0x7fff, sign = x >> (short)15;
       big = __builtin_elementwise_max(big, size);
       const uint32_t o = __builtin_bit_cast(uint32_t, (pair)((size ^ sign) - sign));
-      insert((int)((o << 16) | (uint32_t)(kLow - Place::away(v))));
-      insert((int)((o & 0xFFFF0000u) | (uint32_t)(kLow - Place::away(v + 1))));
+      insert((int)((o << 16) | low(v)));
+      insert((int)((o & 0xFFFF0000u) | low(v + 1)));
     }
     open |= max((int)big[0], (int)big[1]) > kInf16;  // NaN
   } else if constexpr (MODE == kLogit) {
 #pragma unroll
     for (int v = 0; v < V; ++v) {
       const uint32_t q = (uint32_t)fmaf(logit(v) - m, kMost / kLogitRange, kMost);  // negative and NaN: 0
-      insert((int)((q << kShift) | (uint32_t)(kLow - Place::away(v))));
+      insert((int)((q << kShift) | low(v)));
     }
     apart_two = 8;  // each key is cut by less than one unit
   } else {
     // fixed point over the range of the keys, by the largest bias of all experts (infinite or NaN: exact keys)
     float most = 0.f, least = INFINITY;
-    float bias[kWide ? 1 : V];
-    if constexpr (kWide) {
-      for (int e = lane; e < a.E; e += kWave) most = fmaxf(most, fabsf(a.bias[e]));
-    } else {
+    constexpr int kPart = kWide ? 16 : V;  // biases held at a time
+    float bias[kPart];
+    auto fetch = [&](int v0) {
       if (at.whole) {
         typedef float four __attribute__((ext_vector_type(4)));
         typedef __attribute__((aligned(4))) four at4;
 #pragma unroll
-        for (int v = 0; v < V; v += 4) {
-          const four b = *reinterpret_cast<const at4*>(a.bias + max(0, min(at.index(v), a.E - 4)));
+        for (int v = 0; v < kPart; v += 4) {
+          const four b = *reinterpret_cast<const at4*>(a.bias + max(0, min(at.index(v0 + v), a.E - 4)));
 #pragma unroll
           for (int u = 0; u < 4; ++u) bias[v + u] = b[u];
         }
       } else {
 #pragma unroll
-        for (int v = 0; v < V; ++v) bias[v] = a.bias[min(at.index(v), a.E - 1)];
+        for (int v = 0; v < kPart; ++v) bias[v] = a.bias[min(at.index(v0 + v), a.E - 1)];
       }
+    };
+    if constexpr (kWide) {
+      for (int e = lane; e < a.E; e += kWave) most = fmaxf(most, fabsf(a.bias[e]));
+    } else {
+      fetch(0);
 #pragma unroll
       for (int v = 0; v < V; ++v) most = fmaxf(most, fabsf(bias[v]));
     }
@@ -485,18 +503,22 @@ route_few_kernel(RouteArgs a, Layout lay) {
     const float unit = (kMost - 16.f) / (1.f + 2.f * most), zero = most * unit + 4.f;
 #pragma unroll
     for (int v = 0; v < V; ++v) least = fminf(least, logit(v));
-    auto fill = [&](auto masked) {
+    auto fill = [&](int v0, auto masked) {
 #pragma unroll
-      for (int v = 0; v < V; ++v) {
-        const float x = logit(v);
-        const float b = fmaf(kWide ? a.bias[min(at.index(v), a.E - 1)] : bias[kWide ? 0 : v], unit, zero);
+      for (int v = 0; v < kPart; ++v) {
+        const float x = logit(v0 + v), b = fmaf(bias[v], unit, zero);
         const uint32_t k = (uint32_t)fmaf(__builtin_amdgcn_rcpf(1.f + exp_fast(-x)), unit, b);  // NaN: 0
         const uint32_t q = !masked.value || x > -INFINITY ? k : 0u;
-        insert((int)((q << kShift) | (uint32_t)(kLow - Place::away(v))));
+        insert((int)((q << kShift) | low(v0 + v)));
       }
     };
-    if (__ballot(least == -INFINITY) != 0) fill(std::true_type());
-    else fill(std::false_type());
+    const bool masked = __ballot(least == -INFINITY) != 0;
+#pragma unroll
+    for (int v0 = 0; v0 < V; v0 += kPart) {
+      if (kWide) fetch(v0);
+      if (masked) fill(v0, std::true_type());
+      else fill(v0, std::false_type());
+    }
     // The sigmoid's product, exponential, sum and reciprocal stay within 8 units of 2^-24, the exact key within 4
     // of the formula's value and 1 + |bias| of it for the sum; the fixed point adds less than 4 of its units.
     const float slack = 14.f * 0x1p-24f * (1.f + most) * unit;
@@ -504,8 +526,10 @@ route_few_kernel(RouteArgs a, Layout lay) {
     apart = 8 + (int)(2.f * fminf(slack, 1e6f));
     apart_two = 2 * apart;
   }
+  if constexpr (!kByLane) {
 #pragma unroll
-  for (int i = 0; i < DEPTH; ++i) best[i] -= at.first;  // the place's complement becomes the expert's
+    for (int i = 0; i < DEPTH; ++i) best[i] -= at.first;  // the place's complement becomes the expert's
+  }
 
   if constexpr (GROUPED) {
     int b1 = best[0] >> kShift, b2 = best[1] >> kShift, value;
@@ -531,19 +555,27 @@ route_few_kernel(RouteArgs a, Layout lay) {
     for (int i = 0; i < DEPTH; ++i) best[i] = stays ? best[i] : INT32_MIN;
   }
 
-  int mine = 0, top = 0;
+  int mine = 0, top = 0, id = 0;
   const int rounds = MODE == kExact16 ? a.k : a.k + 1;
   for (int j = 0; j < rounds; ++j) {
     open |= best[0] == kRanOut;
     top = block_reduce<L>(best[0], MaxOp());
     const bool won = best[0] == top && top > kRanOut;
+    if constexpr (kByLane) {
+      const uint64_t who = __ballot(won);
+      const int place = kLow - (best[0] & kLow);
+      const int e = lane_value(at.first + (GROUPED ? place : (place / W) * L * W + place % W),
+                               who != 0 ? __ffsll((unsigned long long)who) - 1 : 0);
+      open |= __popcll(who) > 1;
+      id = sl == j ? e : id;
+    }
 #pragma unroll
     for (int i = 0; i + 1 < DEPTH; ++i) best[i] = won ? best[i + 1] : best[i];
     best[DEPTH - 1] = won ? kRanOut : best[DEPTH - 1];
     mine = sl == j ? top : mine;
   }
   const bool chooses = live && sl < a.k;
-  int id = kLow - (mine & kLow);
+  if constexpr (!kByLane) id = kLow - (mine & kLow);
   if constexpr (MODE == kExact16) {
     id = mine >> kShift > -kInf16 ? id : -1;
   } else {
