@@ -666,7 +666,7 @@ struct Payload {
   int64_t bytes;
 };
 
-template <int WAVES>
+template <int WAVES, bool FAR>
 __device__ __forceinline__ void spread(const Payload& p, int64_t t, int64_t row0, int64_t N, int32_t k,
                                        const int32_t* __restrict__ pos, int lane) {
   constexpr int kLanes = WAVES * kWave;
@@ -688,7 +688,8 @@ __device__ __forceinline__ void spread(const Payload& p, int64_t t, int64_t row0
       const u32x4 w = q >= 0 ? v : u32x4(0);
       char* dst = p.out + (row0 + to) * p.bytes + c;
       if (n == 16) {
-        *reinterpret_cast<u32x4_at*>(dst) = w;
+        if constexpr (FAR) __builtin_nontemporal_store(w, reinterpret_cast<u32x4_at*>(dst));
+        else *reinterpret_cast<u32x4_at*>(dst) = w;
       } else {
 #pragma unroll
         for (int u = 0; u < 16; ++u)
@@ -698,7 +699,7 @@ __device__ __forceinline__ void spread(const Payload& p, int64_t t, int64_t row0
   }
 }
 
-template <int WAVES>
+template <int WAVES, bool FAR>
 __global__ void __launch_bounds__(256)
 rows_kernel(Payload a, Payload b, int64_t all, int64_t tokens, int32_t k, const int32_t* __restrict__ pos) {
   constexpr int kLanes = WAVES * kWave;
@@ -706,8 +707,8 @@ rows_kernel(Payload a, Payload b, int64_t all, int64_t tokens, int32_t k, const 
   if (t >= all) return;
   const int lane = threadIdx.x % kLanes;
   const int64_t N = tokens * k;
-  spread<WAVES>(a, t, row0, N, k, pos + t * k, lane);
-  if (b.in) spread<WAVES>(b, t, row0, N, k, pos + t * k, lane);
+  spread<WAVES, FAR>(a, t, row0, N, k, pos + t * k, lane);
+  if (b.in) spread<WAVES, false>(b, t, row0, N, k, pos + t * k, lane);
 }
 
 template <typename T, int WAVES>
@@ -742,10 +743,10 @@ combine_kernel(const T* __restrict__ y, const int32_t* __restrict__ pos, const f
   }
 }
 
-// dy[pos] = w dout, dw = <dout, y[pos]>; kAhead copies at a time.  The rows of dy
-// are written once, anywhere: past the caches (8192 tokens of 2048 in 16 bits, 8
-// copies: 114 us, 119 through them; 16384 of 512, 4 copies: 26 and 44 us).
-template <typename T, int WAVES>
+// dy[pos] = w dout, dw = <dout, y[pos]>; kAhead copies at a time.  Many rows of dy
+// go past the caches (8192 tokens of 2048 in 16 bits, 8 copies: 114 us, 119
+// through them; 16384 of 512, 4 copies: 26 and 44 us).
+template <typename T, int WAVES, bool FAR>
 __global__ void __launch_bounds__(256)
 combine_backward_kernel(const T* __restrict__ dout, const T* __restrict__ y, const int32_t* __restrict__ pos,
                         const float* __restrict__ weights, int64_t all, int64_t tokens, int32_t k, int32_t H,
@@ -786,8 +787,7 @@ combine_backward_kernel(const T* __restrict__ dout, const T* __restrict__ y, con
         if (any[u]) {
           T* p = dy + (row0 + (to[u] >= 0 ? to[u] : ~to[u])) * H + c;
           const f32x8 o = to[u] >= 0 ? d * w[u] : f32x8(0.f);
-          if (n >= 8) __builtin_nontemporal_store(__builtin_convertvector(o, Raw), reinterpret_cast<typename Row8<T>::at*>(p));
-          else store_row(p, o, n);
+          store_row<FAR>(p, o, n);
         }
       }
     }
@@ -934,8 +934,10 @@ taot_status launch_dispatch_rows(const void* x, int64_t row_bytes, const void* x
   const Payload a{static_cast<const char*>(x), static_cast<char*>(out), row_bytes};
   const Payload b{static_cast<const char*>(x_more), static_cast<char*>(out_more), more_bytes};
   const int64_t all = rows * tokens;
-  if (row_bytes > 2048) rows_kernel<4><<<(unsigned)all, 256, 0, stream>>>(a, b, all, tokens, k, pos);
-  else rows_kernel<1><<<(unsigned)((all + 3) / 4), 256, 0, stream>>>(a, b, all, tokens, k, pos);
+  with_far(all * k * row_bytes, [&](auto far) {
+    if (row_bytes > 2048) rows_kernel<4, far.value><<<(unsigned)all, 256, 0, stream>>>(a, b, all, tokens, k, pos);
+    else rows_kernel<1, far.value><<<(unsigned)((all + 3) / 4), 256, 0, stream>>>(a, b, all, tokens, k, pos);
+  });
   return hipGetLastError() == hipSuccess ? TAOT_OK : TAOT_ERR_LAUNCH;
 }
 
@@ -961,11 +963,11 @@ taot_status launch_combine_rows_backward(const void* dout, const void* y, const 
     using T = decltype(z);
     const T *d = static_cast<const T*>(dout), *in = static_cast<const T*>(y);
     T* o = static_cast<T*>(dy);
-    if (H > 1024)
-      combine_backward_kernel<T, 4><<<(unsigned)all, 256, 0, stream>>>(d, in, pos, weights, all, tokens, k, H, o, dweights);
-    else
-      combine_backward_kernel<T, 1><<<(unsigned)((all + 3) / 4), 256, 0, stream>>>(d, in, pos, weights, all, tokens, k, H,
-                                                                                  o, dweights);
+    with_far(all * k * H * (int64_t)sizeof(T), [&](auto far) {
+      auto* kernel = H > 1024 ? combine_backward_kernel<T, 4, far.value> : combine_backward_kernel<T, 1, far.value>;
+      kernel<<<(unsigned)(H > 1024 ? all : (all + 3) / 4), 256, 0, stream>>>(d, in, pos, weights, all, tokens, k, H, o,
+                                                                           dweights);
+    });
   });
 }
 

@@ -33,9 +33,12 @@ __device__ __forceinline__ u32x2 to_f8(f32x8 v, float inv) {
   return r;
 }
 
+template <bool FAR>
 __device__ __forceinline__ void store_f8(uint8_t* p, u32x2 v, int n) {
   if (n >= 8) {
-    *reinterpret_cast<u32x2_at*>(p) = v;
+    auto* to = reinterpret_cast<u32x2_at*>(p);
+    if constexpr (FAR) __builtin_nontemporal_store(v, to);
+    else *to = v;
     return;
   }
 #pragma unroll
@@ -60,7 +63,7 @@ __device__ __forceinline__ float row_reduce(float v, Op op, float (*part)[16], i
 // `waves` waves hold a row (one: four rows a block); of their lanes, lane l has
 // columns 8 (i lanes + l) .. + 7 for i < CPL, so a wave's accesses are contiguous
 // and a group of 8 m columns is m neighbouring lanes at one i.
-template <typename T, int CPL>
+template <typename T, int CPL, bool FAR>
 __global__ void __launch_bounds__(1024)
 add_rms_norm_kernel(const T* __restrict__ x, const T* __restrict__ residual, const void* __restrict__ weight,
                     bool w_f32, int64_t rows, int32_t H, float eps, int32_t group, T* __restrict__ h,
@@ -88,7 +91,7 @@ add_rms_norm_kernel(const T* __restrict__ x, const T* __restrict__ residual, con
 #pragma unroll
     for (int i = 0; i < CPL; ++i) {
       const int col = 8 * (i * lanes + lane);
-      store_row(h + at + col, v[i], H - col);
+      store_row<FAR>(h + at + col, v[i], H - col);
     }
   }
   const float s = 1.f / sqrtf(row_reduce(ss, SumOp(), part, 0, waves) / (float)H + eps);
@@ -99,14 +102,14 @@ add_rms_norm_kernel(const T* __restrict__ x, const T* __restrict__ residual, con
   for (int i = 0; i < CPL; ++i) {
     const int col = 8 * (i * lanes + lane), n = H - col;
     v[i] = v[i] * s * load_row_either<T>(weight, w_f32, col, n);
-    if (y) store_row(y + at + col, v[i], n);
+    if (y) store_row<FAR>(y + at + col, v[i], n);
     if (q) {
       float a = 0.f;
 #pragma unroll
       for (int u = 0; u < 8; ++u) a = fmaxf(a, fabsf(v[i][u]));
       if (group > 0) {
         a = fmaxf(block_max(a, group / 8), kF8Floor);
-        store_f8(q + at + col, to_f8(v[i], kF8Max / a), n);
+        store_f8<FAR>(q + at + col, to_f8(v[i], kF8Max / a), n);
         if (n > 0 && col % group == 0) scale[row * groups + col / group] = a / kF8Max;
       } else {
         amax = fmaxf(amax, a);
@@ -120,7 +123,7 @@ add_rms_norm_kernel(const T* __restrict__ x, const T* __restrict__ residual, con
 #pragma unroll
     for (int i = 0; i < CPL; ++i) {
       const int col = 8 * (i * lanes + lane);
-      store_f8(q + at + col, to_f8(v[i], inv), H - col);
+      store_f8<FAR>(q + at + col, to_f8(v[i], inv), H - col);
     }
   }
 }
@@ -129,7 +132,7 @@ add_rms_norm_kernel(const T* __restrict__ x, const T* __restrict__ residual, con
 // share of dw in registers until it writes it as one row of `partial`.  The
 // next row is on its way while the present one is worked on, as long as the
 // registers of 16 waves hold both (CPL <= 2).
-template <typename T, int CPL>
+template <typename T, int CPL, bool FAR>
 __global__ void __launch_bounds__(1024)
 add_rms_norm_backward_kernel(const T* __restrict__ dy, const T* __restrict__ dh, const T* __restrict__ h,
                              const float* __restrict__ rstd, const void* __restrict__ weight, bool w_f32,
@@ -182,7 +185,7 @@ add_rms_norm_backward_kernel(const T* __restrict__ dy, const T* __restrict__ dh,
       const int col = 8 * (i * lanes + lane), n = H - col;
       f32x8 r = s * (widen(g[i]) * load_row_either<T>(weight, w_f32, col, n) - widen(a[i]) * c);
       if (dh) r += kAhead ? widen(d[i]) : load_row(dh + row * H + col, n);
-      store_row(dx + row * H + col, r, n);
+      store_row<FAR>(dx + row * H + col, r, n);
     }
     if constexpr (kAhead) {
       s = next_s;
@@ -228,11 +231,13 @@ struct Shape {
   int waves, cpl;
 };
 // Waves, and chunks of eight columns per lane, that hold a row of H: as few
-// chunks as 16 waves allow (a row of 4096 in 16 bits, 16384 rows: 116 us with
-// one chunk in 8 waves, 120 with four in two; backward, 98 and 124 with two).
-Shape shape_of(int32_t H) {
+// chunks as 16 waves allow (16384 rows of 2048 in 32 bits: 109 us, 116 with two;
+// the gradient of 16384 x 4096, 98 and 124).  Forward, rows of 16 bits that would
+// take 8 to 15 waves take two (16384 x 4096: 104 us, 110 with one; 4096 x 8192,
+// which keeps one, 54 and 56).
+Shape shape_of(int32_t H, bool forward16) {
   const int chunks = (H + 7) / 8;
-  int cpl = 1;
+  int cpl = forward16 && chunks >= 512 && chunks < 1024 ? 2 : 1;
   while (cpl * 16 * kWave < chunks) cpl *= 2;
   return {(chunks + cpl * kWave - 1) / (cpl * kWave), cpl};
 }
@@ -241,7 +246,7 @@ Shape shape_of(int32_t H) {
 // more partial sums, fewer leave loads unissued (32768 rows of 1024: 53 us with
 // half the waves, 48 us; 4096 rows of 8192: 54 us, 62 with twice as many).
 int32_t backward_workers(int64_t rows, int32_t H) {
-  const int64_t most = 4096 / shape_of(H).waves;
+  const int64_t most = 4096 / shape_of(H, false).waves;
   return (int32_t)(rows < most ? rows : most);
 }
 
@@ -257,10 +262,13 @@ template <typename T>
 taot_status forward(const void* x, const void* residual, const void* weight, bool w_f32, int64_t rows, int32_t H,
                     float eps, int32_t group, void* h, void* y, uint8_t* q, float* scale, float* rstd,
                     hipStream_t stream) {
-  const Shape s = shape_of(H);
+  const Shape s = shape_of(H, sizeof(T) == 2);
   const int per = s.waves == 1 ? kRowsOfBlock : 1;
   const bool ok = with_chunks(s.cpl, [&](auto C) {
-    add_rms_norm_kernel<T, C.value><<<(unsigned)((rows + per - 1) / per), kWave * s.waves * per, 0, stream>>>(
+    auto* kernel = with_far(rows * H * (int64_t)sizeof(T), [](auto far) {
+      return add_rms_norm_kernel<T, decltype(C)::value, far.value>;
+    });
+    kernel<<<(unsigned)((rows + per - 1) / per), kWave * s.waves * per, 0, stream>>>(
         static_cast<const T*>(x), static_cast<const T*>(residual), weight, w_f32, rows, H, eps, group,
         static_cast<T*>(h), static_cast<T*>(y), q, scale, rstd, s.waves);
     return true;
@@ -274,13 +282,15 @@ taot_status backward(const void* dy, const void* dh, const void* h, const float*
   const int32_t workers = backward_workers(rows, H);
   bool ok = true;
   if (rows > 0) {
-    const Shape s = shape_of(H);
+    const Shape s = shape_of(H, false);
     const int per = s.waves == 1 ? kRowsOfBlock : 1;
     ok = with_chunks(s.cpl, [&](auto C) {
-      add_rms_norm_backward_kernel<T, C.value>
-          <<<(unsigned)((workers + per - 1) / per), kWave * s.waves * per, 0, stream>>>(
-              static_cast<const T*>(dy), static_cast<const T*>(dh), static_cast<const T*>(h), rstd, weight, w_f32,
-              rows, H, static_cast<T*>(dx), partial, workers, s.waves);
+      auto* kernel = with_far(rows * H * (int64_t)sizeof(T), [](auto far) {
+        return add_rms_norm_backward_kernel<T, decltype(C)::value, far.value>;
+      });
+      kernel<<<(unsigned)((workers + per - 1) / per), kWave * s.waves * per, 0, stream>>>(
+          static_cast<const T*>(dy), static_cast<const T*>(dh), static_cast<const T*>(h), rstd, weight, w_f32, rows, H,
+          static_cast<T*>(dx), partial, workers, s.waves);
       return true;
     });
   }
