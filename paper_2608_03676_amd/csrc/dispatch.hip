@@ -26,10 +26,19 @@ namespace {
 constexpr int kThreads = 256, kTableThreads = 1024;
 constexpr int kUnroll = 4;
 constexpr int32_t kChunkMin = 256, kChunkMax = 32768;
-constexpr int64_t kWavesWanted = 4096;  // 64 rows of 131072: 54 us, 58 with twice as many (more counts), 58 with half
-constexpr size_t kTableLds = 32768;  // a row's tables are kept in LDS up to this size
-constexpr size_t kKeepLds = 65536;   // and beside its waves' stretches up to this one
-constexpr int64_t kRowIds = 8192;    // rows up to this length are done by one block
+// 64 rows of 131072 ids, 256 experts: the kernels take 53 us in all; 53 with half as many waves, 58 with twice (more counts)
+constexpr int64_t kWavesWanted = 4096;
+// A row's tables are made in LDS up to this size, else in memory (1024 ranks: from 3 slots a rank).
+constexpr size_t kTableLds = 32768;
+// Waves keep their stretches in LDS beside the row's tables, as many waves a block as there is room for (8 rows of
+// 131072, 1024 experts: 42 us, 48 with copies that look theirs up), unless a block would bring many words of tables for
+// each of its ids (8 rows of 65536, 256 experts, 8192 slots, 16 words an id: 135 us, 117 without; 8 of 131072, 4096
+// experts, 512 slots, 3 words: 92 and 137).
+constexpr size_t kKeepLds = 163840;
+constexpr int64_t kBroughtWords = 8;
+// Rows up to this length are done by one block and in one launch (384 experts, 512 slots, calls from end to end: a row
+// of 8192 24 us, 30 in four launches; 256 such rows 29 and 59; from there on a block takes 5 us more for 4096 ids more).
+constexpr int64_t kRowIds = 8192;
 constexpr size_t kRowLds = 65536;
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
@@ -227,7 +236,7 @@ count_kernel(Lists l, int32_t B, int32_t R, int32_t K, const int32_t* __restrict
 // hist becomes the copies of e before the chunk; total[row][e] those of the row.
 // A block has 64 experts of a row, 16 threads each, which share the chunks and
 // hold up to kHeld counts each.
-constexpr int kBaseThreads = 1024, kHeld = 8;
+constexpr int kBaseThreads = 1024, kHeld = 16;
 __global__ void __launch_bounds__(kBaseThreads)
 bases_kernel(int32_t* __restrict__ hist, int32_t E, int32_t chunks, int32_t* __restrict__ total) {
   constexpr int kGroups = kBaseThreads / kWave;
@@ -391,6 +400,18 @@ struct Shares {
 struct Stretch {
   int32_t base, end;
 };
+// The wave's lanes that hold the same expert meet in an LDS word of the expert's:
+// lanes in it, among those that are `in`; the word is 0 before and after.
+__device__ __forceinline__ Same meet(unsigned long long* word, bool in, int lane) {
+  if (in) __hip_atomic_fetch_or(word, 1ull << lane, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+  __builtin_amdgcn_wave_barrier();  // a wave's LDS operations are done in order
+  const uint64_t all = __hip_atomic_load(word, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+  __builtin_amdgcn_wave_barrier();
+  __hip_atomic_store(word, 0ull, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+  __builtin_amdgcn_wave_barrier();
+  return Same{(uint32_t)all, (uint32_t)(all >> 32)};
+}
+
 __device__ __forceinline__ Stretch stretch(const Shares& s, int32_t e, int32_t j) {
   const int2 o = s.own[e];
   if (j >= o.x) return Stretch{o.y, INT32_MAX};
@@ -405,14 +426,18 @@ __device__ __forceinline__ Stretch stretch(const Shares& s, int32_t e, int32_t j
 }
 
 // A wave: ids src[0 .. n) of a row, n > 0, in order; mine[e]: occurrences of e
-// before them.  E <= 2^BITS.  KEEP: mine[e] holds the stretch of the next
-// occurrence too (j, base, end), which most copies fall into; else every copy
-// looks its own up.
-template <int BITS, bool KEEP>
+// before them.  kKept: mine[e] holds the stretch of the next occurrence too (j,
+// base, end), which most copies fall into, and `words` a word of each expert where
+// its lanes meet.  Else E <= 2^BITS, the lanes compare their experts bit by bit and
+// every copy looks its stretch up.
+constexpr int kKept = 0;
+constexpr int kKeptWords = 6;  // 32-bit words an expert and wave
+template <int BITS>
 __device__ __forceinline__ void place(const int32_t* __restrict__ src, int32_t n, int32_t E, int32_t* mine,
                                       const Shares& shares, int32_t placed, int32_t dropped,
-                                      int32_t* __restrict__ dst) {
+                                      int32_t* __restrict__ dst, unsigned long long* words = nullptr) {
   const int lane = threadIdx.x & (kWave - 1);
+  constexpr bool KEEP = BITS == kKept;
   int4* kept = reinterpret_cast<int4*>(mine);
   int32_t next[kUnroll];
   auto fetch = [&](int32_t i0) {  // past the end: the last id again
@@ -432,6 +457,10 @@ __device__ __forceinline__ void place(const int32_t* __restrict__ src, int32_t n
     fetch(i0 + kUnroll * kWave);
 #pragma unroll
     for (int u = 0; u < kUnroll; ++u) {  // ids that are no expert are one key more
+      if constexpr (KEEP) {
+        m[u] = meet(words + e[u], in[u], lane);
+        continue;
+      }
       const uint64_t experts = __ballot(in[u] & (e[u] < E)), others = __ballot(in[u] & (e[u] == E));
       m[u] = same_key<BITS>((uint32_t)e[u], experts);
       if (others != 0) {
@@ -478,14 +507,17 @@ __device__ __forceinline__ void bring(int32_t* to, const int32_t* __restrict__ f
   }
 }
 
-// KEEP as in place(), four words of LDS an expert and wave instead of one; the
-// row's tables are brought into LDS then, which the waves' first stretches come
-// from.  A block works on chunks of one row.
-template <bool KEEP, int BITS>
+// BITS as in place().  kKept: the row's tables are brought into LDS too, which the
+// waves' first stretches come from.  A block works on chunks of one row.
+// 64 rows of 131072 ids, 256 experts: 28 us for 67 MB, bound by its instructions;
+// 30 where the lanes compare experts bit by bit, 65 where every copy looks its
+// stretch up as well.
+template <int BITS>
 __global__ void __launch_bounds__(kThreads)
 place_kernel(const int32_t* __restrict__ ids, Tables t, const int32_t* __restrict__ hist, int64_t N, int32_t rows,
              int32_t E, int32_t S, int32_t chunk, int32_t chunks, int32_t blocks_of_row, int waves,
              int32_t* __restrict__ pos) {
+  constexpr bool KEEP = BITS == kKept;
   extern __shared__ int4 stretches[];
   const int lane = threadIdx.x & (kWave - 1), wid = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const uint32_t at_row = blockIdx.x / (uint32_t)blocks_of_row;
@@ -496,8 +528,9 @@ place_kernel(const int32_t* __restrict__ ids, Tables t, const int32_t* __restric
   Shares shares{t.shares + row * (E + S), t.slot_first + b * (E + 1), t.shares + row * (E + S) + E};
   const int32_t dropped = (int32_t)(N - t.total[row * (E + 1) + E]);  // where ids that are no expert begin
   int32_t* mine = reinterpret_cast<int32_t*>(stretches) + (KEEP ? 4 : 1) * wid * (E + 1);
+  unsigned long long* words = reinterpret_cast<unsigned long long*>(stretches + waves * (E + 1));
   if constexpr (KEEP) {
-    int32_t *own = reinterpret_cast<int32_t*>(stretches + waves * (E + 1)), *first = own + 2 * (E + S);
+    int32_t *own = reinterpret_cast<int32_t*>(words + waves * (E + 1)), *first = own + 2 * (E + S);
     int32_t j[4], f[4];
     const int32_t* base = hist + job * (E + 1);
 #pragma unroll
@@ -511,6 +544,7 @@ place_kernel(const int32_t* __restrict__ ids, Tables t, const int32_t* __restric
       if ((int)threadIdx.x + u * kThreads <= E) first[threadIdx.x + u * kThreads] = f[u];
     if (E >= 4 * kThreads) bring(first, shares.first, E + 1, threadIdx.x + 4 * kThreads, kThreads);
     shares = Shares{reinterpret_cast<const int2*>(own), first, reinterpret_cast<const int2*>(own) + E};
+    for (int32_t e = threadIdx.x; e < waves * (E + 1); e += kThreads) words[e] = 0;
     __syncthreads();
     if (!works) return;
     int4* kept = reinterpret_cast<int4*>(mine);
@@ -533,7 +567,7 @@ place_kernel(const int32_t* __restrict__ ids, Tables t, const int32_t* __restric
   __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
   __builtin_amdgcn_wave_barrier();
   const int32_t n = (int32_t)min((int64_t)chunk, N - lo);
-  place<BITS, KEEP>(ids + row * N + lo, n, E, mine, shares, t.placed[row], dropped, pos + row * N + lo);
+  place<BITS>(ids + row * N + lo, n, E, mine, shares, t.placed[row], dropped, pos + row * N + lo, words + wid * (E + 1));
 }
 
 // A short row by one block and in one launch: everything above, in LDS.
@@ -635,17 +669,17 @@ row_kernel(const int32_t* __restrict__ home, const int32_t* __restrict__ slot_ex
   if (tid == 0) bad[row] = (bad_home ? TAOT_ST_BAD_INPUT : 0u) | (total[E] > 0 ? TAOT_ST_BAD_ID : 0u);
   __syncthreads();
   if (wid < waves && n > 0)
-    place<BITS, false>(src, n, E, mine, Shares{own, first, guest}, placed, N - total[E], pos + row * N + lo);
+    place<BITS>(src, n, E, mine, Shares{own, first, guest}, placed, N - total[E], pos + row * N + lo);
 }
 
-// status[b] of the rows' bits.
-__global__ void __launch_bounds__(kThreads)
-status_kernel(const uint32_t* __restrict__ bad, int32_t B, int32_t rows, uint32_t* __restrict__ status) {
-  const int64_t b = (int64_t)blockIdx.x * kThreads + threadIdx.x;
-  if (b >= B) return;
+// status[b] of the rows' bits, a wave a problem.
+__global__ void __launch_bounds__(kWave)
+status_kernel(const uint32_t* __restrict__ bad, int32_t rows, uint32_t* __restrict__ status) {
+  const int64_t b = blockIdx.x;
   uint32_t s = 0;
-  for (int32_t r = 0; r < rows; ++r) s |= bad[b * rows + r];
-  status[b] = s;
+  for (int32_t r = threadIdx.x; r < rows; r += kWave) s |= bad[b * rows + r];
+  const uint64_t input = __ballot((s & TAOT_ST_BAD_INPUT) != 0), ids = __ballot((s & TAOT_ST_BAD_ID) != 0);
+  if (threadIdx.x == 0) status[b] = (input ? TAOT_ST_BAD_INPUT : 0u) | (ids ? TAOT_ST_BAD_ID : 0u);
 }
 
 // The token of a group of WAVES waves, among `all`, and the first row of its row of copies.
@@ -901,7 +935,7 @@ taot_status launch_dispatch_map(const int32_t* ids, int32_t B, int32_t rows, int
       kernel<<<(unsigned)n, kTableThreads, lds, stream>>>(home, slot_expert, X, ids, (int32_t)N, rows, rank0, R, E, K,
                                                           row_waves, pos, offsets, sends, bad);
       if (status && rows > 1)
-        status_kernel<<<(unsigned)((B + kThreads - 1) / kThreads), kThreads, 0, stream>>>(bad, B, rows, status);
+        status_kernel<<<(unsigned)B, kWave, 0, stream>>>(bad, rows, status);
       return hipGetLastError() == hipSuccess ? TAOT_OK : TAOT_ERR_LAUNCH;
     }
   }
@@ -916,14 +950,18 @@ taot_status launch_dispatch_map(const int32_t* ids, int32_t B, int32_t rows, int
                                                                stream>>>(p.t, slot_expert, X, rows, rank0, R, E, K,
                                                                          offsets, sends, status);
   if (chunks > 0) {
-    const size_t kept = 4 * waves * row_lds + (size_t)(E + S) * sizeof(int2) + row_lds;
-    const bool keep = kept <= kKeepLds;
-    const size_t lds = keep ? kept : waves * row_lds;
-    auto* kernel = keep ? with_bits(bits, [](auto n) { return place_kernel<true, n.value>; })
-                        : with_bits(bits, [](auto n) { return place_kernel<false, n.value>; });
+    auto kept = [&](int w) { return kKeptWords * w * row_lds + (size_t)(E + S) * sizeof(int2) + row_lds; };
+    int place_waves = 4;
+    while (place_waves > 1 && kept(place_waves) > kKeepLds) place_waves /= 2;
+    const int64_t brought = 2 * (int64_t)(E + S) + E + 1, placed = (int64_t)place_waves * chunk;
+    const bool keep = kept(place_waves) <= kKeepLds && brought <= kBroughtWords * placed;
+    if (!keep) place_waves = waves;
+    const int32_t place_blocks = (chunks + place_waves - 1) / place_waves;
+    const size_t lds = keep ? kept(place_waves) : waves * row_lds;
+    auto* kernel = keep ? place_kernel<kKept> : with_bits(bits, [](auto n) { return place_kernel<n.value>; });
     if (!allow_lds(reinterpret_cast<const void*>(kernel), lds)) return TAOT_ERR_LAUNCH;
-    kernel<<<(unsigned)(n * blocks), kThreads, lds, stream>>>(ids, p.t, p.hist, N, rows, E, S, chunk, chunks, blocks, waves,
-                                                            pos);
+    kernel<<<(unsigned)(n * place_blocks), kThreads, lds, stream>>>(ids, p.t, p.hist, N, rows, E, S, chunk, chunks,
+                                                                  place_blocks, place_waves, pos);
   }
   return hipGetLastError() == hipSuccess ? TAOT_OK : TAOT_ERR_LAUNCH;
 }

@@ -119,6 +119,15 @@ def test_shapes(gpu, B, R, rows, E, K, N):
     _check_map(gpu, *_instance(B, R, rows, E, K, N, seed=R + E), K, rank0=R - rows)
 
 
+@pytest.mark.parametrize("B,R,rows,E,K,N", [(1, 4, 4, 8, 2, 70001), (2, 64, 3, 256, 2, 20001), (1, 128, 2, 600, 2, 30000),
+                                            (1, 256, 1, 1025, 4, 66000), (1, 16, 2, 4096, 1, 40003),
+                                            (1, 1024, 1, 256, 8, 12000)])
+@pytest.mark.parametrize("bad", [0.0, 0.1])
+def test_rows_of_many_blocks(gpu, B, R, rows, E, K, N, bad):
+    print(f"[map] B = {B}, R = {R}, rows = {rows}, E = {E}, K = {K}, N = {N}, bad = {bad}", flush=True)
+    _check_map(gpu, *_instance(B, R, rows, E, K, N, seed=R + E, bad=bad, wild=bad > 0), K, rank0=R - rows)
+
+
 def test_most_experts_and_ranks(gpu):
     _check_map(gpu, *_instance(1, 2048, 1, 32768, 2, 40000, seed=3, zipf=0.3), 2, rank0=2047)
 
