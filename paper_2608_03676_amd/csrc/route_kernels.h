@@ -42,10 +42,10 @@ __device__ __forceinline__ float sigmoid(float x) { return 1.f / (1.f + expf(-x)
 
 // Weights of the chosen experts; lane j of a block of L has the j-th (id -1: none).
 // m, sum: the largest logit and the sum of exp(x - m), where the plain softmax needs them.
-template <int L, typename T>
-__device__ __forceinline__ void finish(const RouteArgs& a, int64_t t, bool mine, int j, int id, float m, float sum) {
+template <int L>
+__device__ __forceinline__ void finish_with(const RouteArgs& a, int64_t t, bool mine, int j, int id, float x, float m,
+                                            float sum) {
   const bool has = mine && id >= 0 && id < a.E;
-  const float x = has ? fminf((float)static_cast<const T*>(a.logits)[t * a.E + id], kBig) : -INFINITY;
   float w;
   if (a.flags & TAOT_ROUTE_SIGMOID) {
     w = has ? sigmoid(x) : 0.f;
@@ -63,11 +63,19 @@ __device__ __forceinline__ void finish(const RouteArgs& a, int64_t t, bool mine,
     a.weights[t * a.k + j] = w * a.scale;
   }
 }
+template <int L, typename T>
+__device__ __forceinline__ void finish(const RouteArgs& a, int64_t t, bool mine, int j, int id, float m, float sum) {
+  const bool has = mine && id >= 0 && id < a.E;
+  const float x = has ? fminf((float)static_cast<const T*>(a.logits)[t * a.E + id], kBig) : -INFINITY;
+  finish_with<L>(a, t, mine, j, id, x, m, sum);
+}
 
 // Where a token's experts lie when L lanes hold it, V a lane.  One group: runs
-// of a 16-byte load per lane, interleaved.  More: a group is `lpg` lanes, a lane
-// has `per` experts in a row.  `whole`: every such load is inside its lane's part
-// or outside it altogether; `full`: all are inside.
+// of a 16-byte load per lane, interleaved.  More: a group is `lpg` lanes; a whole
+// wave's lanes interleave such runs over their group, fewer lanes have `per`
+// experts in a row (places then differ by the same everywhere).  `whole`: every
+// such load is inside its lane's part or outside it altogether; `full`: all are
+// inside.
 struct Layout {
   int32_t lpg, per;
   bool whole, full;
@@ -76,10 +84,11 @@ struct Layout {
 template <typename T, int L, int V, bool GROUPED>
 struct Lanes {
   static constexpr int W = 16 / (int)sizeof(T), kWords = 4;
+  static constexpr bool kSpread = GROUPED && L == kWave;
   typedef T vec __attribute__((ext_vector_type(W)));
   typedef __attribute__((aligned(sizeof(T)))) vec at;
   typedef uint32_t words __attribute__((ext_vector_type(kWords)));
-  int32_t E, first, mine, sl;
+  int32_t E, first, mine, sl, step;
   int g;
   bool whole, full;
   __device__ __forceinline__ Lanes(const RouteArgs& a, const Layout& lay)
@@ -88,14 +97,19 @@ struct Lanes {
     const int32_t gs = GROUPED ? E / a.groups : E;
     g = GROUPED ? sl / lay.lpg : 0;
     const bool in = !GROUPED || g < a.groups;
-    first = GROUPED ? (in ? g * gs + (sl % lay.lpg) * lay.per : 0) : sl * W;
-    mine = GROUPED ? (in ? min(lay.per, gs - (sl % lay.lpg) * lay.per) : 0) : E;
+    step = lay.lpg * W;
+    first = GROUPED ? (in ? g * gs + (sl % lay.lpg) * (kSpread ? W : lay.per) : 0) : sl * W;
+    // experts of its run, or from its first one to its group's end
+    mine = kSpread ? (in ? gs - (sl % lay.lpg) * W : 0)
+                   : GROUPED ? (in ? min(lay.per, gs - (sl % lay.lpg) * lay.per) : 0) : E;
   }
   // Expert of place v, if the lane has it: its first one and a distance that all lanes share.
   static constexpr int away(int v) { return GROUPED ? v : (v / W) * L * W + v % W; }
-  __device__ __forceinline__ int32_t index(int v) const { return first + away(v); }
+  __device__ __forceinline__ int32_t index(int v) const { return first + (kSpread ? (v / W) * step + v % W : away(v)); }
   // Experts from place v0 on (a multiple of W) in its run: less than W at the end, 0 or less behind it.
-  __device__ __forceinline__ int32_t left(int v0) const { return GROUPED ? mine - v0 : E - index(v0); }
+  __device__ __forceinline__ int32_t left(int v0) const {
+    return kSpread ? mine - (v0 / W) * step : GROUPED ? mine - v0 : E - index(v0);
+  }
 
   // The row's logits by place, -infinity where the lane has none.
   __device__ __forceinline__ void load(const T* row, vec* d) const {
@@ -182,7 +196,8 @@ __device__ __forceinline__ void join_two(V& b1, V& b2, int32_t lpg) {
 }
 
 // Tokens by keys of 32 bits, rounded as the formulas say: a round takes the
-// maximum over the registers and removes it.
+// maximum over the registers and removes it.  Any number of choices; bound by
+// k passes over the registers (65536 x 256 bfloat16, 12 choices: 33 us, 40 MB).
 template <typename T, int L, int V, bool GROUPED>
 __device__ __forceinline__ void route_exact(const RouteArgs& a, int64_t t, const Layout& lay) {
   const Lanes<T, L, V, GROUPED> at(a, lay);
@@ -259,7 +274,8 @@ route_kernel(RouteArgs a, Layout lay) {
 }
 
 // A token by a block of 256 threads, any number of experts: the keys of
-// route_exact in LDS.
+// route_exact in LDS.  Bound by its barriers, one a round (8192 x 4096 bfloat16,
+// 8 choices: 104 us, where route_wide_kernel takes 18).
 template <typename T>
 __device__ void route_block(const RouteArgs& a, int64_t t, int* keys) {
   __shared__ int value[TAOT_MAX_ROUTE_GROUPS];
@@ -385,6 +401,9 @@ route_block_kernel(RouteArgs a) {
 // A token whose first k + 1 words or whose groups are undecided, one with a lane
 // that ran out of words, and one with keys that the fixed point does not hold
 // (0: masked, or too low) is done again by exact keys, with the whole wave.
+// Bound by the eight medians of every expert: 65536 x 256 float32, bias, 8 groups:
+// 29 us (71 MB, 2.5 TB/s; the vector units issue 62 % of the time); 65536 x 256
+// bfloat16: 12.6 us.
 constexpr int kExact16 = 0, kLogit = 1, kSigmoid = 2;
 constexpr float kLogitRange = 32.f;
 
@@ -398,21 +417,18 @@ __device__ __forceinline__ float exp_fast(float x) { return __builtin_amdgcn_exp
 
 constexpr int log2_of(int n) { return n <= 1 ? 0 : 1 + log2_of(n / 2); }
 
-template <typename T, int L, int V, int DEPTH, int MODE, bool GROUPED>
+template <typename T, int L, int V, int MODE, bool GROUPED>
 __global__ void __launch_bounds__(256, sizeof(T) == 4 || MODE == kSigmoid ? 4 : 5)
 route_few_kernel(RouteArgs a, Layout lay) {
   using Place = Lanes<T, L, V, GROUPED>;
-  static_assert(V >= DEPTH, "every place of the list holds a word");
+  constexpr int DEPTH = 8;
+  static_assert(L < kWave && V >= DEPTH, "a lane's list holds every choice");
   constexpr int W = Place::W;
   constexpr int kInf16 = std::is_same<T, __bf16>::value ? 0x7F80 : 0x7C00;
-  constexpr bool kWide = L == 64 && V > 16;
-  // Words of a wide row's keys in fixed point hold the place alone, which leaves more bits to the key: two lanes'
-  // words may then be equal, and are undecided.
-  constexpr bool kByLane = kWide && MODE != kExact16;
-  constexpr int kShift = MODE == kExact16 ? 16 : log2_of(kByLane ? V : L * V), kLow = (1 << kShift) - 1;
+  constexpr int kShift = MODE == kExact16 ? 16 : log2_of(L * V), kLow = (1 << kShift) - 1;
   constexpr float kMost = (float)((1 << (31 - kShift < 24 ? 31 - kShift : 24)) - 1);  // largest key in fixed point
   constexpr int kRanOut = INT32_MIN + 1;  // behind a lane's last word
-  auto low = [](int v) { return (uint32_t)(kLow - (kByLane ? v : Place::away(v))); };
+  auto low = [](int v) { return (uint32_t)(kLow - Place::away(v)); };
   const int lane = threadIdx.x & (kWave - 1), sl = lane % L, base = lane - sl;
   const int64_t t = ((int64_t)blockIdx.x * 256 + threadIdx.x) / L;
   const bool live = t < a.T;
@@ -475,50 +491,37 @@ route_few_kernel(RouteArgs a, Layout lay) {
   } else {
     // fixed point over the range of the keys, by the largest bias of all experts (infinite or NaN: exact keys)
     float most = 0.f, least = INFINITY;
-    constexpr int kPart = kWide ? 16 : V;  // biases held at a time
-    float bias[kPart];
-    auto fetch = [&](int v0) {
-      if (at.whole) {
-        typedef float four __attribute__((ext_vector_type(4)));
-        typedef __attribute__((aligned(4))) four at4;
+    float bias[V];
+    if (at.whole) {
+      typedef float four __attribute__((ext_vector_type(4)));
+      typedef __attribute__((aligned(4))) four at4;
 #pragma unroll
-        for (int v = 0; v < kPart; v += 4) {
-          const four b = *reinterpret_cast<const at4*>(a.bias + max(0, min(at.index(v0 + v), a.E - 4)));
+      for (int v = 0; v < V; v += 4) {
+        const four b = *reinterpret_cast<const at4*>(a.bias + max(0, min(at.index(v), a.E - 4)));
 #pragma unroll
-          for (int u = 0; u < 4; ++u) bias[v + u] = b[u];
-        }
-      } else {
-#pragma unroll
-        for (int v = 0; v < kPart; ++v) bias[v] = a.bias[min(at.index(v0 + v), a.E - 1)];
+        for (int u = 0; u < 4; ++u) bias[v + u] = b[u];
       }
-    };
-    if constexpr (kWide) {
-      for (int e = lane; e < a.E; e += kWave) most = fmaxf(most, fabsf(a.bias[e]));
     } else {
-      fetch(0);
 #pragma unroll
-      for (int v = 0; v < V; ++v) most = fmaxf(most, fabsf(bias[v]));
+      for (int v = 0; v < V; ++v) bias[v] = a.bias[min(at.index(v), a.E - 1)];
     }
+#pragma unroll
+    for (int v = 0; v < V; ++v) most = fmaxf(most, fabsf(bias[v]));
     most = block_reduce<L>(most, MaxOp());
     const float unit = (kMost - 16.f) / (1.f + 2.f * most), zero = most * unit + 4.f;
 #pragma unroll
     for (int v = 0; v < V; ++v) least = fminf(least, logit(v));
-    auto fill = [&](int v0, auto masked) {
+    auto fill = [&](auto masked) {
 #pragma unroll
-      for (int v = 0; v < kPart; ++v) {
-        const float x = logit(v0 + v), b = fmaf(bias[v], unit, zero);
+      for (int v = 0; v < V; ++v) {
+        const float x = logit(v), b = fmaf(bias[v], unit, zero);
         const uint32_t k = (uint32_t)fmaf(__builtin_amdgcn_rcpf(1.f + exp_fast(-x)), unit, b);  // NaN: 0
         const uint32_t q = !masked.value || x > -INFINITY ? k : 0u;
-        insert((int)((q << kShift) | low(v0 + v)));
+        insert((int)((q << kShift) | low(v)));
       }
     };
-    const bool masked = __ballot(least == -INFINITY) != 0;
-#pragma unroll
-    for (int v0 = 0; v0 < V; v0 += kPart) {
-      if (kWide) fetch(v0);
-      if (masked) fill(v0, std::true_type());
-      else fill(v0, std::false_type());
-    }
+    if (__ballot(least == -INFINITY) != 0) fill(std::true_type());
+    else fill(std::false_type());
     // The sigmoid's product, exponential, sum and reciprocal stay within 8 units of 2^-24, the exact key within 4
     // of the formula's value and 1 + |bias| of it for the sum; the fixed point adds less than 4 of its units.
     const float slack = 14.f * 0x1p-24f * (1.f + most) * unit;
@@ -526,10 +529,8 @@ route_few_kernel(RouteArgs a, Layout lay) {
     apart = 8 + (int)(2.f * fminf(slack, 1e6f));
     apart_two = 2 * apart;
   }
-  if constexpr (!kByLane) {
 #pragma unroll
-    for (int i = 0; i < DEPTH; ++i) best[i] -= at.first;  // the place's complement becomes the expert's
-  }
+  for (int i = 0; i < DEPTH; ++i) best[i] -= at.first;  // the place's complement becomes the expert's
 
   if constexpr (GROUPED) {
     int b1 = best[0] >> kShift, b2 = best[1] >> kShift, value;
@@ -555,27 +556,19 @@ route_few_kernel(RouteArgs a, Layout lay) {
     for (int i = 0; i < DEPTH; ++i) best[i] = stays ? best[i] : INT32_MIN;
   }
 
-  int mine = 0, top = 0, id = 0;
+  int mine = 0, top = 0;
   const int rounds = MODE == kExact16 ? a.k : a.k + 1;
   for (int j = 0; j < rounds; ++j) {
     open |= best[0] == kRanOut;
     top = block_reduce<L>(best[0], MaxOp());
     const bool won = best[0] == top && top > kRanOut;
-    if constexpr (kByLane) {
-      const uint64_t who = __ballot(won);
-      const int place = kLow - (best[0] & kLow);
-      const int e = lane_value(at.first + (GROUPED ? place : (place / W) * L * W + place % W),
-                               who != 0 ? __ffsll((unsigned long long)who) - 1 : 0);
-      open |= __popcll(who) > 1;
-      id = sl == j ? e : id;
-    }
 #pragma unroll
     for (int i = 0; i + 1 < DEPTH; ++i) best[i] = won ? best[i + 1] : best[i];
     best[DEPTH - 1] = won ? kRanOut : best[DEPTH - 1];
     mine = sl == j ? top : mine;
   }
   const bool chooses = live && sl < a.k;
-  if constexpr (!kByLane) id = kLow - (mine & kLow);
+  int id = kLow - (mine & kLow);
   if constexpr (MODE == kExact16) {
     id = mine >> kShift > -kInf16 ? id : -1;
   } else {
@@ -585,31 +578,227 @@ route_few_kernel(RouteArgs a, Layout lay) {
   }
   uint64_t again = __ballot(open && live);
   // a token is done again if one of its lanes says so
-  const uint64_t seg = (L == 64 ? ~0ull : (1ull << (L & 63)) - 1) << base;
+  const uint64_t seg = ((1ull << L) - 1) << base;
   const bool redo = (again & seg) != 0;
   finish<L, T>(a, t, chooses && !redo, sl, id, m, sum);
-  if constexpr (kWide) {  // by the whole block, one wave's token after the other
-    extern __shared__ int keys[];
-    __shared__ int32_t undecided[4];
-    if (lane == 0) undecided[threadIdx.x / kWave] = redo;
-    __syncthreads();
-    for (int w = 0; w < 4; ++w)
-      if (undecided[w]) route_block<T>(a, (int64_t)blockIdx.x * 4 + w, keys);
-  } else {
-    constexpr int kV = L == 64 ? V : 8;  // the same experts over 64 lanes
-    Layout wide = lay;
-    if constexpr (GROUPED && L < 64) {
-      wide.lpg = lay.lpg * (64 / L);
-      wide.per = (a.E / a.groups + wide.lpg - 1) / wide.lpg;
+  Layout wide = lay;  // the same experts over 64 lanes
+  if constexpr (GROUPED) {
+    wide.lpg = lay.lpg * (kWave / L);
+    wide.whole = false;
+  }
+  wide.full = false;
+  while (again != 0) {
+    const int s = __ffsll((unsigned long long)again) - 1;
+    again &= ~(((1ull << L) - 1) << (s / L * L));
+    route_exact<T, kWave, 8, GROUPED>(a, ((int64_t)blockIdx.x * 256 + (threadIdx.x & ~(kWave - 1)) + s) / L, wide);
+  }
+}
+
+// ---- wide rows, up to sixteen choices ------------------------------------------------
+// A wave per token, 64 lanes with V experts each.  The k-th largest of the lanes'
+// own maxima is a bound that the k best reach: few others do.  Those that reach it go to LDS, one a lane,
+// where exact keys are compared with one another: one comparison an expert, where
+// lists would take a median for each of their places.  Without a bias the logits
+// themselves are the keys; with one, keys from the hardware's exponential and
+// reciprocal set the bound, lowered by twice their error.  A token with groups
+// nearer than that error, with infinite or NaN values, or with more than 64
+// experts that reach the bound is done again by the block.
+// 8192 x 4096 bfloat16, plain softmax: 18 us (68 MB, 3.8 TB/s; 22 with a lane's
+// four largest in a list), bound by the softmax's sum (15 us without it); float32:
+// 25 us (134 MB, 5.4 TB/s); sigmoid and bias, bfloat16: 35 us, bound by the sigmoid.
+constexpr int kWideMost = 16;
+
+template <typename T, int V, bool BIAS, bool GROUPED>
+__global__ void __launch_bounds__(256, sizeof(T) == 4 && BIAS ? 2 : sizeof(T) == 4 || BIAS ? 3 : 6)
+route_wide_kernel(RouteArgs a, Layout lay) {
+  using Place = Lanes<T, kWave, V, GROUPED>;
+  constexpr int W = Place::W;
+  extern __shared__ int keys[];
+  __shared__ int2 found[4][kWave + 1];  // an expert and its logit; behind the 64th all in one place
+  __shared__ int32_t undecided[4];
+  __shared__ float part[4];
+  const int lane = threadIdx.x & (kWave - 1), wid = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const int64_t t = (int64_t)blockIdx.x * 4 + wid;
+  const bool live = t < a.T;
+  const T* row = static_cast<const T*>(a.logits) + (live ? t : a.T - 1) * a.E;
+  const Place at(a, lay);
+  typename Place::vec d[V / W];
+  at.load(row, d);
+  auto logit = [&](int v) { return (float)d[v / W][v % W]; };
+  // From here on the logits are widened anew: V of them would take more registers than leave room for enough waves.
+  auto narrow = [&] {
+    if constexpr (sizeof(T) == 2) {
+#pragma unroll
+      for (int v = 0; v < V; v += W) {
+        typename Place::words r = __builtin_bit_cast(typename Place::words, d[v / W]);
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          uint32_t w = r[u];
+          asm("" : "+v"(w));
+          r[u] = w;
+        }
+        d[v / W] = __builtin_bit_cast(typename Place::vec, r);
+      }
     }
-    if (L < 64) wide.full = false;
-    if (GROUPED && L < 64) wide.whole = false;
-    while (again != 0) {
-      const int s = __ffsll((unsigned long long)again) - 1;
-      again &= ~((L == 64 ? ~0ull : (1ull << (L & 63)) - 1) << (s / L * L));
-      route_exact<T, 64, kV, GROUPED>(a, ((int64_t)blockIdx.x * 256 + (threadIdx.x & ~(kWave - 1)) + s) / L, wide);
+  };
+  bool open = false;
+
+  // the lane's largest key, and the second where groups need it
+  float b1 = -INFINITY, b2 = -INFINITY, m = 0.f, sum = 1.f, slack = 0.f;
+  float key[BIAS ? V : 1];
+  if constexpr (!BIAS) {
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      if (GROUPED) b2 = __builtin_amdgcn_fmed3f(b1, b2, logit(v));
+      b1 = fmaxf(b1, logit(v));
+      // keeps the compiler from widening all V first, which spills
+      if (GROUPED && v % W == W - 1) asm volatile("" : "+v"(b1), "+v"(b2));
+    }
+    m = block_reduce<kWave>(b1, MaxOp());
+    open |= m == INFINITY;
+    m = m > -INFINITY ? m : 0.f;
+    narrow();
+    if (!(a.flags & (TAOT_ROUTE_SIGMOID | TAOT_ROUTE_RENORM))) {
+      sum = 0.f;
+#pragma unroll
+      for (int v = 0; v < V; ++v) sum += exp_fast(logit(v) - m);
+      sum = block_reduce<kWave>(sum, SumOp());
+      open |= sum != sum;
+    } else if (GROUPED) {  // NaN: the second largest is not to be relied on
+      float all = 0.f;
+#pragma unroll
+      for (int v = 0; v < V; ++v) all += logit(v);
+      open |= all != all;
+    }
+  } else {
+    float most = 0.f, least = INFINITY;
+    float* bias = reinterpret_cast<float*>(keys);  // the biases in LDS: by the block once, not by each wave
+    for (int e = threadIdx.x; e < a.E; e += 256) {
+      bias[e] = a.bias[e];
+      most = fmaxf(most, fabsf(bias[e]));
+    }
+    most = block_reduce<kWave>(most, MaxOp());
+    if (lane == 0) part[wid] = most;
+    __syncthreads();
+    most = fmaxf(fmaxf(part[0], part[1]), fmaxf(part[2], part[3]));
+    open |= !(most < 1e30f);
+    // The sigmoid's product, exponential, sum and reciprocal stay within 8 units of 2^-24, the exact key within 4
+    // of the formula's value, and each sum's rounding within 1 + |bias| of them.
+    slack = 16.f * 0x1p-24f * (1.f + most);
+#pragma unroll
+    for (int v = 0; v < V; ++v) least = fminf(least, logit(v));
+    narrow();
+    typedef float four __attribute__((ext_vector_type(4)));
+    auto fill = [&](auto masked, auto whole) {
+#pragma unroll
+      for (int v0 = 0; v0 < V; v0 += 4) {
+        four b;
+        if constexpr (whole.value) {
+          b = *reinterpret_cast<const four*>(bias + max(0, min(at.index(v0), a.E - 4)));
+        } else {
+#pragma unroll
+          for (int u = 0; u < 4; ++u) b[u] = bias[min(at.index(v0 + u), a.E - 1)];
+        }
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          const float x = logit(v0 + u), y = __builtin_amdgcn_rcpf(1.f + exp_fast(-x)) + b[u];
+          key[v0 + u] = !masked.value || x > -INFINITY ? y : -INFINITY;
+        }
+        if (v0 % 8 == 4) asm volatile("" : "+v"(key[v0]), "+v"(key[v0 + 1]), "+v"(key[v0 + 2]), "+v"(key[v0 + 3]));
+      }
+    };
+    const bool masked = __ballot(least == -INFINITY) != 0;
+    if (!at.whole) fill(std::true_type(), std::false_type());
+    else if (masked) fill(std::true_type(), std::true_type());
+    else fill(std::false_type(), std::true_type());
+    float all = 0.f;
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      if (GROUPED) {
+        b2 = __builtin_amdgcn_fmed3f(b1, b2, key[v]);
+        all += key[v];
+      }
+      b1 = fmaxf(b1, key[v]);
+    }
+    open |= all != all;
+  }
+  auto value_of = [&](int v) {
+    if constexpr (BIAS) return key[v];
+    else return logit(v);
+  };
+
+  bool stays = true;
+  if constexpr (GROUPED) {
+    float g1 = b1, g2 = b2;
+    join_two(g1, g2, lay.lpg);
+    const bool two = (a.flags & TAOT_ROUTE_GROUP_TWO) && g2 > -INFINITY, in = at.g < a.groups;
+    const float value = two ? g1 + g2 : g1;
+    stays = in && group_rank(a, key_of(value), at.g, 0, lay.lpg) < a.top_groups;
+    if constexpr (BIAS) {
+      const float last = -block_reduce<kWave>(stays ? -value : -INFINITY, MaxOp());
+      const float next = block_reduce<kWave>(!stays && in ? value : -INFINITY, MaxOp());
+      open |= next > -INFINITY && !(last - next > 4.f * slack);
     }
   }
+
+  // the largest number that k lanes' maxima reach, of a float's upper bits in order: all of bfloat16's; else 26, so
+  // that keys close to one another (sigmoids near 1, logits far from 0) do not all reach it
+  constexpr int kLastBit = std::is_same<T, __bf16>::value && !BIAS ? 16 : 6;
+  const uint32_t mine = (uint32_t)key_of(stays ? b1 : -INFINITY) ^ 0x80000000u;
+  uint32_t bound = 0;
+#pragma unroll
+  for (int bit = 31; bit >= kLastBit; --bit) {
+    const uint32_t trial = bound | 1u << bit;
+    bound = __popcll(__ballot(mine >= trial)) >= a.k ? trial : bound;
+  }
+  const float reach = unordered(max((int)(bound ^ 0x80000000u), ordered(-kBig))) - 2.f * slack;
+  const float limit = stays ? reach : INFINITY;
+
+  if constexpr (!BIAS) narrow();
+  int n = 0;
+#pragma unroll
+  for (int v = 0; v < V; ++v) {
+    const float x = value_of(v);
+    const bool in = x >= limit;
+    const uint64_t who = __ballot(in);
+    if (who == 0) continue;
+    const int below = __builtin_amdgcn_mbcnt_hi((uint32_t)(who >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)who, 0));
+    if (in) found[wid][min(n + below, kWave)] = int2{at.index(v), __float_as_int(x)};
+    n += __popcll(who);
+  }
+  open |= n > kWave;
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+
+  const int count = min(n, kWave);
+  int2 f = found[wid][lane];
+  bool has = lane < count;
+  const int e = has ? f.x : 0;
+  float x = __int_as_float(f.y);
+  if constexpr (BIAS) x = (float)row[e];
+  x = fminf(x, kBig);
+  int exact = key_of(x);
+  if constexpr (BIAS) exact = key_of(sigmoid(x) + a.bias[e]);
+  exact = has ? exact : kNone;
+  has = exact != kNone;
+  int rank = 0;
+  for (int c = 0; c < count; ++c) {
+    const int other = lane_value(exact, c), oe = lane_value(e, c);
+    rank += other > exact || (other == exact && oe < e) ? 1 : 0;
+  }
+  __builtin_amdgcn_wave_barrier();
+  if (has && rank < a.k) found[wid][rank] = int2{e, __float_as_int(x)};
+  const int chosen = min((int)__popcll(__ballot(has)), a.k);
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  f = found[wid][lane];
+  const bool redo = __ballot(open && live) != 0;
+  finish_with<kWave>(a, t, live && lane < a.k && !redo, lane, lane < chosen ? f.x : -1,
+                     lane < chosen ? __int_as_float(f.y) : -INFINITY, m, sum);
+  if (lane == 0) undecided[wid] = redo;
+  __syncthreads();
+  for (int w = 0; w < 4; ++w)
+    if (undecided[w]) route_block<T>(a, (int64_t)blockIdx.x * 4 + w, keys);
 }
 
 // ---- gradient ------------------------------------------------------------------
@@ -770,20 +959,24 @@ route_backward_kernel(const float* __restrict__ dweights, const T* __restrict__ 
 
 template <typename T, int L, int V, bool GROUPED>
 taot_status go(const RouteArgs& a, Layout lay, hipStream_t stream) {
-  constexpr int kDepth = L == 64 ? 4 : 8, kPlain = std::is_same<T, float>::value ? kLogit : kExact16;
+  constexpr int kPlain = std::is_same<T, float>::value ? kLogit : kExact16;
   constexpr int W = 16 / (int)sizeof(T);
-  constexpr bool kWide = L == 64 && V > 16;
   const unsigned blocks = (unsigned)((a.T * L + 255) / 256);
-  const size_t lds = kWide ? (size_t)a.E * sizeof(int) : 0;
+  const size_t lds = (size_t)a.E * sizeof(int);
   const int32_t gs = a.E / a.groups;
   if (GROUPED && round_up(lay.per, W) <= V) lay.per = (int32_t)round_up(lay.per, W);
-  lay.whole = GROUPED ? gs % W == 0 && lay.per % W == 0 : a.E % W == 0;
-  lay.full = GROUPED ? a.groups * lay.lpg == L && lay.per == V && gs == lay.lpg * V : a.E == L * V;
-  if (a.k <= 8 && !a.bias) route_few_kernel<T, L, V, kDepth, kPlain, GROUPED><<<blocks, 256, lds, stream>>>(a, lay);
-  else if (a.k <= 8 && (a.flags & TAOT_ROUTE_SIGMOID))
-    route_few_kernel<T, L, V, kDepth, kSigmoid, GROUPED><<<blocks, 256, lds, stream>>>(a, lay);
-  else if constexpr (!kWide)
-    route_kernel<T, L, V, GROUPED><<<blocks, 256, 0, stream>>>(a, lay);
+  lay.whole = !GROUPED ? a.E % W == 0 : gs % W == 0 && (L == kWave || lay.per % W == 0);
+  lay.full = GROUPED ? a.groups * lay.lpg == L && (L == kWave || lay.per == V) && gs == lay.lpg * V : a.E == L * V;
+  const bool sigm = a.flags & TAOT_ROUTE_SIGMOID;
+  if constexpr (L == kWave) {
+    if (a.k <= kWideMost && !a.bias) route_wide_kernel<T, V, false, GROUPED><<<blocks, 256, lds, stream>>>(a, lay);
+    else if (a.k <= kWideMost && sigm) route_wide_kernel<T, V, true, GROUPED><<<blocks, 256, lds, stream>>>(a, lay);
+    else if constexpr (V <= 16) route_kernel<T, L, V, GROUPED><<<blocks, 256, 0, stream>>>(a, lay);
+  } else {
+    if (a.k <= 8 && !a.bias) route_few_kernel<T, L, V, kPlain, GROUPED><<<blocks, 256, 0, stream>>>(a, lay);
+    else if (a.k <= 8 && sigm) route_few_kernel<T, L, V, kSigmoid, GROUPED><<<blocks, 256, 0, stream>>>(a, lay);
+    else route_kernel<T, L, V, GROUPED><<<blocks, 256, 0, stream>>>(a, lay);
+  }
   return hipGetLastError() == hipSuccess ? TAOT_OK : TAOT_ERR_LAUNCH;
 }
 
@@ -801,14 +994,17 @@ taot_status route_of(const RouteArgs& a, hipStream_t stream) {
     lay.per = (a.E / a.groups + lay.lpg - 1) / lay.lpg;
     return lay;
   };
+  // As few lanes a token as hold it: a round's reduction serves more tokens (65536 tokens, bfloat16, 8 choices; us by
+  // 8, 16 and 64 lanes: 128 experts 9, 14 and 48; 256 experts 13, 14 and 46; 384 experts by 16 and 64: 21 and 46;
+  // 16384 tokens of 1000 experts by 64 lanes and by a block: 15 and 78).
   const Layout by8 = layout(8), by16 = layout(16), by64 = layout(kWave);
-  const bool few = a.k <= 8 && (!a.bias || (a.flags & TAOT_ROUTE_SIGMOID));
+  const bool known = !a.bias || (a.flags & TAOT_ROUTE_SIGMOID), few = a.k <= 8 && known;
   if (few && a.groups <= 8 && by8.per <= 16) return go<T, 8, 16>(a, by8, stream);
   if (few && a.groups <= 8 && by8.per <= 32) return go<T, 8, 32>(a, by8, stream);
   if (a.k <= 16 && a.groups <= 16 && by16.per <= 16) return go<T, 16, 16>(a, by16, stream);
   if (a.k <= 16 && a.groups <= 16 && by16.per <= 32) return go<T, 16, 32>(a, by16, stream);
   if (a.groups <= kWave && by64.per <= 16) return go<T, 64, 16>(a, by64, stream);
-  if (few && a.groups <= kWave && by64.per <= 64) return go<T, 64, 64>(a, by64, stream);
+  if (a.k <= kWideMost && known && a.groups <= kWave && by64.per <= 64) return go<T, 64, 64>(a, by64, stream);
   const size_t lds = (size_t)a.E * sizeof(int);
   auto* kernel = route_block_kernel<T>;
   if (!allow_lds(reinterpret_cast<const void*>(kernel), lds)) return TAOT_ERR_LAUNCH;

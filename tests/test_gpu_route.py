@@ -136,6 +136,24 @@ def test_groups_by_two(gpu, E, groups, k):
     _check(gpu, x, k, groups=groups, top_groups=groups // 2, flags=REN | TWO, tol=3e-6)
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("E,k", [(520, 9), (1000, 16), (1024, 12), (1700, 16), (4096, 16), (4090, 11)])
+@pytest.mark.parametrize("step", [1 / 64, 1.0])
+def test_wide_rows(gpu, dtype, E, k, step):
+    """More choices, and (step 1) many experts that are as good as the last one chosen."""
+    print(f"[route wide] {dtype} E = {E}, k = {k}, step = {step}", flush=True)
+    x = _logits(11, E, dtype, seed=E + k, step=step)
+    x[3] += 100                      # far from 0: sigmoids are 1
+    x[4, :] = -np.inf
+    x[4, 7:7 + k // 2] = 1.0         # fewer than are chosen
+    x[5, E // 2:] = float("nan")
+    x[6, 1::3] = float("inf")
+    for a in (dict(), dict(groups=2, top_groups=1)):
+        _check(gpu, x, k, flags=0, **a)
+        _check(gpu, x, k, flags=REN, tol=3e-6, **a)
+        _check(gpu, x, k, bias=_bias(E, k), flags=SIG | REN, tol=3e-6, **a)
+
+
 def test_ties_go_to_the_lower_expert(gpu):
     for E in (64, 300, 2000, 5000):
         r = taot.route(torch.zeros(3, E, device=gpu), 8)
