@@ -58,6 +58,10 @@ __device__ __forceinline__ void store_row(T* p, f32x8 v, int n) {
 // 111 through the caches; 2048 x 4096: 13.6 and 13.6).
 constexpr int64_t kFarBytes = 32 << 20;
 
+// Blocks of a launch: their threads, up to 1024 each, are counted in 32 bits.
+// Larger work is done by several launches.
+constexpr int64_t kMaxBlocks = 1 << 21;
+
 // f by whether `bytes` of output go past the caches.
 template <typename F>
 auto with_far(int64_t bytes, F f) {
