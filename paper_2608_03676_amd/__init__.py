@@ -353,13 +353,15 @@ class Norm:
     scale: Optional[torch.Tensor] = None  # [..., ceil(H / group)] float32 ([..., 1] for group = 0)
     rstd: Optional[torch.Tensor] = None   # [...] float32
     h: Optional[torch.Tensor] = None      # [..., H], x's type: x + residual (x itself without a residual)
+    h_is_x: bool = False                  # h is the x of a call without a residual: no memory to write a sum to
 
 
 def add_rms_norm(x: torch.Tensor, weight: torch.Tensor, eps: float, residual: Optional[torch.Tensor] = None,
                  group: Optional[int] = None, out: Optional[Norm] = None, stream=None) -> Norm:
     """h = x + residual, y = h * rsqrt(mean(h^2) + eps) * weight over the last dimension (taot_add_rms_norm).
     weight: [H] of x's type or float32.  group: also y in 8 bits with a scale for each `group` columns (a power
-    of two from 8 to 512), 0: one scale a row; None: no 8-bit output."""
+    of two from 8 to 512), 0: one scale a row; None: no 8-bit output.  out: tensors to write to, or an earlier
+    call's result to use again."""
     _rows(x, "x")
     H = x.shape[-1] if x.dim() else 0
     _shape(_rows(weight, "weight", None if weight.dtype == torch.float32 else x), "weight", (H,))
@@ -370,7 +372,8 @@ def add_rms_norm(x: torch.Tensor, weight: torch.Tensor, eps: float, residual: Op
         out = Norm()
     out.y = _like(out.y, "out.y", x, stream)
     out.rstd = _into(out.rstd, "out.rstd", lead, torch.float32, dev, stream)
-    out.h = x if residual is None else _like(out.h, "out.h", x, stream)
+    out.h = x if residual is None else _like(None if out.h_is_x else out.h, "out.h", x, stream)
+    out.h_is_x = residual is None
     q = s = None
     if group is not None:
         q = out.q = _into(out.q, "out.q", x.shape, torch.float8_e4m3fn, dev, stream)

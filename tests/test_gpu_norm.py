@@ -237,3 +237,16 @@ def test_refusals(gpu):
     with pytest.raises(taot.TaotError) as e:
         taot.add_rms_norm(wide, wide[0], 1e-6)
     assert e.value.code == 2
+
+def test_a_result_used_again_leaves_an_earlier_input_alone(gpu):
+    """A call without a residual gives its x as h; the next one, with a residual, writes its sum elsewhere."""
+    x, r, w = _inputs(gpu, 5, 96, torch.bfloat16)
+    before = x.clone()
+    n = taot.add_rms_norm(x, w, 1e-6)
+    n = taot.add_rms_norm(r, w, 1e-6, residual=x, out=n)
+    assert torch.equal(x, before)
+    _check_forward(n, r, x, w, 1e-6, None)
+    h, y = n.h, n.y
+    n = taot.add_rms_norm(x, w, 1e-6, residual=r, out=n)
+    assert n.h is h and n.y is y
+    _check_forward(n, x, r, w, 1e-6, None)
