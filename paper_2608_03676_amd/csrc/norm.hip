@@ -135,7 +135,7 @@ add_rms_norm_kernel(const T* __restrict__ x, const T* __restrict__ residual, con
 // share of dw in registers until it writes it as one row of `partial`.  The
 // next row is on its way while the present one is worked on, as long as the
 // registers of 16 waves hold both (CPL <= 2).  8192 x 5120 bfloat16 with a
-// residual's gradient: 74 us for 335 MB, 4.5 TB/s.
+// residual's gradient: 66 us for 335 MB, 5.1 TB/s.
 template <typename T, int CPL, bool FAR>
 __global__ void __launch_bounds__(1024)
 add_rms_norm_backward_kernel(const T* __restrict__ dy, const T* __restrict__ dh, const T* __restrict__ h,
@@ -246,11 +246,19 @@ Shape shape_of(int32_t H, bool forward16) {
   return {(chunks + cpl * kWave - 1) / (cpl * kWave), cpl};
 }
 
-// Workers of the gradient: 16 waves a compute unit.  More would write and read
-// more partial sums, fewer leave loads unissued (32768 rows of 1024: 53 us with
-// half the waves, 48 us; 4096 rows of 8192: 54 us, 62 with twice as many).
+// Workers of the gradient: as many on each of the 256 compute units, for a unit
+// with one more than others is waited for by all.  16 waves a unit and up to what
+// fills the last block, where the registers hold those (24 waves with one chunk a
+// lane, 16 with more), else one block less.  In 16 bits, us with 4096 waves shared
+// out as they come and so: 8192 rows of 5120 79 and 71, 8192 of 6144 97 and 79,
+// 10000 of 3584 68 and 60; 4096 of 7168 84, 60 with the last block and 57 without.
+// Of many more the partial sums cost more than they bring (60000 rows of 512: 57
+// us, 62 with 24 waves a unit).
 int32_t backward_workers(int64_t rows, int32_t H) {
-  const int64_t most = 4096 / shape_of(H, false).waves;
+  const Shape s = shape_of(H, false);
+  int blocks = (16 + s.waves - 1) / s.waves;
+  if (blocks * s.waves > (s.cpl == 1 ? 24 : 16)) --blocks;
+  const int64_t most = 256 * blocks;
   return (int32_t)(rows < most ? rows : most);
 }
 
