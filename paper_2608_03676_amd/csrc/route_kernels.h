@@ -541,7 +541,7 @@ route_few_kernel(RouteArgs a, Layout lay) {
         return o > -kInf16 ? fminf((float)__builtin_bit_cast(T, (short)(o < 0 ? 0x8000 | -o : o)), kBig) : -INFINITY;
       };
       const float x = float_of(b1), y = float_of(b2);
-      value = key_of(two && y > -INFINITY ? x + y : x);
+      value = x > -INFINITY ? ordered(two && y > -INFINITY ? x + y : x) : kNone;  // a sum of lowest values is a value
     } else {
       value = b1 + (two ? b2 : 0);
       open |= in && (b1 <= 0 || (two && b2 <= 0));
@@ -733,7 +733,7 @@ route_wide_kernel(RouteArgs a, Layout lay) {
     join_two(g1, g2, lay.lpg);
     const bool two = (a.flags & TAOT_ROUTE_GROUP_TWO) && g2 > -INFINITY, in = at.g < a.groups;
     const float value = two ? g1 + g2 : g1;
-    stays = in && group_rank(a, key_of(value), at.g, 0, lay.lpg) < a.top_groups;
+    stays = in && group_rank(a, g1 > -INFINITY ? ordered(value) : kNone, at.g, 0, lay.lpg) < a.top_groups;
     if constexpr (BIAS) {
       const float last = -block_reduce<kWave>(stays ? -value : -INFINITY, MaxOp());
       const float next = block_reduce<kWave>(!stays && in ? value : -INFINITY, MaxOp());
