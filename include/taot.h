@@ -306,12 +306,16 @@ taot_status taot_add_rms_norm_backward(const void* dy, const void* dh, const voi
 #define TAOT_ROUTE_SIGMOID 0x1u   /* scores are sigmoid(x), not softmax(x)         */
 #define TAOT_ROUTE_RENORM 0x2u    /* weights of a token sum to `scale`             */
 #define TAOT_ROUTE_GROUP_TWO 0x4u /* a group counts as the sum of its two largest
-                                     keys, not as its largest                    */
+                                     scores (with their biases), not as its
+                                     largest key                                 */
 /* Routing of tokens to experts.  Score s_e = softmax_e(x) or sigmoid(x_e); key_e =
  * s_e + bias_e, or x_e where there is no bias (the same order, without the
  * score's rounding).  Experts fall into `groups` equal runs; those of the best
  * `top_groups` stay, and the k largest keys among them are chosen, in
- * descending order.  Equal keys or groups: the lower index first.
+ * descending order.  A group counts as its largest key; with GROUP_TWO as the
+ * sum of its two largest s_e + bias_e (s_e without a bias; of the softmax before
+ * the division by its sum), in 32 bits, or as the one that it has.  Equal keys or
+ * groups: the lower index first.
  * Weights: scale * s_e; with RENORM scale * softmax over the chosen x, or
  * scale * s_e / (sum of the chosen s + 1e-20) for the sigmoid.  The bias enters
  * the choice only.

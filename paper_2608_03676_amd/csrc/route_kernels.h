@@ -3,7 +3,9 @@
 //
 //   score  s = softmax(x) or sigmoid(x);   key = s + bias, or x without a bias
 //   groups: the best `top_groups` of `groups` equal runs of experts stay, by
-//           their largest key or the sum of their two largest
+//           their largest key, or by the sum of their two largest s + bias
+//           (without a bias s, of the softmax without its common divisor: x has
+//           the order of s, but a sum of two x not that of two s)
 //   chosen: the k largest keys, the lower expert first among equals
 //   weight: c s;  renormalised: c softmax over the chosen x, or c s / (sum s + 1e-20)
 //
@@ -39,6 +41,27 @@ __device__ __forceinline__ float unordered(int b) { return __int_as_float(b ^ ((
 __device__ __forceinline__ int key_of(float x) { return x > -INFINITY ? ordered(x) : kNone; }
 
 __device__ __forceinline__ float sigmoid(float x) { return 1.f / (1.f + expf(-x)); }
+
+// Without a bias: value of a group by two, from its two largest logits (-infinity: none); m: the token's largest.
+__device__ __forceinline__ int two_scores(const RouteArgs& a, float x1, float x2, float m) {
+  if (!(x1 > -INFINITY)) return kNone;
+  return ordered(a.flags & TAOT_ROUTE_SIGMOID ? sigmoid(x1) + sigmoid(x2) : expf(x1 - m) + expf(x2 - m));
+}
+
+// Value of a group from its two largest keys.
+__device__ __forceinline__ int group_value(const RouteArgs& a, int b1, int b2, float m) {
+  if (!(a.flags & TAOT_ROUTE_GROUP_TWO) || b1 == kNone) return b1;
+  const float x2 = b2 == kNone ? -INFINITY : unordered(b2);
+  if (!a.bias) return two_scores(a, unordered(b1), x2, m);
+  return b2 == kNone ? b1 : ordered(unordered(b1) + x2);
+}
+
+// Whether the largest logit and the sum of exponentials are needed: of every softmax score that is more than a weight
+// among the chosen.
+__device__ __forceinline__ bool needs_sum(const RouteArgs& a) {
+  if (a.flags & TAOT_ROUTE_SIGMOID) return false;
+  return a.bias || !(a.flags & TAOT_ROUTE_RENORM) || (a.groups > 1 && (a.flags & TAOT_ROUTE_GROUP_TWO));
+}
 
 // Weights of the chosen experts; lane j of a block of L has the j-th (id -1: none).
 // m, sum: the largest logit and the sum of exp(x - m), where the plain softmax needs them.
@@ -212,7 +235,7 @@ __device__ __forceinline__ void route_exact(const RouteArgs& a, int64_t t, const
   };
   const bool sigm = a.flags & TAOT_ROUTE_SIGMOID;
   float m = 0.f, sum = 1.f;
-  if (!sigm && (a.bias || !(a.flags & TAOT_ROUTE_RENORM))) {
+  if (needs_sum(a)) {
     m = logit(0);
 #pragma unroll
     for (int v = 1; v < V; ++v) m = fmaxf(m, logit(v));
@@ -242,9 +265,7 @@ __device__ __forceinline__ void route_exact(const RouteArgs& a, int64_t t, const
       b1 = max(b1, key[v]);
     }
     join_two(b1, b2, lay.lpg);
-    int value = b1;
-    if ((a.flags & TAOT_ROUTE_GROUP_TWO) && b2 != kNone) value = ordered(unordered(b1) + unordered(b2));
-    if (group_rank(a, value, at.g, base, lay.lpg) >= a.top_groups) {
+    if (group_rank(a, group_value(a, b1, b2, m), at.g, base, lay.lpg) >= a.top_groups) {
 #pragma unroll
       for (int v = 0; v < V; ++v) key[v] = kNone;
     }
@@ -290,7 +311,7 @@ __device__ void route_block(const RouteArgs& a, int64_t t, int* keys) {
   };
   const bool sigm = a.flags & TAOT_ROUTE_SIGMOID;
   float m = 0.f, sum = 1.f;
-  if (!sigm && (a.bias || !(a.flags & TAOT_ROUTE_RENORM))) {
+  if (needs_sum(a)) {
     m = -INFINITY;
     for (int e = tid; e < a.E; e += 256) m = fmaxf(m, logit(e));
     m = block_reduce<kWave>(m, MaxOp());
@@ -327,10 +348,7 @@ __device__ void route_block(const RouteArgs& a, int64_t t, int* keys) {
         b2 = max(min(b1, o1), max(b2, o2));
         b1 = max(b1, o1);
       }
-      if (lane == 0) {
-        const bool two = (a.flags & TAOT_ROUTE_GROUP_TWO) && b2 != kNone;
-        value[g] = two ? ordered(unordered(b1) + unordered(b2)) : b1;
-      }
+      if (lane == 0) value[g] = group_value(a, b1, b2, m);
     }
     __syncthreads();
     for (int g = wid; g < a.groups; g += 4) {
@@ -440,7 +458,8 @@ route_few_kernel(RouteArgs a, Layout lay) {
 
   float m = 0.f, sum = 1.f;
   const bool plain = !(a.flags & (TAOT_ROUTE_SIGMOID | TAOT_ROUTE_RENORM));
-  if (MODE == kLogit || (MODE == kExact16 && plain)) {
+  const bool two = GROUPED && (a.flags & TAOT_ROUTE_GROUP_TWO);
+  if (MODE == kLogit || (MODE == kExact16 && (plain || (two && !(a.flags & TAOT_ROUTE_SIGMOID))))) {
     m = logit(0);
 #pragma unroll
     for (int v = 1; v < V; ++v) m = fmaxf(m, logit(v));
@@ -454,6 +473,20 @@ route_few_kernel(RouteArgs a, Layout lay) {
       sum = block_reduce<L>(sum, SumOp());
       open |= sum != sum;
     }
+  }
+
+  // by two without a bias: the lane's best logits themselves, so that the sums of scores decide as exact keys' would
+  float x1 = -INFINITY, x2 = -INFINITY;
+  if (MODE == kLogit && two) {
+    float all = 0.f;
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      const float x = logit(v);
+      x2 = __builtin_amdgcn_fmed3f(x1, x2, x);
+      x1 = fmaxf(x1, x);
+      all += x;
+    }
+    open |= all != all;  // NaN: the second largest is not to be relied on
   }
 
   int best[DEPTH];
@@ -533,24 +566,30 @@ route_few_kernel(RouteArgs a, Layout lay) {
   for (int i = 0; i < DEPTH; ++i) best[i] -= at.first;  // the place's complement becomes the expert's
 
   if constexpr (GROUPED) {
-    int b1 = best[0] >> kShift, b2 = best[1] >> kShift, value;
-    join_two(b1, b2, lay.lpg);
-    const bool two = a.flags & TAOT_ROUTE_GROUP_TWO, in = at.g < a.groups;
-    if constexpr (MODE == kExact16) {
-      auto float_of = [&](int o) {
-        return o > -kInf16 ? fminf((float)__builtin_bit_cast(T, (short)(o < 0 ? 0x8000 | -o : o)), kBig) : -INFINITY;
-      };
-      const float x = float_of(b1), y = float_of(b2);
-      value = x > -INFINITY ? ordered(two && y > -INFINITY ? x + y : x) : kNone;  // a sum of lowest values is a value
+    const bool in = at.g < a.groups;
+    bool stays;
+    if (MODE == kLogit && two) {
+      join_two(x1, x2, lay.lpg);
+      stays = in && group_rank(a, two_scores(a, x1, x2, m), at.g, base, lay.lpg) < a.top_groups;
     } else {
-      value = b1 + (two ? b2 : 0);
-      open |= in && (b1 <= 0 || (two && b2 <= 0));
-    }
-    const bool stays = in && group_rank(a, value, at.g, base, lay.lpg) < a.top_groups;
-    if constexpr (MODE != kExact16) {
-      const int last = -block_reduce<L>(stays ? -value : INT32_MIN, MaxOp());
-      const int next = block_reduce<L>(!stays && in ? value : 0, MaxOp());
-      open |= next > 0 && last - next < apart_two;
+      int b1 = best[0] >> kShift, b2 = best[1] >> kShift, value;
+      join_two(b1, b2, lay.lpg);
+      if constexpr (MODE == kExact16) {
+        auto float_of = [&](int o) {
+          return o > -kInf16 ? fminf((float)__builtin_bit_cast(T, (short)(o < 0 ? 0x8000 | -o : o)), kBig) : -INFINITY;
+        };
+        const float x = float_of(b1);
+        value = two ? two_scores(a, x, float_of(b2), m) : key_of(x);
+      } else {
+        value = b1 + (two ? b2 : 0);
+        open |= in && (b1 <= 0 || (two && b2 <= 0));
+      }
+      stays = in && group_rank(a, value, at.g, base, lay.lpg) < a.top_groups;
+      if constexpr (MODE != kExact16) {
+        const int last = -block_reduce<L>(stays ? -value : INT32_MIN, MaxOp());
+        const int next = block_reduce<L>(!stays && in ? value : 0, MaxOp());
+        open |= next > 0 && last - next < apart_two;
+      }
     }
 #pragma unroll
     for (int i = 0; i < DEPTH; ++i) best[i] = stays ? best[i] : INT32_MIN;
@@ -731,9 +770,10 @@ route_wide_kernel(RouteArgs a, Layout lay) {
   if constexpr (GROUPED) {
     float g1 = b1, g2 = b2;
     join_two(g1, g2, lay.lpg);
-    const bool two = (a.flags & TAOT_ROUTE_GROUP_TWO) && g2 > -INFINITY, in = at.g < a.groups;
-    const float value = two ? g1 + g2 : g1;
-    stays = in && group_rank(a, g1 > -INFINITY ? ordered(value) : kNone, at.g, 0, lay.lpg) < a.top_groups;
+    const bool two = a.flags & TAOT_ROUTE_GROUP_TWO, in = at.g < a.groups;
+    const float value = two && g2 > -INFINITY ? g1 + g2 : g1;
+    const int rank_by = !BIAS && two ? two_scores(a, g1, g2, m) : g1 > -INFINITY ? ordered(value) : kNone;
+    stays = in && group_rank(a, rank_by, at.g, 0, lay.lpg) < a.top_groups;
     if constexpr (BIAS) {
       const float last = -block_reduce<kWave>(stays ? -value : -INFINITY, MaxOp());
       const float next = block_reduce<kWave>(!stays && in ? value : -INFINITY, MaxOp());

@@ -124,3 +124,50 @@ def test_masked_rows_of_every_type(gpu, dtype, E, groups, k, flags):
     x[8, :] = low
     r, _ = _check(gpu, x, k, groups, max(1, groups // 2), flags)
     assert (r.ids[0] == -1).all() and not r.weights[0].any() and not torch.isnan(r.weights).any()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_two_logits_are_not_added(gpu, dtype):
+    """10 + 0 is more than 4 + 4, but sigmoid(10) + sigmoid(0) = 1.50 is less than 2 sigmoid(4) = 1.96."""
+    x = torch.tensor([[10.0, 0.0, 4.0, 4.0]], dtype=dtype)
+    r, _ = _check(gpu, x, 1, 2, 1, SIG | TWO)
+    assert r.ids.tolist() == [[2]]
+    # 3 - 9 is less than 0.5 + 0.5, but e^3 + e^-9 = 20.1 is more than 2 e^0.5 = 3.3
+    x = torch.tensor([[3.0, -9.0, 0.5, 0.5]], dtype=dtype)
+    r, _ = _check(gpu, x, 2, 2, 1, TWO)
+    assert r.ids.tolist() == [[0, 1]]
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("E,groups,top_groups,k", [(16, 4, 2, 4), (60, 3, 2, 6), (64, 64, 20, 8), (64, 4, 2, 6),
+                                                   (160, 8, 4, 6), (256, 8, 4, 8), (256, 16, 5, 8), (384, 8, 3, 12),
+                                                   (500, 5, 2, 8), (512, 32, 7, 8), (520, 4, 2, 8), (1000, 8, 4, 8),
+                                                   (4096, 16, 8, 8), (4096, 8, 3, 16), (1000, 4, 2, 20),
+                                                   (256, 128, 30, 8), (6000, 4, 2, 8), (9000, 8, 3, 8)])
+@pytest.mark.parametrize("flags", [TWO, REN | TWO, SIG | TWO, SIG | REN | TWO])
+def test_groups_by_two_scores(gpu, dtype, E, groups, top_groups, k, flags):
+    """By the sum of two scores, without a bias and with one; a bias of zeros chooses as none does."""
+    x = _logits(43, E, dtype, seed=E + groups, step=1 / 64)
+    r, sure = _check(gpu, x, k, groups, top_groups, flags)
+    z, sure_z = _check(gpu, x, k, groups, top_groups, flags, bias=torch.zeros(E))
+    both = torch.from_numpy(sure & sure_z)
+    assert torch.equal(r.ids.cpu()[both], z.ids.cpu()[both])
+    b = torch.randint(-20, 21, (E,), generator=torch.Generator().manual_seed(E)).float() / 256
+    _check(gpu, x, k, groups, top_groups, flags, bias=b)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("E,groups", [(64, 4), (256, 8), (512, 16), (1000, 8), (4096, 16), (6000, 4)])
+@pytest.mark.parametrize("flags", [TWO, REN | TWO, SIG | TWO])
+def test_equal_groups_and_few_experts_by_two(gpu, dtype, E, groups, flags):
+    """Equal sums: the lower group; a group with one expert counts as its score; infinities and NaN."""
+    gs = E // groups
+    x = _logits(6, E, dtype, seed=E, step=1 / 8)
+    x[0] = x[0, :gs].repeat(groups)              # groups that are alike
+    x[1] = -np.inf
+    x[1, ::gs] = x[2, ::gs]                      # one expert a group
+    x[2, gs + 1:2 * gs] = -np.inf
+    x[3, 3 * gs - 1] = float("inf")
+    x[4, ::3] = float("nan")
+    x[5] = x[5].abs().neg() - 9                  # all far below zero
+    _check(gpu, x, 2, groups, groups // 2, flags)
