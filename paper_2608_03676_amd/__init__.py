@@ -360,8 +360,8 @@ def add_rms_norm(x: torch.Tensor, weight: torch.Tensor, eps: float, residual: Op
                  group: Optional[int] = None, out: Optional[Norm] = None, stream=None) -> Norm:
     """h = x + residual, y = h * rsqrt(mean(h^2) + eps) * weight over the last dimension (taot_add_rms_norm).
     weight: [H] of x's type or float32.  group: also y in 8 bits with a scale for each `group` columns (a power
-    of two from 8 to 512), 0: one scale a row; None: no 8-bit output.  out: tensors to write to, or an earlier
-    call's result to use again."""
+    of two from 8 to 512), 0: one scale a row; None: no 8-bit output, and none left in out.  out: tensors to write
+    to, or an earlier call's result to use again."""
     _rows(x, "x")
     H = x.shape[-1] if x.dim() else 0
     _shape(_rows(weight, "weight", None if weight.dtype == torch.float32 else x), "weight", (H,))
@@ -370,20 +370,21 @@ def add_rms_norm(x: torch.Tensor, weight: torch.Tensor, eps: float, residual: Op
     lead, dev = x.shape[:-1], x.device
     if out is None:
         out = Norm()
-    out.y = _like(out.y, "out.y", x, stream)
-    out.rstd = _into(out.rstd, "out.rstd", lead, torch.float32, dev, stream)
-    out.h = x if residual is None else _like(None if out.h_is_x else out.h, "out.h", x, stream)
-    out.h_is_x = residual is None
+    y = _like(out.y, "out.y", x, stream)
+    rstd = _into(out.rstd, "out.rstd", lead, torch.float32, dev, stream)
+    h = x if residual is None else _like(None if out.h_is_x else out.h, "out.h", x, stream)
     q = s = None
     if group is not None:
-        q = out.q = _into(out.q, "out.q", x.shape, torch.float8_e4m3fn, dev, stream)
+        q = _into(out.q, "out.q", x.shape, torch.float8_e4m3fn, dev, stream)
         n = -(-H // group) if group > 0 else 1
-        s = out.scale = _into(out.scale, "out.scale", (*lead, n), torch.float32, dev, stream)
+        s = _into(out.scale, "out.scale", (*lead, n), torch.float32, dev, stream)
     T = x.numel() // H if H else 0
     _check("taot_add_rms_norm", lib().taot_add_rms_norm(
         x.data_ptr(), _ptr(residual), weight.data_ptr(), T, H, _DTYPE[x.dtype], _DTYPE[weight.dtype], float(eps),
-        int(group or 0), None if residual is None else out.h.data_ptr(), out.y.data_ptr(), _ptr(q), _ptr(s),
-        out.rstd.data_ptr(), _queue(stream, dev)))
+        int(group or 0), None if residual is None else h.data_ptr(), y.data_ptr(), _ptr(q), _ptr(s), rstd.data_ptr(),
+        _queue(stream, dev)))
+    # all of it at once: nothing of an earlier call stays beside this one's, and a refused call changes nothing
+    out.y, out.q, out.scale, out.rstd, out.h, out.h_is_x = y, q, s, rstd, h, residual is None
     return out
 
 

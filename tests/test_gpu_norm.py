@@ -250,3 +250,21 @@ def test_a_result_used_again_leaves_an_earlier_input_alone(gpu):
     n = taot.add_rms_norm(x, w, 1e-6, residual=r, out=n)
     assert n.h is h and n.y is y
     _check_forward(n, x, r, w, 1e-6, None)
+
+
+def test_a_result_used_again_keeps_nothing_of_an_earlier_call(gpu):
+    """Without an 8-bit output there is none beside the new y; a refused call leaves the result as it was."""
+    x, r, w = _inputs(gpu, 5, 96, torch.bfloat16)
+    n = taot.add_rms_norm(x, w, 1e-6, residual=r, group=32)
+    n = taot.add_rms_norm(r, w, 1e-6, residual=x, out=n)
+    assert n.q is None and n.scale is None
+    _check_forward(n, r, x, w, 1e-6, None)
+    n = taot.add_rms_norm(x, w, 1e-6, residual=r, group=32, out=n)
+    _check_forward(n, x, r, w, 1e-6, 32)
+    h, y = n.h, n.y
+    with pytest.raises(ValueError):  # another number of scales
+        taot.add_rms_norm(r, w, 1e-6, group=8, out=n)
+    with pytest.raises(taot.TaotError):
+        taot.add_rms_norm(r, w, -1.0, out=n)
+    assert n.h is h and n.y is y and not n.h_is_x
+    _check_forward(n, x, r, w, 1e-6, 32)
