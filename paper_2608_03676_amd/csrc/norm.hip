@@ -63,15 +63,15 @@ __device__ __forceinline__ float row_reduce(float v, Op op, float (*part)[16], i
 // `waves` waves hold a row (one: four rows a block); of their lanes, lane l has
 // columns 8 (i lanes + l) .. + 7 for i < CPL, so a wave's accesses are contiguous
 // and a group of 8 m columns is m neighbouring lanes at one i.
+// h and y may lie in x's or the residual's memory: a lane has read all of its columns before it writes them.
 // Bound by memory: 16384 x 4096 bfloat16, residual, groups of 128: 103 us for
 // 604 MB, 5.8 TB/s; 1237 x 5003 float16, one scale a row: 11 us for 31 MB, which
 // is one generation of waves: load, reduce, reduce, store.
 template <typename T, int CPL, bool FAR>
 __global__ void __launch_bounds__(1024)
-add_rms_norm_kernel(const T* __restrict__ x, const T* __restrict__ residual, const void* __restrict__ weight,
-                    bool w_f32, int64_t rows, int32_t H, float eps, int32_t group, T* __restrict__ h,
-                    T* __restrict__ y, uint8_t* __restrict__ q, float* __restrict__ scale,
-                    float* __restrict__ rstd, int waves) {
+add_rms_norm_kernel(const T* x, const T* residual, const void* __restrict__ weight, bool w_f32, int64_t rows,
+                    int32_t H, float eps, int32_t group, T* h, T* y, uint8_t* __restrict__ q,
+                    float* __restrict__ scale, float* __restrict__ rstd, int waves) {
   __shared__ float part[2][16];
   const int lanes = waves * kWave;
   const int lane = waves == 1 ? threadIdx.x & (kWave - 1) : threadIdx.x;
