@@ -433,6 +433,14 @@ __device__ __forceinline__ int median(int a, int b, int c) {
 
 __device__ __forceinline__ float exp_fast(float x) { return __builtin_amdgcn_exp2f(x * 1.44269504f); }
 
+// The same for x <= 0 with what the product rounds away: within 1.5 units in the last place (the fast one's error grows
+// with the distance from 0: 31 units of 2^-24 at -40), 0 below the smallest normal number.  -infinity gives 0, NaN too.
+__device__ __forceinline__ float exp_near(float x) {
+  const float c = fmaxf(x, -128.f), t = c * 1.44269504f, e = __builtin_amdgcn_exp2f(t);
+  const float d = fmaf(t, 1.90465429e-9f, fmaf(t, -0.693147182f, c));  // c - t ln 2, ln 2 in two parts
+  return fmaf(e, d, e);
+}
+
 constexpr int log2_of(int n) { return n <= 1 ? 0 : 1 + log2_of(n / 2); }
 
 template <typename T, int L, int V, int MODE, bool GROUPED>
@@ -861,6 +869,8 @@ route_backward_kernel(const float* __restrict__ dweights, const T* __restrict__ 
   if constexpr (CPL <= 2) {
     for (int e = lane; e < pitch; e += kWave) at[e] = 0.f;
   }
+  // The fast exponential's error is less than a hundredth of what rounding to 16 bits costs, but not of 32.
+  auto exponential = [](float x) { return sizeof(T) == 4 ? exp_near(x) : exp_fast(x); };
   const bool sigm = flags & TAOT_ROUTE_SIGMOID, renorm = flags & TAOT_ROUTE_RENORM, dense = !sigm && !renorm;
   for (int64_t t = (int64_t)blockIdx.x * waves + wid; t < tokens; t += (int64_t)gridDim.x * waves) {
     const T* row = logits + t * E;
@@ -911,7 +921,7 @@ route_backward_kernel(const float* __restrict__ dweights, const T* __restrict__ 
       auto add = [&](f32x8& r) {
 #pragma unroll
         for (int u = 0; u < 8; ++u) {
-          r[u] = exp_fast(r[u] - m);
+          r[u] = exponential(r[u] - m);
           sum += r[u];
         }
       };
@@ -935,7 +945,7 @@ route_backward_kernel(const float* __restrict__ dweights, const T* __restrict__ 
       }
       sum = block_reduce<kWave>(sum, SumOp());
       inv = sum > 0.f ? 1.f / sum : 0.f;
-      q = block_reduce<kWave>(has ? dw * (exp_fast(x - m) * inv) : 0.f, SumOp());
+      q = block_reduce<kWave>(has ? dw * (exponential(x - m) * inv) : 0.f, SumOp());
     }
     if constexpr (CPL > 2) {
       f32x8 r[CPL];
@@ -985,7 +995,7 @@ route_backward_kernel(const float* __restrict__ dweights, const T* __restrict__ 
           if (dense) {
             z = chunk(e);
 #pragma unroll
-            for (int u = 0; u < 8; ++u) z[u] = exp_fast(z[u] - m);
+            for (int u = 0; u < 8; ++u) z[u] = exponential(z[u] - m);
           }
           write(e, z);
         }

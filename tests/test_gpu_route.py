@@ -324,3 +324,19 @@ def test_empty_and_refusals(gpu):
     ids = torch.zeros(4, 2, dtype=torch.int32, device=gpu)
     with pytest.raises(ValueError):
         taot.route_backward(torch.zeros(4, 3, device=gpu), x, ids)
+
+
+def test_backward_of_experts_far_below_the_best(gpu):
+    """Softmax: the best expert's probability is 1 here, that of the others e^(x - m), x - m exact.  Their gradient is
+    -e^(x - m): 2 units of 2^-24 for the exponential (1 unit in the last place), a quarter for the sum that is taken as
+    1 (7 e^-20), and one for what is left to the products."""
+    g = torch.Generator().manual_seed(8)
+    for E in (8, 1000, 4096, 5000):  # one to eight chunks of experts a lane, and any number; far ones are masked
+        x = torch.full((400, E), -np.inf)
+        x[:, 1:8] = -torch.randint(20 * 64, 80 * 64, (400, 7), generator=g).float() / 64
+        x[:, 0] = 0.0
+        ids = torch.zeros(400, 1, dtype=torch.int32)
+        d = taot.route_backward(torch.ones(400, 1, device=gpu), x.to(gpu), ids.to(gpu)).double().cpu()
+        p = torch.softmax(x[:, :8].double(), 1)
+        want = -p[:, 1:] * p[:, :1]
+        assert ((d[:, 1:8] - want).abs() <= 3.5 * 2.0 ** -24 * want.abs()).all(), ((d[:, 1:8] - want) / want).abs().max() * 2 ** 24
