@@ -431,6 +431,11 @@ __device__ __forceinline__ int median(int a, int b, int c) {
   return r;
 }
 
+// Its error at -d is at most 0.8 d + 2 units of 2^-24 (the product's rounding, the constant's, the instruction's).
+// Good enough for keys that are looked at again where it could decide, and for the sum of a softmax: mass at a distance
+// d takes e^d experts, so that of 4096 the sum is off by 9 units at most, 1 for normally distributed logits, where
+// its own 70 additions are worth as much.  With the remainder (exp_near): 8192 x 4096 bfloat16 19.6 us instead of 17.4,
+// 65536 x 256 14.2 instead of 12.8.
 __device__ __forceinline__ float exp_fast(float x) { return __builtin_amdgcn_exp2f(x * 1.44269504f); }
 
 // The same for x <= 0 with what the product rounds away: within 1.5 units in the last place (the fast one's error grows
