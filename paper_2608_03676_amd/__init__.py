@@ -14,7 +14,8 @@ Around them: add_rms_norm (residual addition, norm, 8-bit output) and route
 (logits to expert ids, which plan_loads reads, and weights) before; then
 dispatch_map (the schedule on the single copies), dispatch_rows and
 combine_rows (rows to the send buffer and back).  The *_backward calls are
-their gradients.
+their gradients.  None of them is part of torch's graph: inputs whose gradient
+is being recorded are refused.
 """
 from __future__ import annotations
 
@@ -315,6 +316,16 @@ def _shape(t: torch.Tensor, name: str, shape):
         raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
 
 
+def _inputs(fn: str, names: str, *tensors):
+    """Refuses inputs whose gradient is being recorded: these calls are no part of torch's graph, and their results
+    would carry none."""
+    grad = torch.is_grad_enabled()
+    for i, t in enumerate(tensors):
+        if t is not None and grad and t.requires_grad:
+            raise RuntimeError(f"{names.split()[i]} requires a gradient, which {fn} does not record: detach it or call "
+                               "under torch.no_grad(), and take the gradients from the *_backward calls")
+
+
 def _empty(shape, dtype, device, stream) -> torch.Tensor:
     """New memory of the stream that the call's work goes to: what used it before is done when that work begins, and
     it is not handed out again before that work is done."""
@@ -367,6 +378,7 @@ def add_rms_norm(x: torch.Tensor, weight: torch.Tensor, eps: float, residual: Op
     _shape(_rows(weight, "weight", None if weight.dtype == torch.float32 else x), "weight", (H,))
     if residual is not None:
         _shape(_rows(residual, "residual", x), "residual", x.shape)
+    _inputs("add_rms_norm", "x weight residual", x, weight, residual)
     lead, dev = x.shape[:-1], x.device
     if out is None:
         out = Norm()
@@ -405,6 +417,7 @@ def add_rms_norm_backward(dy: torch.Tensor, h: torch.Tensor, rstd: torch.Tensor,
         _shape(_rows(dh, "dh", h), "dh", h.shape)
     _shape(_rows(weight, "weight", None if weight.dtype == torch.float32 else h), "weight", (H,))
     _shape(_dev(rstd, "rstd", torch.float32), "rstd", h.shape[:-1])
+    _inputs("add_rms_norm_backward", "dy h rstd weight dh", dy, h, rstd, weight, dh)
     if out is None:
         out = NormGrad()
     out.dx = _like(out.dx, "out.dx", h, stream)
@@ -433,6 +446,7 @@ def route(logits: torch.Tensor, top_k: int, bias: Optional[torch.Tensor] = None,
     E = logits.shape[-1] if logits.dim() else 0
     if bias is not None:
         _shape(_dev(bias, "bias", torch.float32), "bias", (E,))
+    _inputs("route", "logits bias", logits, bias)
     shape = (*logits.shape[:-1], top_k)
     if out is None:
         out = Routing()
@@ -454,6 +468,7 @@ def route_backward(dweights: torch.Tensor, logits: torch.Tensor, ids: torch.Tens
     shape = (*logits.shape[:-1], top_k)
     _shape(_dev(ids, "ids", torch.int32), "ids", shape)
     _shape(_dev(dweights, "dweights", torch.float32), "dweights", shape)
+    _inputs("route_backward", "dweights logits", dweights, logits)
     out = _like(out, "out", logits, stream)
     T = logits.numel() // E if E else 0
     _check("taot_route_backward", lib().taot_route_backward(
@@ -523,10 +538,12 @@ def dispatch_rows(x: torch.Tensor, pos: torch.Tensor, scale: Optional[torch.Tens
         raise ValueError("x must be contiguous")
     lead = x.shape[:-1]
     rows, tokens, k = _tokens(pos, lead, "x")
+    if scale is not None:
+        _shape(_dev(scale, "scale", torch.float32), "scale", (*lead, scale.shape[-1]))
+    _inputs("dispatch_rows", "x scale", x, scale)
     out = _into(out, "out", (*pos.shape, x.shape[-1]), x.dtype, x.device, stream)
     more = 0
     if scale is not None:
-        _shape(_dev(scale, "scale", torch.float32), "scale", (*lead, scale.shape[-1]))
         out_scale = _into(out_scale, "out_scale", (*pos.shape, scale.shape[-1]), torch.float32, x.device, stream)
         more = 4 * scale.shape[-1]
     _check("taot_dispatch_rows", lib().taot_dispatch_rows(
@@ -546,6 +563,7 @@ def combine_rows(y: torch.Tensor, pos: torch.Tensor, weights: Optional[torch.Ten
         raise ValueError(f"{N} copies are not top_k = {top_k} of each token")
     if weights is not None and _dev(weights, "weights", torch.float32).numel() != pos.numel():
         raise ValueError("weights must have a value for each copy")
+    _inputs("combine_rows", "y weights", y, weights)
     lead = (*y.shape[:-2], N // top_k)
     out = _into(out, "out", (*lead, H), y.dtype, y.device, stream)
     rows, tokens, _ = _tokens(pos, lead, "y")
@@ -576,6 +594,7 @@ def combine_rows_backward(dout: torch.Tensor, y: torch.Tensor, pos: torch.Tensor
     _shape(dout, "dout", (*dout.shape[:-1], H))
     if _dev(weights, "weights", torch.float32).numel() != pos.numel():
         raise ValueError("weights must have a value for each copy")
+    _inputs("combine_rows_backward", "dout y weights", dout, y, weights)
     if out is None:
         out = CombineGrad()
     out.dy = _like(out.dy, "out.dy", y, stream)

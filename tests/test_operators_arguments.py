@@ -1,0 +1,45 @@
+"""The calls around the planner refuse what they cannot answer: inputs whose
+gradient they would lose, shapes without the dimensions they need, tensors of
+several devices."""
+import pytest
+import torch
+
+import paper_2608_03676_amd as taot
+
+gpu_test = pytest.mark.gpu
+
+
+def _calls(gpu):
+    """name -> (call, its floating inputs)"""
+    T, H, E, k = 4, 16, 8, 2
+    f = {n: torch.ones(s, device=gpu) for n, s in dict(
+        x=(T, H), residual=(T, H), weight=(H,), dy=(T, H), dh=(T, H), h=(T, H), rstd=(T,), logits=(T, E), bias=(E,),
+        dweights=(T, k), rows=(T, H), scale=(T, 1), y=(T * k, H), weights=(T * k,), dout=(T, H)).items()}
+    ids = torch.arange(T * k, dtype=torch.int32, device=gpu).view(T, k) % E
+    pos = torch.arange(T * k, dtype=torch.int32, device=gpu)
+    return f, {
+        "add_rms_norm": (lambda a: taot.add_rms_norm(a["x"], a["weight"], 1e-6, residual=a["residual"]),
+                         ("x", "weight", "residual")),
+        "add_rms_norm_backward": (lambda a: taot.add_rms_norm_backward(a["dy"], a["h"], a["rstd"], a["weight"], dh=a["dh"]),
+                                  ("dy", "h", "rstd", "weight", "dh")),
+        "route": (lambda a: taot.route(a["logits"], k, bias=a["bias"]), ("logits", "bias")),
+        "route_backward": (lambda a: taot.route_backward(a["dweights"], a["logits"], ids), ("dweights", "logits")),
+        "dispatch_rows": (lambda a: taot.dispatch_rows(a["rows"], pos, scale=a["scale"]), ("rows", "scale")),
+        "combine_rows": (lambda a: taot.combine_rows(a["y"], pos, weights=a["weights"], top_k=k), ("y", "weights")),
+        "combine_rows_backward": (lambda a: taot.combine_rows_backward(a["dout"], a["y"], pos, a["weights"]),
+                                  ("dout", "y", "weights"))}
+
+
+@gpu_test
+def test_inputs_that_want_a_gradient(gpu):
+    """The results carry no gradient: refused while gradients are recorded, taken under no_grad and when detached."""
+    f, calls = _calls(gpu)
+    for name, (call, inputs) in calls.items():
+        call(f)
+        for i in inputs:
+            a = dict(f, **{i: f[i].clone().requires_grad_()})
+            with pytest.raises(RuntimeError, match=i if i != "rows" else "x"):
+                call(a)
+            with torch.no_grad():
+                call(a)
+            call(dict(f, **{i: a[i].detach()}))
