@@ -352,9 +352,16 @@ def _like(t: Optional[torch.Tensor], name: str, x: torch.Tensor, stream) -> torc
 def _room(workspace: Optional[torch.Tensor], nbytes: int, device, stream) -> torch.Tensor:
     if workspace is None:
         return _into(None, "workspace", (max(int(nbytes), 1),), torch.uint8, device, stream)
+    if not isinstance(workspace, torch.Tensor):
+        raise TypeError("workspace must be a GPU tensor")
     if not workspace.is_cuda or not workspace.is_contiguous():
         raise ValueError("workspace must be a contiguous GPU tensor")
     return workspace
+
+
+def _weight(t: torch.Tensor, like: torch.Tensor, H: int):
+    f32 = isinstance(t, torch.Tensor) and t.dtype == torch.float32
+    _shape(_rows(t, "weight", None if f32 else like), "weight", (H,))
 
 
 @dataclasses.dataclass
@@ -375,7 +382,7 @@ def add_rms_norm(x: torch.Tensor, weight: torch.Tensor, eps: float, residual: Op
     to, or an earlier call's result to use again."""
     _rows(x, "x")
     H = x.shape[-1] if x.dim() else 0
-    _shape(_rows(weight, "weight", None if weight.dtype == torch.float32 else x), "weight", (H,))
+    _weight(weight, x, H)
     if residual is not None:
         _shape(_rows(residual, "residual", x), "residual", x.shape)
     _inputs("add_rms_norm", "x weight residual", x, weight, residual)
@@ -415,7 +422,7 @@ def add_rms_norm_backward(dy: torch.Tensor, h: torch.Tensor, rstd: torch.Tensor,
     _shape(_rows(dy, "dy", h), "dy", h.shape)
     if dh is not None:
         _shape(_rows(dh, "dh", h), "dh", h.shape)
-    _shape(_rows(weight, "weight", None if weight.dtype == torch.float32 else h), "weight", (H,))
+    _weight(weight, h, H)
     _shape(_dev(rstd, "rstd", torch.float32), "rstd", h.shape[:-1])
     _inputs("add_rms_norm_backward", "dy h rstd weight dh", dy, h, rstd, weight, dh)
     if out is None:
@@ -464,9 +471,9 @@ def route_backward(dweights: torch.Tensor, logits: torch.Tensor, ids: torch.Tens
     """Gradient of route's weights by the logits (taot_route_backward): [..., E] of the logits' type."""
     _rows(logits, "logits")
     E = logits.shape[-1] if logits.dim() else 0
-    top_k = ids.shape[-1]
+    top_k = ids.shape[-1] if _dev(ids, "ids", torch.int32).dim() else 0
     shape = (*logits.shape[:-1], top_k)
-    _shape(_dev(ids, "ids", torch.int32), "ids", shape)
+    _shape(ids, "ids", shape)
     _shape(_dev(dweights, "dweights", torch.float32), "dweights", shape)
     _inputs("route_backward", "dweights logits", dweights, logits)
     out = _like(out, "out", logits, stream)
@@ -519,6 +526,8 @@ def dispatch_map(ids: torch.Tensor, home: torch.Tensor, slot_expert: torch.Tenso
 def _tokens(pos: torch.Tensor, lead, name: str):
     """(rows, tokens, top_k) of positions [..., N] and a tensor of shape [*lead, tokens, ...]."""
     _dev(pos, "pos", torch.int32)
+    if not pos.dim() or not len(lead):
+        raise ValueError(f"{name} must be [..., rows, H] and pos [..., N]")
     N, tokens = pos.shape[-1], lead[-1]
     if tuple(pos.shape[:-1]) != tuple(lead[:-1]) or (N % tokens if tokens else N):
         raise ValueError(f"{name} of {tuple(lead)} tokens does not go with positions of shape {tuple(pos.shape)}")
@@ -526,6 +535,13 @@ def _tokens(pos: torch.Tensor, lead, name: str):
     for d in lead[:-1]:
         rows *= d
     return rows, tokens, N // tokens if tokens else 1
+
+
+def _sent(y: torch.Tensor, pos: torch.Tensor):
+    """Checks rows of a send buffer and the positions in it."""
+    if _rows(y, "y").dim() < 2:
+        raise ValueError(f"y must be [..., N, H], got {tuple(y.shape)}")
+    _shape(_dev(pos, "pos", torch.int32), "pos", y.shape[:-1])
 
 
 def dispatch_rows(x: torch.Tensor, pos: torch.Tensor, scale: Optional[torch.Tensor] = None,
@@ -539,7 +555,7 @@ def dispatch_rows(x: torch.Tensor, pos: torch.Tensor, scale: Optional[torch.Tens
     lead = x.shape[:-1]
     rows, tokens, k = _tokens(pos, lead, "x")
     if scale is not None:
-        _shape(_dev(scale, "scale", torch.float32), "scale", (*lead, scale.shape[-1]))
+        _shape(_dev(scale, "scale", torch.float32), "scale", (*lead, scale.shape[-1] if scale.dim() else 1))
     _inputs("dispatch_rows", "x scale", x, scale)
     out = _into(out, "out", (*pos.shape, x.shape[-1]), x.dtype, x.device, stream)
     more = 0
@@ -556,8 +572,7 @@ def combine_rows(y: torch.Tensor, pos: torch.Tensor, weights: Optional[torch.Ten
                  out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """Weighted sum of each token's top_k rows of y [..., N, H] back in the tokens' order, [..., N / top_k, H]
     (taot_combine_rows).  weights [..., N] float32 or None (all 1), as route gives them: [..., tokens, top_k] too."""
-    _rows(y, "y")
-    _shape(_dev(pos, "pos", torch.int32), "pos", y.shape[:-1])
+    _sent(y, pos)
     N, H = y.shape[-2:]
     if top_k < 1 or N % top_k:
         raise ValueError(f"{N} copies are not top_k = {top_k} of each token")
@@ -586,9 +601,8 @@ def combine_rows_backward(dout: torch.Tensor, y: torch.Tensor, pos: torch.Tensor
                           out: Optional[CombineGrad] = None, stream=None) -> CombineGrad:
     """Gradient of combine_rows by y and the weights (taot_combine_rows_backward).  Without weights the gradient is
     dispatch_rows(dout, pos)."""
-    _rows(y, "y")
+    _sent(y, pos)
     _rows(dout, "dout", y)
-    _shape(_dev(pos, "pos", torch.int32), "pos", y.shape[:-1])
     H = y.shape[-1]
     rows, tokens, k = _tokens(pos, dout.shape[:-1], "dout")
     _shape(dout, "dout", (*dout.shape[:-1], H))

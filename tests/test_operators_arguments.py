@@ -43,3 +43,32 @@ def test_inputs_that_want_a_gradient(gpu):
             with torch.no_grad():
                 call(a)
             call(dict(f, **{i: a[i].detach()}))
+
+
+@gpu_test
+def test_what_lacks_a_dimension_or_is_no_tensor(gpu):
+    f, _ = _calls(gpu)
+    x, w, logits, y = f["x"], f["weight"], f["logits"], f["y"]
+    pos = torch.arange(8, dtype=torch.int32, device=gpu)
+    ids = torch.zeros((4, 2), dtype=torch.int32, device=gpu)
+    one, zero_dim = torch.ones(8, device=gpu), torch.zeros((), dtype=torch.int32, device=gpu)
+    for call in (lambda: taot.dispatch_rows(x[0], pos), lambda: taot.dispatch_rows(x, zero_dim),
+                 lambda: taot.dispatch_rows(x, pos, scale=one[0]), lambda: taot.dispatch_rows(one[0], pos),
+                 lambda: taot.combine_rows(one, pos), lambda: taot.combine_rows(one, zero_dim),
+                 lambda: taot.combine_rows(one[0], zero_dim), lambda: taot.combine_rows_backward(one, y, pos, f["weights"]),
+                 lambda: taot.combine_rows_backward(x, one, pos, f["weights"]),
+                 lambda: taot.combine_rows_backward(x, one, zero_dim, f["weights"]),
+                 lambda: taot.combine_rows_backward(one[0], one[0], zero_dim, one[0]),
+                 lambda: taot.route_backward(f["dweights"], logits, zero_dim),
+                 lambda: taot.dispatch_map(ids[None], pos, ids, zero_dim, 1),
+                 lambda: taot.dispatch_map(zero_dim, pos, ids, ids[None], 1)):
+        with pytest.raises(ValueError):
+            call()
+    for call in (lambda: taot.add_rms_norm(x, None, 1e-6), lambda: taot.add_rms_norm(x, 1.0, 1e-6),
+                 lambda: taot.add_rms_norm_backward(x, x, f["rstd"], None), lambda: taot.add_rms_norm_backward(None, x, f["rstd"], w),
+                 lambda: taot.add_rms_norm_backward(x, x, f["rstd"], w, workspace=1 << 20),
+                 lambda: taot.route_backward(f["dweights"], logits, None), lambda: taot.route_backward(None, logits, ids),
+                 lambda: taot.dispatch_rows(x, None), lambda: taot.combine_rows(y, None),
+                 lambda: taot.combine_rows_backward(x, y, pos, None)):
+        with pytest.raises(TypeError):
+            call()
