@@ -37,6 +37,7 @@ ROUTE_SIGMOID, ROUTE_RENORM, ROUTE_GROUP_TWO = 0x1, 0x2, 0x4  # route flags
 STATUS_NAMES = {0: "ok", 1: "invalid argument", 2: "unsupported shape", 3: "workspace", 4: "launch"}
 
 _lib = None
+_devices = 0  # GPUs that the process sees, once the library is loaded
 _P, _I32, _I64, _F32, _F64, _SZ, _U32 = (ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_float,
                                          ctypes.c_double, ctypes.c_size_t, ctypes.c_uint32)
 
@@ -49,7 +50,7 @@ class TaotError(RuntimeError):
 
 def lib():
     """Load libtaot.so (raises if it has not been built)."""
-    global _lib
+    global _lib, _devices
     if _lib is None:
         if not os.path.exists(LIB_PATH):
             raise RuntimeError(f"{LIB_PATH} is missing: build it with __graft_entry__.build()")
@@ -92,6 +93,7 @@ def lib():
         L.taot_topology_pref.restype = ctypes.c_int
         L.taot_topology_pref.argtypes = [_P, _I32, _P, _P]
         _lib = L
+        _devices = torch.cuda.device_count()
     return _lib
 
 
@@ -316,14 +318,34 @@ def _shape(t: torch.Tensor, name: str, shape):
         raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
 
 
-def _inputs(fn: str, names: str, *tensors):
-    """Refuses inputs whose gradient is being recorded: these calls are no part of torch's graph, and their results
-    would carry none."""
-    grad = torch.is_grad_enabled()
+def _inputs(fn: str, names: str, stream, *tensors):
+    """Refuses tensors (and a stream) of several devices, and inputs whose gradient is being recorded: these calls are
+    no part of torch's graph, and their results would carry none."""
+    if torch.is_grad_enabled():
+        for i, t in enumerate(tensors):
+            if t is not None and t.requires_grad:
+                raise RuntimeError(f"{names.split()[i]} requires a gradient, which {fn} does not record: detach it or "
+                                   "call under torch.no_grad(), and take the gradients from the *_backward calls")
+    if _devices == 1:
+        return
+    dev = tensors[0].get_device()
     for i, t in enumerate(tensors):
-        if t is not None and grad and t.requires_grad:
-            raise RuntimeError(f"{names.split()[i]} requires a gradient, which {fn} does not record: detach it or call "
-                               "under torch.no_grad(), and take the gradients from the *_backward calls")
+        if t is not None and t.get_device() != dev:
+            raise ValueError(f"{names.split()[i]} is on cuda:{t.get_device()}, {names.split()[0]} on cuda:{dev}")
+    if stream is not None and stream.device_index != dev:
+        raise ValueError(f"the stream is of cuda:{stream.device_index}, {names.split()[0]} on cuda:{dev}")
+
+
+def _launch(fn: str, device, stream, *args):
+    """Calls the library with the tensors' device as the current one, which a launch goes to."""
+    call = getattr(lib(), fn)
+    if _devices == 1 or torch._C._cuda_getDevice() == device.index:
+        code = call(*args, _queue(stream, device))
+    else:
+        with torch.cuda.device(device):
+            code = call(*args, _queue(stream, device))
+    if code != 0:
+        raise TaotError(fn, code)
 
 
 def _empty(shape, dtype, device, stream) -> torch.Tensor:
@@ -333,12 +355,18 @@ def _empty(shape, dtype, device, stream) -> torch.Tensor:
         return torch.empty(shape, dtype=dtype, device=device)
 
 
+def _on(t: torch.Tensor, name: str, device):
+    if _devices != 1 and t.get_device() != device.index:
+        raise ValueError(f"{name} is on cuda:{t.get_device()}, the inputs on {device}")
+
+
 def _into(t: Optional[torch.Tensor], name: str, shape, dtype, device, stream) -> torch.Tensor:
     """The caller's output tensor, checked, or a new one."""
     if t is None:
         return (torch.empty(tuple(shape), dtype=dtype, device=device) if stream is None else
                 _empty(shape, dtype, device, stream))
     _shape(_dev(t, name, dtype), name, shape)
+    _on(t, name, device)
     return t
 
 
@@ -356,6 +384,7 @@ def _room(workspace: Optional[torch.Tensor], nbytes: int, device, stream) -> tor
         raise TypeError("workspace must be a GPU tensor")
     if not workspace.is_cuda or not workspace.is_contiguous():
         raise ValueError("workspace must be a contiguous GPU tensor")
+    _on(workspace, "workspace", device)
     return workspace
 
 
@@ -385,7 +414,7 @@ def add_rms_norm(x: torch.Tensor, weight: torch.Tensor, eps: float, residual: Op
     _weight(weight, x, H)
     if residual is not None:
         _shape(_rows(residual, "residual", x), "residual", x.shape)
-    _inputs("add_rms_norm", "x weight residual", x, weight, residual)
+    _inputs("add_rms_norm", "x weight residual", stream, x, weight, residual)
     lead, dev = x.shape[:-1], x.device
     if out is None:
         out = Norm()
@@ -398,10 +427,9 @@ def add_rms_norm(x: torch.Tensor, weight: torch.Tensor, eps: float, residual: Op
         n = -(-H // group) if group > 0 else 1
         s = _into(out.scale, "out.scale", (*lead, n), torch.float32, dev, stream)
     T = x.numel() // H if H else 0
-    _check("taot_add_rms_norm", lib().taot_add_rms_norm(
+    _launch("taot_add_rms_norm", dev, stream,
         x.data_ptr(), _ptr(residual), weight.data_ptr(), T, H, _DTYPE[x.dtype], _DTYPE[weight.dtype], float(eps),
-        int(group or 0), None if residual is None else h.data_ptr(), y.data_ptr(), _ptr(q), _ptr(s), rstd.data_ptr(),
-        _queue(stream, dev)))
+        int(group or 0), None if residual is None else h.data_ptr(), y.data_ptr(), _ptr(q), _ptr(s), rstd.data_ptr())
     # all of it at once: nothing of an earlier call stays beside this one's, and a refused call changes nothing
     out.y, out.q, out.scale, out.rstd, out.h, out.h_is_x = y, q, s, rstd, h, residual is None
     return out
@@ -424,17 +452,17 @@ def add_rms_norm_backward(dy: torch.Tensor, h: torch.Tensor, rstd: torch.Tensor,
         _shape(_rows(dh, "dh", h), "dh", h.shape)
     _weight(weight, h, H)
     _shape(_dev(rstd, "rstd", torch.float32), "rstd", h.shape[:-1])
-    _inputs("add_rms_norm_backward", "dy h rstd weight dh", dy, h, rstd, weight, dh)
+    _inputs("add_rms_norm_backward", "dy h rstd weight dh", stream, dy, h, rstd, weight, dh)
     if out is None:
         out = NormGrad()
     out.dx = _like(out.dx, "out.dx", h, stream)
     out.dweight = _into(out.dweight, "out.dweight", (H,), torch.float32, h.device, stream)
     T = h.numel() // H if H else 0
     ws = _room(workspace, lib().taot_add_rms_norm_backward_workspace_size(T, H), h.device, stream)
-    _check("taot_add_rms_norm_backward", lib().taot_add_rms_norm_backward(
+    _launch("taot_add_rms_norm_backward", h.device, stream,
         dy.data_ptr(), _ptr(dh), h.data_ptr(), rstd.data_ptr(), weight.data_ptr(), T, H, _DTYPE[h.dtype],
         _DTYPE[weight.dtype], out.dx.data_ptr(), out.dweight.data_ptr(), ws.data_ptr(),
-        ws.numel() * ws.element_size(), _queue(stream, h.device)))
+        ws.numel() * ws.element_size())
     return out
 
 
@@ -453,16 +481,16 @@ def route(logits: torch.Tensor, top_k: int, bias: Optional[torch.Tensor] = None,
     E = logits.shape[-1] if logits.dim() else 0
     if bias is not None:
         _shape(_dev(bias, "bias", torch.float32), "bias", (E,))
-    _inputs("route", "logits bias", logits, bias)
+    _inputs("route", "logits bias", stream, logits, bias)
     shape = (*logits.shape[:-1], top_k)
     if out is None:
         out = Routing()
     out.ids = _into(out.ids, "out.ids", shape, torch.int32, logits.device, stream)
     out.weights = _into(out.weights, "out.weights", shape, torch.float32, logits.device, stream)
     T = logits.numel() // E if E else 0
-    _check("taot_route", lib().taot_route(
+    _launch("taot_route", logits.device, stream,
         logits.data_ptr(), _ptr(bias), T, E, int(top_k), int(groups), int(top_groups), float(scale), int(flags),
-        _DTYPE[logits.dtype], out.ids.data_ptr(), out.weights.data_ptr(), _queue(stream, logits.device)))
+        _DTYPE[logits.dtype], out.ids.data_ptr(), out.weights.data_ptr())
     return out
 
 
@@ -475,12 +503,12 @@ def route_backward(dweights: torch.Tensor, logits: torch.Tensor, ids: torch.Tens
     shape = (*logits.shape[:-1], top_k)
     _shape(ids, "ids", shape)
     _shape(_dev(dweights, "dweights", torch.float32), "dweights", shape)
-    _inputs("route_backward", "dweights logits", dweights, logits)
+    _inputs("route_backward", "logits ids dweights", stream, logits, ids, dweights)
     out = _like(out, "out", logits, stream)
     T = logits.numel() // E if E else 0
-    _check("taot_route_backward", lib().taot_route_backward(
+    _launch("taot_route_backward", logits.device, stream,
         dweights.data_ptr(), logits.data_ptr(), ids.data_ptr(), T, E, top_k, float(scale), int(flags),
-        _DTYPE[logits.dtype], out.data_ptr(), _queue(stream, logits.device)))
+        _DTYPE[logits.dtype], out.data_ptr())
     return out
 
 
@@ -508,6 +536,7 @@ def dispatch_map(ids: torch.Tensor, home: torch.Tensor, slot_expert: torch.Tenso
     S = R * K
     _shape(X, "X", (B, R, S))
     _shape(slot_expert, "slot_expert", (B, S))
+    _inputs("dispatch_map", "ids home slot_expert X", stream, ids, home, slot_expert, X)
     dev = ids.device
     if out is None:
         out = Dispatch()
@@ -516,10 +545,10 @@ def dispatch_map(ids: torch.Tensor, home: torch.Tensor, slot_expert: torch.Tenso
     out.sends = _into(out.sends, "out.sends", (B, rows, R), torch.int32, dev, stream)
     out.status = _into(out.status, "out.status", (B,), torch.int32, dev, stream)
     ws = _room(workspace, lib().taot_dispatch_map_workspace_size(B, rows, N, R, E, K), dev, stream)
-    _check("taot_dispatch_map", lib().taot_dispatch_map(
+    _launch("taot_dispatch_map", dev, stream,
         ids.data_ptr(), B, rows, int(rank0), N, home.data_ptr(), R, E, int(K), slot_expert.data_ptr(), X.data_ptr(),
         out.pos.data_ptr(), out.offsets.data_ptr(), out.sends.data_ptr(), out.status.data_ptr(), ws.data_ptr(),
-        ws.numel() * ws.element_size(), _queue(stream, dev)))
+        ws.numel() * ws.element_size())
     return out
 
 
@@ -556,15 +585,15 @@ def dispatch_rows(x: torch.Tensor, pos: torch.Tensor, scale: Optional[torch.Tens
     rows, tokens, k = _tokens(pos, lead, "x")
     if scale is not None:
         _shape(_dev(scale, "scale", torch.float32), "scale", (*lead, scale.shape[-1] if scale.dim() else 1))
-    _inputs("dispatch_rows", "x scale", x, scale)
+    _inputs("dispatch_rows", "x pos scale", stream, x, pos, scale)
     out = _into(out, "out", (*pos.shape, x.shape[-1]), x.dtype, x.device, stream)
     more = 0
     if scale is not None:
         out_scale = _into(out_scale, "out_scale", (*pos.shape, scale.shape[-1]), torch.float32, x.device, stream)
         more = 4 * scale.shape[-1]
-    _check("taot_dispatch_rows", lib().taot_dispatch_rows(
+    _launch("taot_dispatch_rows", x.device, stream,
         x.data_ptr(), x.shape[-1] * x.element_size(), _ptr(scale), more, rows, tokens, k, pos.data_ptr(),
-        out.data_ptr(), _ptr(out_scale) if scale is not None else None, _queue(stream, x.device)))
+        out.data_ptr(), _ptr(out_scale) if scale is not None else None)
     return out if scale is None else (out, out_scale)
 
 
@@ -578,13 +607,12 @@ def combine_rows(y: torch.Tensor, pos: torch.Tensor, weights: Optional[torch.Ten
         raise ValueError(f"{N} copies are not top_k = {top_k} of each token")
     if weights is not None and _dev(weights, "weights", torch.float32).numel() != pos.numel():
         raise ValueError("weights must have a value for each copy")
-    _inputs("combine_rows", "y weights", y, weights)
+    _inputs("combine_rows", "y pos weights", stream, y, pos, weights)
     lead = (*y.shape[:-2], N // top_k)
     out = _into(out, "out", (*lead, H), y.dtype, y.device, stream)
     rows, tokens, _ = _tokens(pos, lead, "y")
-    _check("taot_combine_rows", lib().taot_combine_rows(
-        y.data_ptr(), pos.data_ptr(), _ptr(weights), rows, tokens, int(top_k), H, _DTYPE[y.dtype], out.data_ptr(),
-        _queue(stream, y.device)))
+    _launch("taot_combine_rows", y.device, stream,
+        y.data_ptr(), pos.data_ptr(), _ptr(weights), rows, tokens, int(top_k), H, _DTYPE[y.dtype], out.data_ptr())
     return out
 
 
@@ -608,14 +636,14 @@ def combine_rows_backward(dout: torch.Tensor, y: torch.Tensor, pos: torch.Tensor
     _shape(dout, "dout", (*dout.shape[:-1], H))
     if _dev(weights, "weights", torch.float32).numel() != pos.numel():
         raise ValueError("weights must have a value for each copy")
-    _inputs("combine_rows_backward", "dout y weights", dout, y, weights)
+    _inputs("combine_rows_backward", "y pos dout weights", stream, y, pos, dout, weights)
     if out is None:
         out = CombineGrad()
     out.dy = _like(out.dy, "out.dy", y, stream)
     out.dweights = _like(out.dweights, "out.dweights", weights, stream)
-    _check("taot_combine_rows_backward", lib().taot_combine_rows_backward(
+    _launch("taot_combine_rows_backward", y.device, stream,
         dout.data_ptr(), y.data_ptr(), pos.data_ptr(), weights.data_ptr(), rows, tokens, k, H, _DTYPE[y.dtype],
-        out.dy.data_ptr(), out.dweights.data_ptr(), _queue(stream, y.device)))
+        out.dy.data_ptr(), out.dweights.data_ptr())
     return out
 
 

@@ -1,6 +1,9 @@
 """The calls around the planner refuse what they cannot answer: inputs whose
 gradient they would lose, shapes without the dimensions they need, tensors of
 several devices."""
+import contextlib
+import types
+
 import pytest
 import torch
 
@@ -72,3 +75,44 @@ def test_what_lacks_a_dimension_or_is_no_tensor(gpu):
                  lambda: taot.combine_rows_backward(x, y, pos, None)):
         with pytest.raises(TypeError):
             call()
+
+
+def _stand_in(index):
+    return types.SimpleNamespace(get_device=lambda: index, device_index=index, requires_grad=False)
+
+
+def test_tensors_of_several_devices(monkeypatch):
+    """The checks alone, on the CPU: one device for all tensors and the stream."""
+    monkeypatch.setattr(taot, "_devices", 2)
+    a, b = _stand_in(0), _stand_in(1)
+    taot._inputs("f", "x w", None, a, a)
+    taot._inputs("f", "x w", a, a, None)
+    with pytest.raises(ValueError, match="w is on cuda:1, x on cuda:0"):
+        taot._inputs("f", "x y w", None, a, None, b)
+    with pytest.raises(ValueError, match="the stream is of cuda:1"):
+        taot._inputs("f", "x", b, a)
+    taot._on(a, "out", torch.device("cuda:0"))
+    with pytest.raises(ValueError, match="out is on cuda:1"):
+        taot._on(b, "out", torch.device("cuda:0"))
+
+
+@pytest.mark.parametrize("device,current", [(0, 0), (1, 0), (2, 1)])
+def test_a_launch_goes_to_the_tensors_device(monkeypatch, device, current):
+    """On the CPU, with a library that notes the device that is current when it is called."""
+    now, seen = [current], []
+
+    @contextlib.contextmanager
+    def switch(d):
+        was, now[0] = now[0], d.index
+        yield
+        now[0] = was
+
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: now[0], raising=False)
+    monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda i: 100 + i, raising=False)
+    monkeypatch.setattr(torch.cuda, "device", switch)
+    fake = types.SimpleNamespace(f=lambda *a: seen.append((now[0], a)) or 0)
+    monkeypatch.setattr(taot, "lib", lambda: fake)
+    monkeypatch.setattr(taot, "_devices", 3)
+    taot._launch("f", torch.device("cuda", device), None, 1, 2)
+    taot._launch("f", torch.device("cuda", device), types.SimpleNamespace(cuda_stream=7), 3)
+    assert seen == [(device, (1, 2, 100 + device)), (device, (3, 7))] and now == [current]
