@@ -892,14 +892,16 @@ Plan carve(void* ws, int32_t B, int32_t rows, int64_t N, int32_t R, int32_t E, i
   return p;
 }
 
-// f by the number of bits of an expert, as a constant that is large enough.
-template <typename F>
+// f by the number of bits of an expert (MOST at most), as a constant that is large enough.
+template <int MOST, typename F>
 auto with_bits(int bits, F f) {
   if (bits <= 6) return f(std::integral_constant<int, 6>());
   if (bits <= 8) return f(std::integral_constant<int, 8>());
   if (bits <= 9) return f(std::integral_constant<int, 9>());
-  if (bits <= 12) return f(std::integral_constant<int, 12>());
-  return f(std::integral_constant<int, 15>());
+  if constexpr (MOST > 12) {
+    if (bits > 12) return f(std::integral_constant<int, MOST>());
+  }
+  return f(std::integral_constant<int, 12>());
 }
 
 template <typename F>
@@ -945,7 +947,9 @@ taot_status launch_dispatch_map(const int32_t* ids, int32_t B, int32_t rows, int
     const int wanted = (int)((N + kWave - 1) / kWave), row_waves = wanted < 1 ? 1 : wanted < 16 ? wanted : 16;
     const size_t lds = row_room(R, E, S, row_waves).bytes;
     if (lds <= kRowLds) {
-      auto* kernel = with_bits(bits, [](auto n) { return row_kernel<n.value>; });
+      // an expert takes 32 bytes of a row's LDS and more: no 4096 of them fit
+      static_assert(kRowLds < 32 << 12, "bits of an expert of a short row");
+      auto* kernel = with_bits<12>(bits, [](auto n) { return row_kernel<n.value>; });
       if (!allow_lds(reinterpret_cast<const void*>(kernel), lds)) return TAOT_ERR_LAUNCH;
       // one row a problem: its bits are the problem's status
       uint32_t* bad = status && rows == 1 ? status : reinterpret_cast<uint32_t*>(p.t.placed);
@@ -975,7 +979,7 @@ taot_status launch_dispatch_map(const int32_t* ids, int32_t B, int32_t rows, int
     if (!keep) place_waves = waves;
     const int32_t place_blocks = (chunks + place_waves - 1) / place_waves;
     const size_t lds = keep ? kept(place_waves) : waves * row_lds;
-    auto* kernel = keep ? place_kernel<kKept> : with_bits(bits, [](auto n) { return place_kernel<n.value>; });
+    auto* kernel = keep ? place_kernel<kKept> : with_bits<kExpertBits>(bits, [](auto n) { return place_kernel<n.value>; });
     if (!allow_lds(reinterpret_cast<const void*>(kernel), lds)) return TAOT_ERR_LAUNCH;
     kernel<<<(unsigned)(n * place_blocks), kThreads, lds, stream>>>(ids, p.t, p.hist, N, rows, E, S, chunk, chunks,
                                                                   place_blocks, place_waves, pos);

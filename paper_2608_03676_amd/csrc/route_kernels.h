@@ -1028,9 +1028,16 @@ taot_status go(const RouteArgs& a, Layout lay, hipStream_t stream) {
     else if (a.k <= kWideMost && sigm) route_wide_kernel<T, V, true, GROUPED><<<blocks, 256, lds, stream>>>(a, lay);
     else if constexpr (V <= 16) route_kernel<T, L, V, GROUPED><<<blocks, 256, 0, stream>>>(a, lay);
   } else {
-    if (a.k <= 8 && !a.bias) route_few_kernel<T, L, V, kPlain, GROUPED><<<blocks, 256, 0, stream>>>(a, lay);
-    else if (a.k <= 8 && sigm) route_few_kernel<T, L, V, kSigmoid, GROUPED><<<blocks, 256, 0, stream>>>(a, lay);
-    else route_kernel<T, L, V, GROUPED><<<blocks, 256, 0, stream>>>(a, lay);
+    // by route_of's rules eight lanes have few choices only, and 16 of 16 experts without groups many only
+    constexpr bool kFew = L != 16 || V != 16 || GROUPED, kMany = L != 8;
+    const bool plain = a.k <= 8 && !a.bias, sigmoids = a.k <= 8 && a.bias && sigm;
+    if constexpr (kFew) {
+      if (plain) route_few_kernel<T, L, V, kPlain, GROUPED><<<blocks, 256, 0, stream>>>(a, lay);
+      else if (sigmoids) route_few_kernel<T, L, V, kSigmoid, GROUPED><<<blocks, 256, 0, stream>>>(a, lay);
+    }
+    if constexpr (kMany) {
+      if (!kFew || !(plain || sigmoids)) route_kernel<T, L, V, GROUPED><<<blocks, 256, 0, stream>>>(a, lay);
+    }
   }
   return hipGetLastError() == hipSuccess ? TAOT_OK : TAOT_ERR_LAUNCH;
 }
