@@ -400,7 +400,7 @@ __device__ void route_block(const RouteArgs& a, int64_t t, int* keys) {
 template <typename T>
 __global__ void __launch_bounds__(256)
 route_block_kernel(RouteArgs a) {
-  extern __shared__ int keys[];
+  extern __shared__ __attribute__((aligned(16))) int keys[];
   route_block<T>(a, blockIdx.x, keys);
 }
 
@@ -665,7 +665,7 @@ __global__ void __launch_bounds__(256, sizeof(T) == 4 && BIAS ? 2 : sizeof(T) ==
 route_wide_kernel(RouteArgs a, Layout lay) {
   using Place = Lanes<T, kWave, V, GROUPED>;
   constexpr int W = Place::W;
-  extern __shared__ int keys[];
+  extern __shared__ __attribute__((aligned(16))) int keys[];  // the wide rows' biases are read 16 bytes at a time
   __shared__ int2 found[4][kWave + 1];  // an expert and its logit; behind the 64th all in one place
   __shared__ int32_t undecided[4];
   __shared__ float part[4];
