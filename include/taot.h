@@ -257,7 +257,8 @@ taot_status taot_round_schedule(const int32_t* n, const int64_t* spill, const in
 /* Around the planner: what makes the routing ids, and what carries a plan out
  * on the tokens.  The calls below take rows of floating values of one of three
  * types; rows may begin at any address that the type allows.  Sums, scores,
- * norms and statistics are in 32 bits and each output is rounded once. */
+ * norms and statistics are in 32 bits and each output is rounded once.  No output
+ * shares memory with an input or with another output, except where it is said. */
 typedef enum {
   TAOT_BF16 = 0,
   TAOT_F16 = 1,
@@ -294,7 +295,8 @@ taot_status taot_add_rms_norm(const void* x, const void* residual, const void* w
  *   dweight = sum_t dy * h * s
  *   dy, h    [T][H] dtype    dh [T][H] dtype, nullable: what reaches h itself
  *   rstd     [T]    float
- * Outputs: dx [T][H] dtype, the gradient of x and of the residual alike;
+ * Outputs: dx [T][H] dtype, the gradient of x and of the residual alike (it may be
+ * dy's, dh's or h's own storage, with the same pointer);
  * dweight [H] float (zero where T = 0; the same bits on every run). */
 size_t taot_add_rms_norm_backward_workspace_size(int64_t T, int32_t H);
 taot_status taot_add_rms_norm_backward(const void* dy, const void* dh, const void* h, const float* rstd,
@@ -334,7 +336,8 @@ taot_status taot_route(const void* logits, const float* bias, int64_t T, int32_t
                        void* stream);
 /* Its gradient by the logits, for the choice as it was made: dweights [T][k]
  * float, logits [T][E], ids [T][k] (distinct within a token; -1: no gradient)
- * -> dlogits [T][E] dtype, zero for experts that the weights do not depend on.
+ * -> dlogits [T][E] dtype, zero for experts that the weights do not depend on (it
+ * may be the logits' own storage, with the same pointer).
  * flags and scale as in the call that chose (GROUP_TWO has no effect). */
 taot_status taot_route_backward(const float* dweights, const void* logits, const int32_t* ids, int64_t T, int32_t E,
                                 int32_t k, float scale, uint32_t flags, int32_t dtype, void* dlogits, void* stream);

@@ -861,12 +861,13 @@ route_wide_kernel(RouteArgs a, Layout lay) {
 // read back as the row to write, or, where that row would leave room for few
 // waves, to their places in registers one after the other (4096 x 4096: 23 us, 29
 // by LDS; 32768 x 384: 26 us, 17 by LDS).  The plain softmax adds
-// -p_e sum_j dw_j w_j to every expert.
+// -p_e sum_j dw_j w_j to every expert.  dlogits may lie in the logits' memory: the
+// chosen experts' are read before the wave writes, the others by the lane that
+// writes them, before it does.
 template <typename T, int CPL>
 __global__ void __launch_bounds__(256)
-route_backward_kernel(const float* __restrict__ dweights, const T* __restrict__ logits,
-                      const int32_t* __restrict__ ids, int64_t tokens, int32_t E, int32_t k, float scale,
-                      uint32_t flags, T* __restrict__ dlogits, int32_t pitch) {
+route_backward_kernel(const float* __restrict__ dweights, const T* logits, const int32_t* __restrict__ ids,
+                      int64_t tokens, int32_t E, int32_t k, float scale, uint32_t flags, T* dlogits, int32_t pitch) {
   extern __shared__ float lds[];
   const int lane = threadIdx.x & (kWave - 1), wid = threadIdx.x / kWave;
   const int waves = blockDim.x / kWave;

@@ -35,3 +35,30 @@ def test_norm(gpu, dtype, T, H):
         m = x.clone()
         n = taot.add_rms_norm(m, w, 1e-6, group=group, out=taot.Norm(y=m))
         assert n.y is m and torch.equal(m, plain.y)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("T,H", SHAPES + [(1500, 512), (700, 9000)])
+def test_gradient(gpu, dtype, T, H):
+    """dx in the memory of what it is made from; rows enough that workers take several."""
+    print(f"[norm's gradient in place] {dtype} {T} x {H}", flush=True)
+    h, dy, dh, w = (_random(gpu, *s, dtype=dtype, seed=H + i) for i, s in enumerate([(T, H)] * 3 + [(H,)]))
+    s = torch.rand(T, device=gpu, generator=torch.Generator(gpu).manual_seed(T)) + 0.5
+    for d in (dh, None):
+        want = taot.add_rms_norm_backward(dy, h, s, w, dh=d)
+        for at in ("h", "dy") + (("dh",) if d is not None else ()):
+            m = dict(h=h.clone(), dy=dy.clone(), dh=None if d is None else d.clone())
+            got = taot.add_rms_norm_backward(m["dy"], m["h"], s, w, dh=m["dh"], out=taot.NormGrad(dx=m[at]))
+            assert got.dx is m[at] and torch.equal(got.dx, want.dx) and torch.equal(got.dweight, want.dweight), at
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("T,E", [(9, 8), (5, 60), (20000, 384), (70, 777), (33, 4096), (9, 4104), (3, 9001)])
+@pytest.mark.parametrize("flags", [0, taot.ROUTE_RENORM, taot.ROUTE_SIGMOID, taot.ROUTE_SIGMOID | taot.ROUTE_RENORM])
+def test_gradient_of_routing(gpu, dtype, T, E, flags):
+    x = _random(gpu, T, E, dtype=dtype, seed=E)
+    r = taot.route(x, 8, flags=flags)
+    dw = _random(gpu, T, 8, dtype=torch.float32, seed=T)
+    want = taot.route_backward(dw, x, r.ids, flags=flags)
+    m = x.clone()
+    assert taot.route_backward(dw, m, r.ids, flags=flags, out=m) is m and torch.equal(m, want)
