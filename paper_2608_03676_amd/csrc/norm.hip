@@ -237,12 +237,19 @@ struct Shape {
 };
 // Waves, and chunks of eight columns per lane, that hold a row of H: as few
 // chunks as 16 waves allow (16384 rows of 2048 in 32 bits: 109 us, 116 with two;
-// the gradient of 16384 x 4096, 98 and 124).  Forward, rows of 16 bits that would
-// take 8 to 15 waves take two (16384 x 4096: 104 us, 110 with one; 4096 x 8192,
-// which keeps one, 54 and 56).
-Shape shape_of(int32_t H, bool forward16) {
-  const int chunks = (H + 7) / 8;
-  int cpl = forward16 && chunks >= 512 && chunks < 1024 ? 2 : 1;
+// the gradient of 16384 x 4096, 98 and 124).
+// Forward, rows of 16 bits take two where one would take 8 to 16 waves, with a
+// residual 9 to 15.  128 MiB of bfloat16, new outputs, us with two and one chunk;
+// y alone without a residual, then h, y and groups of 128 with one:
+//   3592 columns, 8 waves    51, 58     112, 107
+//   4096,         8          47, 53     104, 99
+//   5120,        10          51, 65     102, 112
+//   7168,        14          50, 59     102, 105
+//   8184,        16          52, 60     113, 108
+//   8192,        16          48, 59     104, 103
+Shape shape_of(int32_t H, bool forward16, bool residual) {
+  const int chunks = (H + 7) / 8, waves = (chunks + kWave - 1) / kWave;
+  int cpl = forward16 && waves >= (residual ? 9 : 8) && waves <= (residual ? 15 : 16) ? 2 : 1;
   while (cpl * 16 * kWave < chunks) cpl *= 2;
   return {(chunks + cpl * kWave - 1) / (cpl * kWave), cpl};
 }
@@ -256,7 +263,7 @@ Shape shape_of(int32_t H, bool forward16) {
 // Of many more the partial sums cost more than they bring (60000 rows of 512: 57
 // us, 62 with 24 waves a unit).
 int32_t backward_workers(int64_t rows, int32_t H) {
-  const Shape s = shape_of(H, false);
+  const Shape s = shape_of(H, false, true);
   int blocks = (16 + s.waves - 1) / s.waves;
   if (blocks * s.waves > (s.cpl == 1 ? 24 : 16)) --blocks;
   const int64_t most = 256 * blocks;
@@ -275,7 +282,7 @@ template <typename T>
 taot_status forward(const void* x, const void* residual, const void* weight, bool w_f32, int64_t rows, int32_t H,
                     float eps, int32_t group, void* h, void* y, uint8_t* q, float* scale, float* rstd,
                     hipStream_t stream) {
-  const Shape s = shape_of(H, sizeof(T) == 2);
+  const Shape s = shape_of(H, sizeof(T) == 2, residual != nullptr);
   const int per = s.waves == 1 ? kRowsOfBlock : 1;
   const int64_t groups = group > 0 ? (H + group - 1) / group : 1;
   const bool ok = with_chunks(s.cpl, [&](auto C) {
@@ -300,7 +307,7 @@ taot_status backward(const void* dy, const void* dh, const void* h, const float*
   const int32_t workers = backward_workers(rows, H);
   bool ok = true;
   if (rows > 0) {
-    const Shape s = shape_of(H, false);
+    const Shape s = shape_of(H, false, true);
     const int per = s.waves == 1 ? kRowsOfBlock : 1;
     ok = with_chunks(s.cpl, [&](auto C) {
       auto* kernel = with_far(rows * H * (int64_t)sizeof(T), [](auto far) {
