@@ -782,9 +782,8 @@ combine_kernel(const T* __restrict__ y, const int32_t* __restrict__ pos, const f
   }
 }
 
-// dy[pos] = w dout, dw = <dout, y[pos]>; kAhead copies at a time.  Many rows of dy
-// go past the caches (8192 tokens of 2048 in 16 bits, 8 copies: 112 us for 570 MB, 5.1 TB/s; 119
-// through them; 16384 of 512, 4 copies: 26 and 44 us).
+// dy[pos] = w dout, dw = <dout, y[pos]>; kAhead copies at a time.  8192 tokens of
+// 2048 in 16 bits, 8 copies: 112 us for 570 MB, 5.1 TB/s; 119 through the caches.
 template <typename T, int WAVES, bool FAR>
 __global__ void __launch_bounds__(256)
 combine_backward_kernel(const T* __restrict__ dout, const T* __restrict__ y, const int32_t* __restrict__ pos,
@@ -1002,7 +1001,7 @@ taot_status launch_dispatch_rows(const void* x, int64_t row_bytes, const void* x
   const Payload a{static_cast<const char*>(x), static_cast<char*>(out), row_bytes};
   const Payload b{static_cast<const char*>(x_more), static_cast<char*>(out_more), more_bytes};
   const int64_t all = rows * tokens;
-  with_far(all * k * row_bytes, [&](auto far) {
+  with_far(all * k * (row_bytes + more_bytes), [&](auto far) {
     const bool wide = row_bytes > 2048;
     auto* kernel = wide ? rows_kernel<4, far.value> : rows_kernel<1, far.value>;
     by_blocks(all, wide ? 1 : 4, [&](uint32_t first, unsigned blocks) {

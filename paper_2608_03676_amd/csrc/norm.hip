@@ -285,8 +285,9 @@ taot_status forward(const void* x, const void* residual, const void* weight, boo
   const Shape s = shape_of(H, sizeof(T) == 2, residual != nullptr);
   const int per = s.waves == 1 ? kRowsOfBlock : 1;
   const int64_t groups = group > 0 ? (H + group - 1) / group : 1;
+  const int64_t bytes = rows * H * (((h != nullptr) + (y != nullptr)) * (int64_t)sizeof(T) + (q != nullptr));
   const bool ok = with_chunks(s.cpl, [&](auto C) {
-    auto* kernel = with_far(rows * H * (int64_t)sizeof(T), [](auto far) {
+    auto* kernel = with_far(bytes, [](auto far) {
       return add_rms_norm_kernel<T, decltype(C)::value, far.value>;
     });
     for (int64_t r = 0; r < rows; r += kMaxBlocks * per) {

@@ -52,11 +52,20 @@ __device__ __forceinline__ void store_row(T* p, f32x8 v, int n) {
     if (u < n) p[u] = (T)v[u];
 }
 
-// Outputs larger than the L2 caches (4 MiB in each of the 8 dies) are written
-// past them: nothing of them would be left there for who reads them next, and
-// what is being read keeps its place (norm of 16384 x 4096 in 16 bits: 104 us,
-// 111 through the caches; 2048 x 4096: 13.6 and 13.6).
-constexpr int64_t kFarBytes = 32 << 20;
+// A call's outputs of as much as the memory-side cache holds (256 MiB) are written
+// past the caches: little of them would be left for who reads them next, and what
+// is being read keeps its place.  Smaller ones are not, though the call itself may
+// be faster so, for the next reader finds them there.  Call and the reader of its
+// output (combine_rows of 8), us past the caches and through them, by the outputs'
+// size; bfloat16, 4096 columns, inputs of several calls in turn:
+//                               32       64       128       256       384 MiB
+//   norm, y alone             21, 21   38, 36   76,  68  150, 144  219, 223
+//   norm's gradient with dh   44, 41   74, 69  137, 134  262, 270
+//   8 copies of a row         15, 14   27, 25   55,  47  118, 106  178, 208
+//   the way back's gradient   22, 22   42, 40   90,  74  177, 180  264, 269
+// Norm with h, y and groups of 128, and y's reader, 160, 240 and 320 MiB: 64, 63;
+// 92, 99; 133, 138.
+constexpr int64_t kFarBytes = 256 << 20;
 
 // Blocks of a launch: their threads, up to 1024 each, are counted in 32 bits.
 // Larger work is done by several launches.

@@ -85,3 +85,44 @@ def test_gradient_of_the_way_back_past_the_caches(gpu, dtype, tokens, k, H):
     assert ((c.dy[0][at].double() - want).abs() <= lim).all()
     gone = (pos[0] < 0).nonzero().flatten()
     assert len(gone) and not c.dy[0][~pos[0][gone].long()].any() and not c.dweights[0][gone].any()
+
+
+# 256 MiB of output and more: past the caches, with one, two and four chunks of columns a lane
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("T,H", [(140000, 1000), (16400, 8192), (9000, 16000), (4500, 30011)])
+def test_norm_past_the_caches(gpu, dtype, T, H):
+    print(f"[norm] {dtype} {T} x {H}", flush=True)
+    T = T // (2 if dtype == torch.float32 else 1)
+    x, r, w = norm._inputs(gpu, T, H, dtype)
+    n = taot.add_rms_norm(x, w, 1e-6, residual=r, group=256)
+    h, s, y = norm._reference(x, r, w, 1e-6)
+    del h
+    assert ((n.rstd.double() - s).abs() <= norm.FP * s).all()
+    slack = 2.0 ** -23 * (x.double().abs() + r.double().abs()) * s[:, None] * w.double().abs()
+    assert ((n.y.double() - y).abs() <= (norm.U[dtype] + norm.FP) * y.abs() + norm.LOW[dtype] + slack).all()
+    some = slice(T - 700, T)  # the last rows of all outputs, and that a call on them alone gives the same
+    part = taot.add_rms_norm(x[some], w, 1e-6, residual=r[some], group=256)
+    norm._check_forward(part, x[some], r[some], w, 1e-6, 256)
+    for name in ("h", "y", "q", "scale", "rstd"):
+        assert torch.equal(getattr(n, name)[some].view(torch.uint8), getattr(part, name).view(torch.uint8))
+    del y, slack, part
+    dy, dh = (torch.randn(T, H, generator=torch.Generator(gpu).manual_seed(i), device=gpu).to(dtype) for i in (1, 2))
+    d = taot.add_rms_norm_backward(dy, n.h, n.rstd, w, dh=dh)
+    part = taot.add_rms_norm_backward(dy[some], n.h[some], n.rstd[some], w, dh=dh[some])
+    norm._check_backward(part, dy[some], dh[some], n.h[some], n.rstd[some], w)
+    assert torch.equal(d.dx[some], part.dx)
+    want = (dy.double() * n.h.double() * n.rstd.double()[:, None])
+    size = want.abs().sum(0)
+    assert ((d.dweight.double() - want.sum(0)).abs() <= (T / 512 + 52) * 2.0 ** -24 * size).all()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("tokens,k,H", [(17000, 8, 1000), (8300, 4, 4100)])
+def test_there_and_back_past_the_caches(gpu, dtype, tokens, k, H):
+    test_gradient_of_the_way_back_past_the_caches(gpu, dtype, tokens, k, H)
+    pos = torch.from_numpy(dispatch._positions(1, tokens * k, seed=H, dropped=0.1)).to(gpu)
+    x = torch.randn(1, tokens, H, generator=torch.Generator(gpu).manual_seed(k), device=gpu).to(dtype)
+    out = taot.dispatch_rows(x, pos)
+    there = (pos[0] >= 0).nonzero().flatten()
+    assert torch.equal(out[0][pos[0][there].long()], x[0][there // k])
+    assert not out[0][~pos[0][pos[0] < 0].long()].any()
