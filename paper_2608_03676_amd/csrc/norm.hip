@@ -64,9 +64,9 @@ __device__ __forceinline__ float row_reduce(float v, Op op, float (*part)[16], i
 // columns 8 (i lanes + l) .. + 7 for i < CPL, so a wave's accesses are contiguous
 // and a group of 8 m columns is m neighbouring lanes at one i.
 // h and y may lie in x's or the residual's memory: a lane has read all of its columns before it writes them.
-// Bound by memory: 16384 x 4096 bfloat16, residual, groups of 128: 103 us for
-// 604 MB, 5.8 TB/s; 1237 x 5003 float16, one scale a row: 11 us for 31 MB, which
-// is one generation of waves: load, reduce, reduce, store.
+// Bound by memory: 16384 x 4096 bfloat16, residual, groups of 128: 99 us for
+// 604 MB, 6.1 TB/s.  1237 x 5003 float16, one scale a row: 10 us for 31 MB; all of
+// its waves are resident at once, so nothing loads while others reduce and store.
 template <typename T, int CPL, bool FAR>
 __global__ void __launch_bounds__(1024)
 add_rms_norm_kernel(const T* x, const T* residual, const void* __restrict__ weight, bool w_f32, int64_t rows,
@@ -137,7 +137,7 @@ add_rms_norm_kernel(const T* x, const T* residual, const void* __restrict__ weig
 // registers of 16 waves hold both (CPL <= 2).  dx may lie in dy's, dh's or h's
 // memory: a row is read by its worker alone, each place by the lane that writes
 // it, before it does.  8192 x 5120 bfloat16 with a
-// residual's gradient: 66 us for 335 MB, 5.1 TB/s.
+// residual's gradient: 68 us for 335 MB, 4.9 TB/s.
 template <typename T, int CPL, bool FAR>
 __global__ void __launch_bounds__(1024)
 add_rms_norm_backward_kernel(const T* dy, const T* dh, const T* h, const float* __restrict__ rstd,

@@ -220,7 +220,8 @@ __device__ __forceinline__ void join_two(V& b1, V& b2, int32_t lpg) {
 
 // Tokens by keys of 32 bits, rounded as the formulas say: a round takes the
 // maximum over the registers and removes it.  Any number of choices; bound by
-// k passes over the registers (65536 x 256 bfloat16, 12 choices: 33 us, 40 MB).
+// k passes over the registers (65536 x 256 bfloat16, 12 choices: 43 us for 40 MB,
+// 1600 vector instructions a wave that issue all the time).
 template <typename T, int L, int V, bool GROUPED>
 __device__ __forceinline__ void route_exact(const RouteArgs& a, int64_t t, const Layout& lay) {
   const Lanes<T, L, V, GROUPED> at(a, lay);
@@ -295,8 +296,9 @@ route_kernel(RouteArgs a, Layout lay) {
 }
 
 // A token by a block of 256 threads, any number of experts: the keys of
-// route_exact in LDS.  Bound by its barriers, one a round (8192 x 4096 bfloat16,
-// 8 choices: 104 us, where route_wide_kernel takes 18).
+// route_exact in LDS.  Bound by its passes over the row and its barriers, one a
+// round (8192 x 4096 bfloat16, softmax and bias, 8 choices: 131 us; without the bias
+// route_wide_kernel takes 18).
 template <typename T>
 __device__ void route_block(const RouteArgs& a, int64_t t, int* keys) {
   __shared__ int value[TAOT_MAX_ROUTE_GROUPS];
@@ -420,8 +422,9 @@ route_block_kernel(RouteArgs a) {
 // that ran out of words, and one with keys that the fixed point does not hold
 // (0: masked, or too low) is done again by exact keys, with the whole wave.
 // Bound by the eight medians of every expert: 65536 x 256 float32, bias, 8 groups:
-// 29 us (71 MB, 2.5 TB/s; the vector units issue 62 % of the time); 65536 x 256
-// bfloat16: 12.6 us.
+// 30 us (71 MB, 2.4 TB/s; 1056 vector instructions a wave, 15 us of issue); 65536 x
+// 256 bfloat16: 13 us (806 and 11).  Equal float32 logits among a token's first k + 1
+// are undecided too: rounded to bfloat16 first, 65536 x 256 take 66 us, 20 else.
 constexpr int kExact16 = 0, kLogit = 1, kSigmoid = 2;
 constexpr float kLogitRange = 32.f;
 
