@@ -268,6 +268,8 @@ typedef enum {
 #define TAOT_MAX_WIDTH 32768      /* columns of a row of the norm                */
 #define TAOT_MAX_TOP_K 64         /* experts chosen per token                    */
 #define TAOT_MAX_ROUTE_GROUPS 256 /* groups of experts                           */
+#define TAOT_MAX_INNER 131071     /* terms of a sum of products of 8-bit integers:
+                                     as many as 32 bits hold                     */
 
 /* Residual addition and root-mean-square norm, with an 8-bit output.
  *   h = x + residual,  s = 1 / sqrt(mean_c h^2 + eps),  y = h * s * weight
@@ -390,6 +392,104 @@ taot_status taot_combine_rows(const void* y, const int32_t* pos, const float* we
 taot_status taot_combine_rows_backward(const void* dout, const void* y, const int32_t* pos, const float* weights,
                                        int64_t rows, int64_t tokens, int32_t k, int32_t H, int32_t dtype, void* dy,
                                        float* dweights, void* stream);
+
+/* Norms before and after a block, fused with its gate and the scaled residual.
+ *   a = 1 / sqrt(mean_c x^2 + eps),  n = x * a * post  (n = x without post)
+ *   h = alpha * residual + gate * n                    (without a gate: + n)
+ *   b = 1 / sqrt(mean_c h^2 + eps),  y = h * b * weight
+ *   x        [T][H] dtype    the block's output
+ *   residual [T][H] dtype
+ *   post     [H]    weight_dtype, nullable: no norm behind the block
+ *   gate     [gates][H] gate_dtype, nullable: `gates` divides T, and row t has gate
+ *            t / (T / gates) (1: one for all; T: one a row); weight_dtype and
+ *            gate_dtype: dtype or TAOT_F32
+ *   weight   [H]    weight_dtype, nullable: no norm before the next block, no y
+ *   eps      >= 0, finite;  alpha finite
+ * Outputs (each nullable; y is null without weight):
+ *   h        [T][H] dtype    rounded where it is stored only
+ *   y        [T][H] dtype
+ *   rstd_x, rstd_h [T] float  a and b, for the gradient (written with post and weight)
+ * x and residual may be h or y's own storage only if the pointers are equal.
+ * Limits: 1 <= H <= TAOT_MAX_WIDTH, 0 <= T <= 2^31 - 1. */
+taot_status taot_block_norm(const void* x, const void* residual, const void* post, const void* gate, int64_t gates,
+                            const void* weight, int64_t T, int32_t H, int32_t dtype, int32_t weight_dtype,
+                            int32_t gate_dtype, float eps, float alpha, void* h, void* y, float* rstd_x, float* rstd_h,
+                            void* stream);
+/* Its gradient:
+ *   D = dh + b * (g - h * b^2 * mean_c(g * h)) with g = dy * weight
+ *   dresidual = alpha * D,  t = D * gate * post,  dx = a * (t - x * a^2 * mean_c(t * x))
+ *   (dx = t without post),  dweight = sum_t dy * h * b,
+ *   dgate = sum over the gate's rows of D * n,  dpost = sum_t D * gate * x * a
+ *   dy, h    [T][H] dtype, rstd_h [T] float: null without weight, else given
+ *   dh       [T][H] dtype, nullable: what reaches h itself (given without weight)
+ *   x        [T][H] dtype;  rstd_x [T] float: given with post
+ * Outputs: dx, dresidual [T][H] dtype (each may be an input's own storage, with the
+ * same pointer); dweight [H], dpost [H], dgate [gates][H] float, each nullable and
+ * null without its vector (zero where T = 0; the same bits on every run). */
+size_t taot_block_norm_backward_workspace_size(int64_t T, int32_t H, int64_t gates);
+taot_status taot_block_norm_backward(const void* dy, const void* dh, const void* x, const void* h, const float* rstd_x,
+                                     const float* rstd_h, const void* post, const void* gate, int64_t gates,
+                                     const void* weight, int64_t T, int32_t H, int32_t dtype, int32_t weight_dtype,
+                                     int32_t gate_dtype, float alpha, void* dx, void* dresidual, float* dweight,
+                                     float* dpost, float* dgate, void* ws, size_t ws_bytes, void* stream);
+
+/* The router's balance loss: how far choices and scores of `rows` sets of tokens,
+ * each by itself, are from an even spread over the experts (1 where they are even).
+ *   p_t = softmax(x_t), or with TAOT_ROUTE_SIGMOID sigmoid(x_t) / (their sum + 1e-20)
+ *   c_e = choices of expert e,  n = tokens,  P_e = (1 / n) sum_t p_te
+ *   loss = E * sum_e (c_e / sum c) * P_e,  z = (1 / n) sum_t (log sum_e exp x_te)^2
+ *   logits   [rows][tokens][E] dtype   ids [rows][tokens][k] int32, as taot_route gives them
+ *            (those outside [0, E) are no choice)
+ *   mask     [rows][tokens] bytes, nullable: tokens of mask 0 count nowhere
+ * Outputs: loss [rows] float; z [rows] float, nullable (null with SIGMOID); counts
+ * [rows][E] int32, c; prob [rows][E] float, P; counted [rows] int32, n, nullable.
+ * Where n or sum c is 0 it divides as 1.  An expert whose logit is NaN or -infinity
+ * has p = 0, +infinity counts as the largest float; a token without other experts has
+ * p = 0 throughout and a logarithm of 0.  The same bits on every run.
+ * Limits: 1 <= k <= TAOT_MAX_TOP_K, E <= TAOT_MAX_EXPERTS, rows * tokens * k <= 2^31 - 1. */
+size_t taot_balance_loss_workspace_size(int64_t rows, int64_t tokens, int32_t E);
+taot_status taot_balance_loss(const void* logits, const int32_t* ids, const uint8_t* mask, int64_t rows, int64_t tokens,
+                              int32_t E, int32_t k, uint32_t flags, int32_t dtype, float* loss, float* z,
+                              int32_t* counts, float* prob, int32_t* counted, void* ws, size_t ws_bytes, void* stream);
+/* Its gradient by the logits: the choices are constants, which may come from more
+ * tokens than these (the counts of all ranks: then dloss is scaled to the mean over
+ * these tokens).  With a_e = dloss * E * c_e / (n * sum c):
+ *   dx = p * (a - sum a p + 2 * dz / n * lse), or of the sigmoids s with sum V
+ *   dx = (a - sum a p) / V * s * (1 - s);  dlogits = add + dx
+ *   dloss [rows], dz [rows] float (nullable; null with SIGMOID); counts, counted as given
+ *   add      [rows][tokens][E] dtype, nullable: what reaches the logits otherwise
+ * Output: dlogits [rows][tokens][E] dtype, add alone for tokens of mask 0 (it may be the
+ * logits' or add's own storage, with the same pointer). */
+taot_status taot_balance_loss_backward(const float* dloss, const float* dz, const void* logits, const int32_t* counts,
+                                       const int32_t* counted, const uint8_t* mask, const void* add, int64_t rows,
+                                       int64_t tokens, int32_t E, uint32_t flags, int32_t dtype, void* dlogits,
+                                       void* stream);
+
+/* Rows as 8-bit integers with a scale each.
+ *   v = x, or gated: silu(g) * u of a row [g | u];  a = max_c |v|, of at least 1e-30
+ *   q = v * (127 / a) to the nearest integer (even of two);  scale = a / 127
+ *   x        [T][H] dtype, gated [T][2 H]
+ * Outputs: q [T][H] int8, scale [T] float.  A row that holds NaN or an infinity has
+ * scale NaN and q = 0, so that what is made of it is NaN.
+ * Limits: 1 <= H <= TAOT_MAX_WIDTH, 0 <= T <= 2^31 - 1. */
+taot_status taot_quantize_rows(const void* x, int64_t T, int32_t H, int32_t gated, int32_t dtype, int8_t* q,
+                               float* scale, void* stream);
+/* Products of such rows with 8-bit weights that have a scale for each channel:
+ *   out[t][n] = scale[t] * weight_scale[e][n] * sum_k x[t][k] * weight[e][n][k]
+ * with the sum exact and the product rounded once.
+ *   x        [M][K] int8, scale [M] float;  weight [G][N][K] int8, weight_scale [G][N] float
+ *   offsets  [runs + 1] int32: run i has rows offsets[i] .. offsets[i + 1] - 1 (as
+ *            taot_dispatch_map's instances have); offsets are taken within [0, M], each as at
+ *            least the one before it.  Null, with runs = 0 and G = 1: one run of all rows
+ *   experts  [runs] int32: the weight of each run, nullable (run i has weight i)
+ * Output: out [M][N] dtype; rows of no run, and of runs whose expert is not in
+ * [0, G), are zero.
+ * Limits: 1 <= K <= TAOT_MAX_INNER, 0 <= M <= 2^30, 1 <= N <= 2^30, 0 <= runs <= 2^30.
+ * The workspace is needed with offsets only. */
+size_t taot_matmul_i8_workspace_size(int64_t M, int32_t runs);
+taot_status taot_matmul_i8(const int8_t* x, const float* scale, const int8_t* weight, const float* weight_scale,
+                           const int32_t* offsets, const int32_t* experts, int64_t M, int32_t N, int32_t K, int32_t runs,
+                           int32_t G, int32_t dtype, void* out, void* ws, size_t ws_bytes, void* stream);
 
 /* ------------------------------------------------------------------------ */
 /* Host helper: topology-preference matrices from a cost matrix (Sec. A.3

@@ -13,8 +13,10 @@ plan_step chains them.
 Around them: add_rms_norm (residual addition, norm, 8-bit output) and route
 (logits to expert ids, which plan_loads reads, and weights) before; then
 dispatch_map (the schedule on the single copies), dispatch_rows and
-combine_rows (rows to the send buffer and back).  The *_backward calls are
-their gradients.  None of them is part of torch's graph: inputs whose gradient
+combine_rows (rows to the send buffer and back).  Beside them: block_norm (norms
+before and after a block with its gate and residual), balance_loss (the
+router's), and the experts' products of 8-bit integers, quantize_rows and
+matmul_i8.  The *_backward calls are their gradients.  None of them is part of torch's graph: inputs whose gradient
 is being recorded are refused.
 """
 from __future__ import annotations
@@ -90,6 +92,24 @@ def lib():
         L.taot_combine_rows.argtypes = [_P] * 3 + [_I64, _I64, _I32, _I32, _I32, _P, _P]
         L.taot_combine_rows_backward.restype = ctypes.c_int
         L.taot_combine_rows_backward.argtypes = [_P] * 4 + [_I64, _I64, _I32, _I32, _I32, _P, _P, _P]
+        L.taot_block_norm.restype = ctypes.c_int
+        L.taot_block_norm.argtypes = [_P] * 4 + [_I64, _P, _I64] + [_I32] * 4 + [_F32, _F32] + [_P] * 5
+        L.taot_block_norm_backward_workspace_size.restype = _SZ
+        L.taot_block_norm_backward_workspace_size.argtypes = [_I64, _I32, _I64]
+        L.taot_block_norm_backward.restype = ctypes.c_int
+        L.taot_block_norm_backward.argtypes = [_P] * 8 + [_I64, _P, _I64] + [_I32] * 4 + [_F32] + [_P] * 6 + [_SZ, _P]
+        L.taot_balance_loss_workspace_size.restype = _SZ
+        L.taot_balance_loss_workspace_size.argtypes = [_I64, _I64, _I32]
+        L.taot_balance_loss.restype = ctypes.c_int
+        L.taot_balance_loss.argtypes = [_P] * 3 + [_I64, _I64, _I32, _I32, _U32, _I32] + [_P] * 6 + [_SZ, _P]
+        L.taot_balance_loss_backward.restype = ctypes.c_int
+        L.taot_balance_loss_backward.argtypes = [_P] * 7 + [_I64, _I64, _I32, _U32, _I32, _P, _P]
+        L.taot_quantize_rows.restype = ctypes.c_int
+        L.taot_quantize_rows.argtypes = [_P, _I64, _I32, _I32, _I32, _P, _P, _P]
+        L.taot_matmul_i8_workspace_size.restype = _SZ
+        L.taot_matmul_i8_workspace_size.argtypes = [_I64, _I32]
+        L.taot_matmul_i8.restype = ctypes.c_int
+        L.taot_matmul_i8.argtypes = [_P] * 6 + [_I64] + [_I32] * 5 + [_P, _P, _SZ, _P]
         L.taot_topology_pref.restype = ctypes.c_int
         L.taot_topology_pref.argtypes = [_P, _I32, _P, _P]
         _lib = L
@@ -644,6 +664,275 @@ def combine_rows_backward(dout: torch.Tensor, y: torch.Tensor, pos: torch.Tensor
     _launch("taot_combine_rows_backward", y.device, stream,
         dout.data_ptr(), y.data_ptr(), pos.data_ptr(), weights.data_ptr(), rows, tokens, k, H, _DTYPE[y.dtype],
         out.dy.data_ptr(), out.dweights.data_ptr())
+    return out
+
+
+@dataclasses.dataclass
+class BlockNorm:
+    y: Optional[torch.Tensor] = None       # [..., H], x's type (None without weight)
+    h: Optional[torch.Tensor] = None       # [..., H], x's type: the new residual
+    rstd_x: Optional[torch.Tensor] = None  # [...] float32 (None without post)
+    rstd_h: Optional[torch.Tensor] = None  # [...] float32 (None without weight)
+
+
+def _gates(gate: Optional[torch.Tensor], x: torch.Tensor) -> int:
+    """The number of gates: gate is [H]; or [gates, H] for x [T, H], whose rows have one by equal runs; or [..., H] over
+    the first dimensions of x (those behind them may be there as 1)."""
+    if gate is None:
+        return 0
+    f32 = isinstance(gate, torch.Tensor) and gate.dtype == torch.float32
+    _rows(gate, "gate", None if f32 else x)
+    lead = list(gate.shape[:-1])
+    n = 1
+    for d in lead:
+        n *= d
+    T = x.numel() // x.shape[-1] if x.numel() else 0
+    while lead and lead[-1] == 1 and lead != list(x.shape[:len(lead)]):
+        lead.pop()
+    fits = len(lead) < x.dim() and lead == list(x.shape[:len(lead)])
+    if x.dim() == 2 and gate.dim() == 2 and n and T % n == 0:
+        fits = True
+    if not gate.dim() or gate.shape[-1] != x.shape[-1] or not fits:
+        raise ValueError(f"gate must be [H] or a gate for equal runs of x's rows, {tuple(x.shape)}, got {tuple(gate.shape)}")
+    return max(n, 1)
+
+
+def block_norm(x: torch.Tensor, residual: torch.Tensor, weight: Optional[torch.Tensor], eps: float,
+               post: Optional[torch.Tensor] = None, gate: Optional[torch.Tensor] = None, alpha: float = 1.0,
+               out: Optional[BlockNorm] = None, stream=None) -> BlockNorm:
+    """h = alpha * residual + gate * norm(x) * post, y = norm(h) * weight over the last dimension (taot_block_norm): x is
+    a block's output, h the new residual, y the next block's input.  post None: x without a norm; gate [H], or one for
+    equal runs of rows: [gates, H] for x [T, H], else [..., H] over the first of x's dimensions; weight None: no y.  Vectors are of x's type or
+    float32.  out: tensors to write to, or an earlier call's result."""
+    _rows(x, "x")
+    H = x.shape[-1] if x.dim() else 0
+    _shape(_rows(residual, "residual", x), "residual", x.shape)
+    wide = _vectors(x, H, weight=weight, post=post)
+    gates = _gates(gate, x)
+    _inputs("block_norm", "x residual weight post gate", stream, x, residual, weight, post, gate)
+    lead, dev = x.shape[:-1], x.device
+    o = out or BlockNorm()
+    h = _like(o.h, "out.h", x, stream)
+    y = rstd_h = rstd_x = None
+    if weight is not None:
+        y = _like(o.y, "out.y", x, stream)
+        rstd_h = _into(o.rstd_h, "out.rstd_h", lead, torch.float32, dev, stream)
+    if post is not None:
+        rstd_x = _into(o.rstd_x, "out.rstd_x", lead, torch.float32, dev, stream)
+    T = x.numel() // H if H else 0
+    _launch("taot_block_norm", dev, stream,
+        x.data_ptr(), residual.data_ptr(), _ptr(post), _ptr(gate), gates, _ptr(weight), T, H, _DTYPE[x.dtype], wide,
+        _DTYPE[x.dtype if gate is None else gate.dtype], float(eps), float(alpha), h.data_ptr(), _ptr(y), _ptr(rstd_x),
+        _ptr(rstd_h))
+    o.y, o.h, o.rstd_x, o.rstd_h = y, h, rstd_x, rstd_h
+    return o
+
+
+def _vectors(x: torch.Tensor, H: int, **vectors) -> int:
+    """Checks a norm's vectors [H], all of x's type or all float32; their type's number."""
+    kind = x.dtype
+    for i, (name, v) in enumerate((n, v) for n, v in vectors.items() if v is not None):
+        f32 = isinstance(v, torch.Tensor) and v.dtype == torch.float32
+        _shape(_rows(v, name, None if f32 else x), name, (H,))
+        if i and v.dtype != kind:
+            raise TypeError(f"{name} must be {kind} as the other vector, got {v.dtype}")
+        kind = v.dtype
+    return _DTYPE[kind]
+
+
+@dataclasses.dataclass
+class BlockNormGrad:
+    dx: Optional[torch.Tensor] = None         # [..., H], x's type
+    dresidual: Optional[torch.Tensor] = None  # [..., H], x's type
+    dweight: Optional[torch.Tensor] = None    # [H] float32
+    dpost: Optional[torch.Tensor] = None      # [H] float32
+    dgate: Optional[torch.Tensor] = None      # the gate's shape, float32
+
+
+def block_norm_backward(dy: Optional[torch.Tensor], x: torch.Tensor, h: Optional[torch.Tensor],
+                        rstd_h: Optional[torch.Tensor], weight: Optional[torch.Tensor],
+                        rstd_x: Optional[torch.Tensor] = None, post: Optional[torch.Tensor] = None,
+                        gate: Optional[torch.Tensor] = None, alpha: float = 1.0, dh: Optional[torch.Tensor] = None,
+                        out: Optional[BlockNormGrad] = None, workspace: Optional[torch.Tensor] = None,
+                        stream=None) -> BlockNormGrad:
+    """Gradient of block_norm (taot_block_norm_backward) from its x, h, rstd_x and rstd_h: dy reaches y, dh reaches h.
+    Without weight there are no dy, h and rstd_h, but dh."""
+    _rows(x, "x")
+    H = x.shape[-1] if x.dim() else 0
+    wide = _vectors(x, H, weight=weight, post=post)
+    gates = _gates(gate, x)
+    if weight is not None:
+        _shape(_rows(dy, "dy", x), "dy", x.shape)
+        _shape(_rows(h, "h", x), "h", x.shape)
+        _shape(_dev(rstd_h, "rstd_h", torch.float32), "rstd_h", x.shape[:-1])
+    elif dy is not None or h is not None or rstd_h is not None or dh is None:
+        raise ValueError("without weight there is no y: give dh, and no dy, h and rstd_h")
+    if post is not None:
+        _shape(_dev(rstd_x, "rstd_x", torch.float32), "rstd_x", x.shape[:-1])
+    elif rstd_x is not None:
+        raise ValueError("rstd_x goes with post")
+    if dh is not None:
+        _shape(_rows(dh, "dh", x), "dh", x.shape)
+    _inputs("block_norm_backward", "x dy h rstd_h weight rstd_x post gate dh", stream, x, dy, h, rstd_h, weight, rstd_x, post,
+            gate, dh)
+    dev = x.device
+    o = out or BlockNormGrad()
+    dx, dresidual = _like(o.dx, "out.dx", x, stream), _like(o.dresidual, "out.dresidual", x, stream)
+    dweight = None if weight is None else _into(o.dweight, "out.dweight", (H,), torch.float32, dev, stream)
+    dpost = None if post is None else _into(o.dpost, "out.dpost", (H,), torch.float32, dev, stream)
+    dgate = None if gate is None else _into(o.dgate, "out.dgate", gate.shape, torch.float32, dev, stream)
+    T = x.numel() // H if H else 0
+    ws = _room(workspace, lib().taot_block_norm_backward_workspace_size(T, H, gates), dev, stream)
+    _launch("taot_block_norm_backward", dev, stream,
+        _ptr(dy), _ptr(dh), x.data_ptr(), _ptr(h), _ptr(rstd_x), _ptr(rstd_h), _ptr(post), _ptr(gate), gates, _ptr(weight),
+        T, H, _DTYPE[x.dtype], wide, _DTYPE[x.dtype if gate is None else gate.dtype], float(alpha), dx.data_ptr(),
+        dresidual.data_ptr(), _ptr(dweight), _ptr(dpost), _ptr(dgate), ws.data_ptr(), ws.numel() * ws.element_size())
+    o.dx, o.dresidual, o.dweight, o.dpost, o.dgate = dx, dresidual, dweight, dpost, dgate
+    return o
+
+
+@dataclasses.dataclass
+class Balance:
+    loss: Optional[torch.Tensor] = None    # [...] float32
+    z: Optional[torch.Tensor] = None       # [...] float32 (None with ROUTE_SIGMOID)
+    counts: Optional[torch.Tensor] = None  # [..., E] int32 choices of each expert
+    prob: Optional[torch.Tensor] = None    # [..., E] float32 mean score of each expert
+    tokens: Optional[torch.Tensor] = None  # [...] int32 tokens that count
+
+
+def _set_of_tokens(logits: torch.Tensor, mask: Optional[torch.Tensor], flags: int):
+    """(lead, rows, tokens, E) of logits [..., tokens, E], whose mask [..., tokens] is of truth values or bytes."""
+    _rows(logits, "logits")
+    if logits.dim() < 2:
+        raise ValueError(f"logits must be [..., tokens, E], got {tuple(logits.shape)}")
+    if mask is not None:
+        u8 = isinstance(mask, torch.Tensor) and mask.dtype == torch.uint8
+        _shape(_dev(mask, "mask", torch.uint8 if u8 else torch.bool), "mask", logits.shape[:-1])
+    rows = 1
+    for d in logits.shape[:-2]:
+        rows *= d
+    return logits.shape[:-2], rows, logits.shape[-2], logits.shape[-1]
+
+
+def balance_loss(logits: torch.Tensor, ids: torch.Tensor, mask: Optional[torch.Tensor] = None, flags: int = 0,
+                 out: Optional[Balance] = None, workspace: Optional[torch.Tensor] = None, stream=None) -> Balance:
+    """The router's balance loss over each set of tokens of logits [..., tokens, E] with the choices ids [..., tokens, k]
+    (taot_balance_loss): E times the sum of each expert's share of the choices and its mean score, which is softmax's, or
+    with ROUTE_SIGMOID the share of its sigmoid; and z, the mean square of the logarithm of the sum of exponentials.
+    mask [..., tokens]: tokens that count."""
+    lead, rows, tokens, E = _set_of_tokens(logits, mask, flags)
+    k = _dev(ids, "ids", torch.int32).shape[-1] if isinstance(ids, torch.Tensor) and ids.dim() else 0
+    _shape(_dev(ids, "ids", torch.int32), "ids", (*logits.shape[:-1], k))
+    _inputs("balance_loss", "logits ids mask", stream, logits, ids, mask)
+    dev = logits.device
+    o = out or Balance()
+    loss = _into(o.loss, "out.loss", lead, torch.float32, dev, stream)
+    z = None if flags & ROUTE_SIGMOID else _into(o.z, "out.z", lead, torch.float32, dev, stream)
+    counts = _into(o.counts, "out.counts", (*lead, E), torch.int32, dev, stream)
+    prob = _into(o.prob, "out.prob", (*lead, E), torch.float32, dev, stream)
+    counted = _into(o.tokens, "out.tokens", lead, torch.int32, dev, stream)
+    ws = _room(workspace, lib().taot_balance_loss_workspace_size(rows, tokens, E), dev, stream)
+    _launch("taot_balance_loss", dev, stream,
+        logits.data_ptr(), ids.data_ptr(), _ptr(mask), rows, tokens, E, k, int(flags), _DTYPE[logits.dtype],
+        loss.data_ptr(), _ptr(z), counts.data_ptr(), prob.data_ptr(), counted.data_ptr(), ws.data_ptr(),
+        ws.numel() * ws.element_size())
+    o.loss, o.z, o.counts, o.prob, o.tokens = loss, z, counts, prob, counted
+    return o
+
+
+def balance_loss_backward(dloss: torch.Tensor, logits: torch.Tensor, counts: torch.Tensor, tokens: torch.Tensor,
+                          mask: Optional[torch.Tensor] = None, dz: Optional[torch.Tensor] = None,
+                          add: Optional[torch.Tensor] = None, flags: int = 0, out: Optional[torch.Tensor] = None,
+                          stream=None) -> torch.Tensor:
+    """Gradient of balance_loss by the logits (taot_balance_loss_backward): [..., tokens, E] of their type.  dloss and dz
+    [...] reach loss and z; counts may be those of more tokens (all ranks'), tokens are this call's; add: what reaches the
+    logits otherwise, such as route_backward's result."""
+    lead, rows, n, E = _set_of_tokens(logits, mask, flags)
+    _shape(_dev(dloss, "dloss", torch.float32), "dloss", lead)
+    _shape(_dev(counts, "counts", torch.int32), "counts", (*lead, E))
+    _shape(_dev(tokens, "tokens", torch.int32), "tokens", lead)
+    if dz is not None:
+        _shape(_dev(dz, "dz", torch.float32), "dz", lead)
+    if add is not None:
+        _shape(_rows(add, "add", logits), "add", logits.shape)
+    _inputs("balance_loss_backward", "logits dloss counts tokens mask dz add", stream, logits, dloss, counts, tokens, mask,
+            dz, add)
+    out = _like(out, "out", logits, stream)
+    _launch("taot_balance_loss_backward", logits.device, stream,
+        dloss.data_ptr(), _ptr(dz), logits.data_ptr(), counts.data_ptr(), tokens.data_ptr(), _ptr(mask), _ptr(add), rows, n,
+        E, int(flags), _DTYPE[logits.dtype], out.data_ptr())
+    return out
+
+
+@dataclasses.dataclass
+class Rows8:
+    q: Optional[torch.Tensor] = None      # [..., H] int8
+    scale: Optional[torch.Tensor] = None  # [..., 1] float32
+
+    def __iter__(self):
+        return iter((self.q, self.scale))
+
+
+def quantize_rows(x: torch.Tensor, gated: bool = False, out: Optional[Rows8] = None, stream=None) -> Rows8:
+    """Rows of x [..., H] as 8-bit integers with a scale each (taot_quantize_rows), what matmul_i8 takes and
+    dispatch_rows carries.  gated: x is [..., 2 H], and what is rounded is silu of its first half times its second."""
+    _rows(x, "x")
+    W = x.shape[-1] if x.dim() else 0
+    if gated and W % 2:
+        raise ValueError(f"gated rows have two halves, got {tuple(x.shape)}")
+    H = W // 2 if gated else W
+    _inputs("quantize_rows", "x", stream, x)
+    lead, dev = x.shape[:-1], x.device
+    o = out or Rows8()
+    q = _into(o.q, "out.q", (*lead, H), torch.int8, dev, stream)
+    scale = _into(o.scale, "out.scale", (*lead, 1), torch.float32, dev, stream)
+    _launch("taot_quantize_rows", dev, stream,
+        x.data_ptr(), x.numel() // W if W else 0, H, int(bool(gated)), _DTYPE[x.dtype], q.data_ptr(), scale.data_ptr())
+    o.q, o.scale = q, scale
+    return o
+
+
+def matmul_i8(x: torch.Tensor, scale: torch.Tensor, weight: torch.Tensor, weight_scale: torch.Tensor,
+              offsets: Optional[torch.Tensor] = None, experts: Optional[torch.Tensor] = None,
+              dtype: torch.dtype = torch.bfloat16, out: Optional[torch.Tensor] = None,
+              workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """Products of 8-bit integers with a scale for each row and channel (taot_matmul_i8).  x [..., K] int8 and a value of
+    scale for each row, as quantize_rows gives them.  weight [N, K] int8 and weight_scale [N]: one weight for all rows,
+    [..., N].  With offsets [runs + 1] int32, x is [M, K] and weight [G, N, K]: run i, rows offsets[i] to offsets[i + 1],
+    has weight experts[i] (None: i); rows of no run, or of an expert that is none, become zero.  For rows of several send
+    buffers, add each buffer's first row to its offsets and give an expert of -1 to the run behind its last."""
+    _dev(x, "x", torch.int8)
+    _dev(weight, "weight", torch.int8)
+    if dtype not in _DTYPE:
+        raise TypeError(f"dtype must be bfloat16, float16 or float32, got {dtype}")
+    grouped = offsets is not None
+    if not x.dim() or weight.dim() != (3 if grouped else 2) or (grouped and x.dim() != 2):
+        raise ValueError("x must be [..., K] and weight [N, K]; with offsets x [M, K] and weight [G, N, K]")
+    N, K = weight.shape[-2:]
+    lead, M = x.shape[:-1], x.numel() // K if K else 0
+    _shape(x, "x", (*lead, K))
+    _shape(_dev(weight_scale, "weight_scale", torch.float32), "weight_scale", weight.shape[:-1])
+    if _dev(scale, "scale", torch.float32).numel() != M:
+        raise ValueError("scale must have a value for each row of x")
+    runs, G = 0, 1
+    if grouped:
+        if _dev(offsets, "offsets", torch.int32).dim() != 1 or not offsets.numel():
+            raise ValueError("offsets must be [runs + 1]")
+        runs, G = offsets.numel() - 1, weight.shape[0]
+    if experts is not None:
+        if not grouped:
+            raise ValueError("experts go with offsets")
+        _shape(_dev(experts, "experts", torch.int32), "experts", (runs,))
+    elif grouped and runs != G:
+        raise ValueError(f"{runs} runs without experts need as many weights, got {G}")
+    _inputs("matmul_i8", "x scale weight weight_scale offsets experts", stream, x, scale, weight, weight_scale, offsets,
+            experts)
+    dev = x.device
+    out = _into(out, "out", (*lead, N), dtype, dev, stream)
+    ws = _room(workspace, lib().taot_matmul_i8_workspace_size(M, runs), dev, stream) if grouped else None
+    _launch("taot_matmul_i8", dev, stream,
+        x.data_ptr(), scale.data_ptr(), weight.data_ptr(), weight_scale.data_ptr(), _ptr(offsets), _ptr(experts), M, N, K,
+        runs, G, _DTYPE[dtype], out.data_ptr(), _ptr(ws), 0 if ws is None else ws.numel() * ws.element_size())
     return out
 
 

@@ -16,6 +16,9 @@ bool bad_weight_type(int32_t dtype, int32_t weight_dtype) {
   return bad_type(dtype) || (weight_dtype != dtype && weight_dtype != TAOT_F32);
 }
 
+// A gate's rows: `gates` of them divide the T rows.
+bool bad_gates(const void* gate, int64_t gates, int64_t T) { return gate && (gates < 1 || T % gates); }
+
 constexpr int64_t kMaxGrid = 0x7fffffffLL;  // rows that one launch can number
 constexpr int32_t kMaxWide = 1 << 30;       // columns whose steps 32 bits can count
 
@@ -262,6 +265,107 @@ taot_status taot_combine_rows_backward(const void* dout, const void* y, const in
   if (!dout || !y || !pos || !weights || !dy || !dweights) return TAOT_ERR_INVALID_ARG;
   return launch_combine_rows_backward(dout, y, pos, weights, rows, tokens, k, H, dtype, dy, dweights,
                                       static_cast<hipStream_t>(stream));
+}
+
+taot_status taot_block_norm(const void* x, const void* residual, const void* post, const void* gate, int64_t gates,
+                            const void* weight, int64_t T, int32_t H, int32_t dtype, int32_t weight_dtype,
+                            int32_t gate_dtype, float eps, float alpha, void* h, void* y, float* rstd_x, float* rstd_h,
+                            void* stream) {
+  if (T < 0 || H <= 0 || bad_weight_type(dtype, weight_dtype) || bad_weight_type(dtype, gate_dtype) || !(eps >= 0.f) ||
+      !isfinite(eps) || !isfinite(alpha) || bad_gates(gate, gates, T) || (y && !weight))
+    return TAOT_ERR_INVALID_ARG;
+  if (H > TAOT_MAX_WIDTH || T > kMaxGrid) return TAOT_ERR_UNSUPPORTED;
+  if (T == 0) return TAOT_OK;
+  if (!x || !residual || (weight && !y)) return TAOT_ERR_INVALID_ARG;
+  return launch_block_norm(BlockNormArgs{x, residual, post, gate, weight, T, gate ? gates : 1, H, weight_dtype == TAOT_F32,
+                                         gate_dtype == TAOT_F32, eps, alpha, h, y, rstd_x, rstd_h},
+                           dtype, static_cast<hipStream_t>(stream));
+}
+
+size_t taot_block_norm_backward_workspace_size(int64_t T, int32_t H, int64_t gates) {
+  if (T <= 0 || H <= 0 || gates < 0 || (gates > 0 && T % gates)) return 0;
+  return block_norm_backward_ws(T, H, gates > 0 ? gates : 1);
+}
+
+taot_status taot_block_norm_backward(const void* dy, const void* dh, const void* x, const void* h, const float* rstd_x,
+                                     const float* rstd_h, const void* post, const void* gate, int64_t gates,
+                                     const void* weight, int64_t T, int32_t H, int32_t dtype, int32_t weight_dtype,
+                                     int32_t gate_dtype, float alpha, void* dx, void* dresidual, float* dweight,
+                                     float* dpost, float* dgate, void* ws, size_t ws_bytes, void* stream) {
+  if (T < 0 || H <= 0 || bad_weight_type(dtype, weight_dtype) || bad_weight_type(dtype, gate_dtype) || !isfinite(alpha) ||
+      bad_gates(gate, gates, T) || (dweight && !weight) || (dpost && !post) || (dgate && !gate))
+    return TAOT_ERR_INVALID_ARG;
+  if (H > TAOT_MAX_WIDTH || T > kMaxGrid) return TAOT_ERR_UNSUPPORTED;
+  if (T > 0 && (!x || !dx || !dresidual || (weight && (!dy || !h || !rstd_h)) || (!weight && !dh) || (post && !rstd_x)))
+    return TAOT_ERR_INVALID_ARG;
+  const int64_t sets = gate ? gates : 1;
+  if (T > 0 && (!ws || ws_bytes < block_norm_backward_ws(T, H, sets))) return TAOT_ERR_WORKSPACE;
+  return launch_block_norm_backward(
+      BlockNormGradArgs{dy, dh, x, h, rstd_x, rstd_h, post, gate, weight, T, sets, H, weight_dtype == TAOT_F32,
+                        gate_dtype == TAOT_F32, alpha, dx, dresidual, dweight, dpost, dgate},
+      dtype, ws, static_cast<hipStream_t>(stream));
+}
+
+size_t taot_balance_loss_workspace_size(int64_t rows, int64_t tokens, int32_t E) {
+  if (rows <= 0 || tokens < 0 || E <= 0) return 0;
+  return balance_loss_ws(rows, tokens, E);
+}
+
+taot_status taot_balance_loss(const void* logits, const int32_t* ids, const uint8_t* mask, int64_t rows, int64_t tokens,
+                              int32_t E, int32_t k, uint32_t flags, int32_t dtype, float* loss, float* z,
+                              int32_t* counts, float* prob, int32_t* counted, void* ws, size_t ws_bytes, void* stream) {
+  int64_t n = 0;
+  if (E <= 0 || bad_type(dtype) || (flags & ~TAOT_ROUTE_SIGMOID) || (z && (flags & TAOT_ROUTE_SIGMOID)))
+    return TAOT_ERR_INVALID_ARG;
+  if (taot_status s = check_rows(rows, tokens, k, &n)) return s;
+  if (E > TAOT_MAX_EXPERTS || rows > kMaxGrid || (n > 0 && rows > kMaxGrid / n)) return TAOT_ERR_UNSUPPORTED;
+  if (rows == 0) return TAOT_OK;
+  if ((tokens > 0 && (!logits || !ids)) || !loss || !counts || !prob) return TAOT_ERR_INVALID_ARG;
+  if (!ws || ws_bytes < balance_loss_ws(rows, tokens, E)) return TAOT_ERR_WORKSPACE;
+  return launch_balance_loss(logits, ids, mask, rows, tokens, E, k, flags, dtype, loss, z, counts, prob, counted, ws,
+                             static_cast<hipStream_t>(stream));
+}
+
+taot_status taot_balance_loss_backward(const float* dloss, const float* dz, const void* logits, const int32_t* counts,
+                                       const int32_t* counted, const uint8_t* mask, const void* add, int64_t rows,
+                                       int64_t tokens, int32_t E, uint32_t flags, int32_t dtype, void* dlogits,
+                                       void* stream) {
+  int64_t n = 0;
+  if (E <= 0 || bad_type(dtype) || (flags & ~TAOT_ROUTE_SIGMOID) || (dz && (flags & TAOT_ROUTE_SIGMOID)))
+    return TAOT_ERR_INVALID_ARG;
+  if (taot_status s = check_rows(rows, tokens, 1, &n)) return s;
+  if (E > TAOT_MAX_EXPERTS) return TAOT_ERR_UNSUPPORTED;
+  if (rows == 0 || tokens == 0) return TAOT_OK;
+  if (!dloss || !logits || !counts || !counted || !dlogits) return TAOT_ERR_INVALID_ARG;
+  return launch_balance_loss_backward(dloss, dz, logits, counts, counted, mask, add, rows, tokens, E, flags, dtype, dlogits,
+                                      static_cast<hipStream_t>(stream));
+}
+
+taot_status taot_quantize_rows(const void* x, int64_t T, int32_t H, int32_t gated, int32_t dtype, int8_t* q,
+                               float* scale, void* stream) {
+  if (T < 0 || H <= 0 || bad_type(dtype) || (gated != 0 && gated != 1)) return TAOT_ERR_INVALID_ARG;
+  if (H > TAOT_MAX_WIDTH || T > kMaxGrid) return TAOT_ERR_UNSUPPORTED;
+  if (T == 0) return TAOT_OK;
+  if (!x || !q || !scale) return TAOT_ERR_INVALID_ARG;
+  return launch_quantize_rows(x, T, H, gated != 0, dtype, q, scale, static_cast<hipStream_t>(stream));
+}
+
+size_t taot_matmul_i8_workspace_size(int64_t M, int32_t runs) {
+  if (M < 0 || runs < 0 || M > kMaxWide || runs > kMaxWide) return 0;
+  return matmul_i8_ws(M, runs);
+}
+
+taot_status taot_matmul_i8(const int8_t* x, const float* scale, const int8_t* weight, const float* weight_scale,
+                           const int32_t* offsets, const int32_t* experts, int64_t M, int32_t N, int32_t K, int32_t runs,
+                           int32_t G, int32_t dtype, void* out, void* ws, size_t ws_bytes, void* stream) {
+  if (M < 0 || N <= 0 || K <= 0 || runs < 0 || G <= 0 || bad_type(dtype) || (!offsets && (runs != 0 || G != 1 || experts)))
+    return TAOT_ERR_INVALID_ARG;
+  if (K > TAOT_MAX_INNER || M > kMaxWide || N > kMaxWide || runs > kMaxWide) return TAOT_ERR_UNSUPPORTED;
+  if (M == 0) return TAOT_OK;
+  if (!x || !scale || !weight || !weight_scale || !out) return TAOT_ERR_INVALID_ARG;
+  if (offsets && (!ws || ws_bytes < matmul_i8_ws(M, runs))) return TAOT_ERR_WORKSPACE;
+  return launch_matmul_i8(ProductArgs{x, scale, weight, weight_scale, offsets, experts, M, N, K, runs, G, out}, dtype, ws,
+                          static_cast<hipStream_t>(stream));
 }
 
 taot_status taot_topology_pref(const float* C_host, int32_t R, double* Bpref_host,

@@ -129,4 +129,53 @@ taot_status launch_combine_rows_backward(const void* dout, const void* y, const 
                                          int64_t rows, int64_t tokens, int32_t k, int32_t H, int32_t dtype, void* dy,
                                          float* dweights, hipStream_t stream);
 
+struct BlockNormArgs {
+  const void *x, *residual, *post, *gate, *weight;
+  int64_t rows, gates;
+  int32_t H;
+  bool weight_f32, gate_f32;
+  float eps, alpha;
+  void *h, *y;
+  float *rstd_x, *rstd_h;
+};
+struct BlockNormGradArgs {
+  const void *dy, *dh, *x, *h;
+  const float *rstd_x, *rstd_h;
+  const void *post, *gate, *weight;
+  int64_t rows, gates;
+  int32_t H;
+  bool weight_f32, gate_f32;
+  float alpha;
+  void *dx, *dresidual;
+  float *dweight, *dpost, *dgate;
+};
+taot_status launch_block_norm(const BlockNormArgs& a, int32_t dtype, hipStream_t stream);
+taot_status launch_block_norm_backward(const BlockNormGradArgs& a, int32_t dtype, void* ws, hipStream_t stream);
+size_t block_norm_backward_ws(int64_t rows, int32_t H, int64_t gates);
+
+taot_status launch_balance_loss(const void* logits, const int32_t* ids, const uint8_t* mask, int64_t rows,
+                                int64_t tokens, int32_t E, int32_t k, uint32_t flags, int32_t dtype, float* loss,
+                                float* z, int32_t* counts, float* prob, int32_t* counted, void* ws, hipStream_t stream);
+size_t balance_loss_ws(int64_t rows, int64_t tokens, int32_t E);
+taot_status launch_balance_loss_backward(const float* dloss, const float* dz, const void* logits, const int32_t* counts,
+                                         const int32_t* counted, const uint8_t* mask, const void* add, int64_t rows,
+                                         int64_t tokens, int32_t E, uint32_t flags, int32_t dtype, void* dlogits,
+                                         hipStream_t stream);
+
+taot_status launch_quantize_rows(const void* x, int64_t rows, int32_t H, bool gated, int32_t dtype, int8_t* q,
+                                 float* scale, hipStream_t stream);
+
+struct ProductArgs {
+  const int8_t* x;
+  const float* scale;
+  const int8_t* weight;
+  const float* weight_scale;
+  const int32_t *offsets, *experts;
+  int64_t M;
+  int32_t N, K, runs, G;
+  void* out;
+};
+taot_status launch_matmul_i8(const ProductArgs& a, int32_t dtype, void* ws, hipStream_t stream);
+size_t matmul_i8_ws(int64_t M, int32_t runs);
+
 }  // namespace taot

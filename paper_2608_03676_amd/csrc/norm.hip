@@ -16,7 +16,6 @@ namespace {
 
 constexpr float kF8Max = 448.f;       // largest finite e4m3 value
 constexpr float kF8Floor = 1e-30f;    // a group of smaller values (all zero) has floor / 448 as its scale
-constexpr int kRowsOfBlock = 4;       // where a wave holds a row
 
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef __attribute__((aligned(1))) u32x2 u32x2_at;
@@ -44,20 +43,6 @@ __device__ __forceinline__ void store_f8(uint8_t* p, u32x2 v, int n) {
 #pragma unroll
   for (int u = 0; u < 8; ++u)
     if (u < n) p[u] = (uint8_t)(v[u / 4] >> (8 * (u % 4)));
-}
-
-// Sum (or maximum) over the `waves` waves of a row.  `slot` alternates between
-// two sets of words from call to call, so one barrier a call is enough.
-template <typename Op>
-__device__ __forceinline__ float row_reduce(float v, Op op, float (*part)[16], int slot, int waves) {
-  v = block_reduce<kWave>(v, op);
-  if (waves > 1) {
-    if ((threadIdx.x & (kWave - 1)) == 0) part[slot][threadIdx.x / kWave] = v;
-    __syncthreads();
-    v = part[slot][0];
-    for (int w = 1; w < waves; ++w) v = op(v, part[slot][w]);
-  }
-  return v;
 }
 
 // `waves` waves hold a row (one: four rows a block); of their lanes, lane l has
@@ -268,14 +253,6 @@ int32_t backward_workers(int64_t rows, int32_t H) {
   if (blocks * s.waves > (s.cpl == 1 ? 24 : 16)) --blocks;
   const int64_t most = 256 * blocks;
   return (int32_t)(rows < most ? rows : most);
-}
-
-template <typename F>
-bool with_chunks(int cpl, F f) {
-  if (cpl == 1) return f(std::integral_constant<int, 1>());
-  if (cpl == 2) return f(std::integral_constant<int, 2>());
-  if (cpl == 4) return f(std::integral_constant<int, 4>());
-  return false;
 }
 
 template <typename T>

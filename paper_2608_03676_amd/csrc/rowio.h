@@ -143,4 +143,30 @@ __device__ __forceinline__ float block_max(float v, int lanes) {
   return v;
 }
 
+// ---- rows held by waves -------------------------------------------------------
+constexpr int kRowsOfBlock = 4;  // where a wave holds a row
+
+// Sum (or maximum) over the `waves` waves of a row.  `slot` alternates between
+// two sets of words from call to call, so one barrier a call is enough.
+template <typename Op>
+__device__ __forceinline__ float row_reduce(float v, Op op, float (*part)[16], int slot, int waves) {
+  v = block_reduce<kWave>(v, op);
+  if (waves > 1) {
+    if ((threadIdx.x & (kWave - 1)) == 0) part[slot][threadIdx.x / kWave] = v;
+    __syncthreads();
+    v = part[slot][0];
+    for (int w = 1; w < waves; ++w) v = op(v, part[slot][w]);
+  }
+  return v;
+}
+
+// f by the number of chunks of eight columns that a lane holds.
+template <typename F>
+bool with_chunks(int cpl, F f) {
+  if (cpl == 1) return f(std::integral_constant<int, 1>());
+  if (cpl == 2) return f(std::integral_constant<int, 2>());
+  if (cpl == 4) return f(std::integral_constant<int, 4>());
+  return false;
+}
+
 }  // namespace taot
