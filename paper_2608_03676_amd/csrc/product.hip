@@ -17,6 +17,8 @@ namespace {
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef int i32x16 __attribute__((ext_vector_type(16)));
 typedef __attribute__((aligned(1))) i32x4 i32x4_at;
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((aligned(4))) f32x4 f32x4_at;
 
 // Rows of one run, or (expert < 0) rows that no expert has and that become zero.
 struct Tile {
@@ -93,6 +95,15 @@ __device__ __forceinline__ i32x4 bytes16(const int8_t* __restrict__ row, int32_t
   return v;
 }
 
+// A sum with its scales, rounded to a float: without the empty statement the last
+// product and the rounding to 16 bits become one instruction in some kernels and not in
+// others, and the same call has other bits where its operands begin elsewhere.
+__device__ __forceinline__ float scaled(int sum, float row, float channel) {
+  float v = (float)sum * row * channel;
+  asm("" : "+v"(v));
+  return v;
+}
+
 // Four neighbouring channels of a row.
 template <typename T>
 __device__ __forceinline__ void store4(T* p, const float (&v)[4], int n) {
@@ -115,10 +126,42 @@ struct Work {
   const int32_t* total;
 };
 __device__ __forceinline__ Tile tile_of(const Work& w, int32_t i, int64_t M, int32_t rows_of_tile) {
-  if (w.tiles) return w.tiles[i];
+  if (w.tiles) {
+    const Tile t = w.tiles[i];  // the same for all lanes
+    return Tile{__builtin_amdgcn_readfirstlane(t.row), __builtin_amdgcn_readfirstlane(t.rows),
+                __builtin_amdgcn_readfirstlane(t.expert), 0};
+  }
   const int64_t row = (int64_t)i * rows_of_tile;
   return Tile{(int32_t)row, (int32_t)min((int64_t)rows_of_tile, M - row), 0, 0};
 }
+
+// Which tiles a block works on, and in which order.  Blocks go to the eight dies in
+// turn; a die gets a contiguous part of the tiles, in groups of kGroup tiles of rows
+// by all channels, so that what its blocks read at a time is near a square and is
+// found in its L2 cache.
+constexpr int kDies = 8, kGroup = 4;
+struct Walk {
+  int64_t all, at, end, step;  // all tiles by channels, and the block's part of them
+  int32_t across, tiles;
+  __device__ __forceinline__ Walk(const Work& w, int32_t most, int32_t N, int bn) {
+    across = (N + bn - 1) / bn;
+    tiles = w.tiles ? __builtin_amdgcn_readfirstlane(min(*w.total, most)) : most;
+    all = (int64_t)tiles * across;
+    const int64_t per = (all + kDies - 1) / kDies, die = blockIdx.x % kDies;
+    at = die * per + blockIdx.x / kDies;
+    end = min(die * per + per, all);
+    step = gridDim.x / kDies;
+  }
+  __device__ __forceinline__ bool more() const { return at < end; }
+  // The tile of rows and the tile of channels.
+  __device__ __forceinline__ int32_t place(int32_t& channels) const {
+    const int64_t group = at / (kGroup * (int64_t)across);
+    const int32_t in = (int32_t)(at - group * kGroup * across), first = (int32_t)group * kGroup;
+    const int32_t rows = min(kGroup, tiles - first);
+    channels = in / rows;
+    return first + in % rows;
+  }
+};
 
 // BN channels by BM rows of a tile, by WN x WM waves; kStep bytes of the inner
 // dimension at a time, the next ones on their way in registers while the present
@@ -133,12 +176,11 @@ product_kernel(ProductArgs p, Work work, int32_t most) {
   extern __shared__ i32x4 room[];
   const int tid = threadIdx.x, lane = tid % kWave, wid = tid / kWave;
   const int wn = wid % WN * (BN / WN), wm = wid / WN * (BM / WM);
-  const int32_t across = (p.N + BN - 1) / BN;
-  const int64_t all = (int64_t)(work.tiles ? min(*work.total, most) : most) * across;
   T* const out = static_cast<T*>(p.out);
-  for (int64_t at = blockIdx.x; at < all; at += gridDim.x) {
-    const Tile t = tile_of(work, (int32_t)(at / across), p.M, BM);
-    const int32_t n0 = (int32_t)(at % across) * BN;
+  for (Walk walk(work, most, p.N, BN); walk.more(); walk.at += walk.step) {
+    int32_t channels;
+    const Tile t = tile_of(work, walk.place(channels), p.M, BM);
+    const int32_t n0 = channels * BN;
     if (t.expert < 0) {
       const int32_t wide = min(BN, p.N - n0);
       for (int32_t i = tid; i < t.rows * BN; i += kThreads)
@@ -224,8 +266,177 @@ product_kernel(ProductArgs p, Work work, int32_t most) {
           if (n >= p.N) continue;
           float v[4];
 #pragma unroll
-          for (int u = 0; u < 4; ++u) v[u] = (float)acc[i][j][4 * q + u] * sx * sw[min(n + u, p.N - 1)];
+          for (int u = 0; u < 4; ++u) v[u] = scaled(acc[i][j][4 * q + u], sx, sw[min(n + u, p.N - 1)]);
           store4(to + n, v, p.N - n);
+        }
+    }
+  }
+}
+
+// 16 neighbouring channels of a row, of which the lane has 4 half .. + 3 and 8 + 4 half
+// .. + 3 and the lane 32 further the others.  16-bit values change lanes first, so
+// that a lane writes 16 bytes.
+template <typename T>
+__device__ __forceinline__ void store16(T* p, const float (&v)[2][4], int half, bool in) {
+  if constexpr (sizeof(T) == 4) {
+    if (!in) return;
+    store4(p + 4 * half, v[0], 4);
+    store4(p + 8 + 4 * half, v[1], 4);
+  } else {
+    typedef T two __attribute__((ext_vector_type(2)));
+    typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+    typedef __attribute__((aligned(2))) u32x4 u32x4_at;
+    u32x4 r;
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const uint32_t x = __builtin_bit_cast(uint32_t, two{(T)v[0][2 * u], (T)v[0][2 * u + 1]});
+      const uint32_t y = __builtin_bit_cast(uint32_t, two{(T)v[1][2 * u], (T)v[1][2 * u + 1]});
+      const auto s = __builtin_amdgcn_permlane32_swap(x, y, false, false);
+      r[u] = s[0];
+      r[2 + u] = s[1];
+    }
+    if (in) *reinterpret_cast<u32x4_at*>(p + 8 * half) = r;
+  }
+}
+
+// Many rows, whole 16-byte pieces: a wave on each SIMD holds 128 x 128 results, and
+// pieces go from memory to LDS without passing through registers.  The operands of
+// the next 32 bytes are read out of LDS while the present ones are multiplied, and
+// those of the next step's first 32 before the present step's last are.
+constexpr int kWideN = 256, kWideM = 256, kWideThreads = 256;
+constexpr int kRawBuffer = 0x00027000;  // a buffer's description: untyped, checked by bytes
+constexpr int kAllLoads = 0x0F70;       // waits for memory alone
+
+typedef __attribute__((address_space(3))) void LdsPlace;
+
+template <typename T>
+__global__ void __launch_bounds__(kWideThreads) __attribute__((amdgpu_waves_per_eu(1, 1)))
+product_wide_kernel(ProductArgs p, Work work, int32_t most) {
+  constexpr int kPieces = kStep / 16, kWaves = kWideThreads / kWave, kLoads = (kWideN + kWideM) * kPieces / kWideThreads;
+  __shared__ i32x4 even[(kWideN + kWideM) * kPieces], odd[(kWideN + kWideM) * kPieces];
+  const int tid = threadIdx.x, lane = tid % kWave, wid = __builtin_amdgcn_readfirstlane(tid / kWave);
+  const int wn = wid % 2 * 128, wm = wid / 2 * 128;
+  T* const out = static_cast<T*>(p.out);
+  // where this lane's operands lie in a step's room
+  int at_n[4], at_m[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    at_n[i] = (wn + 32 * i + lane % 32) * kPieces;
+    at_m[i] = (kWideN + wm + 32 * i + lane % 32) * kPieces;
+  }
+  const int turn = lane % kPieces;  // of the row's pieces
+  for (Walk walk(work, most, p.N, kWideN); walk.more(); walk.at += walk.step) {
+    int32_t channels;
+    const Tile t = tile_of(work, walk.place(channels), p.M, kWideM);
+    const int32_t n0 = channels * kWideN;
+    if (t.expert < 0) {
+      const int32_t wide = min(kWideN, p.N - n0);
+      for (int32_t i = tid; i < t.rows * kWideN; i += kWideThreads)
+        if (i % kWideN < wide) out[(int64_t)(t.row + i / kWideN) * p.N + n0 + i % kWideN] = (T)0.f;
+      continue;
+    }
+    // A wave brings eight rows at a time, a lane the piece whose place is its own.  Rows and pieces behind the ends are
+    // out of the buffers' ranges, and come as zeros.
+    const int own = 16 * ((lane % kPieces) ^ (lane / kPieces));
+    const uint32_t first = (uint32_t)((wid * 8 + lane / kPieces) * p.K + own);
+    const auto rows_n = __builtin_amdgcn_make_buffer_rsrc(
+        const_cast<int8_t*>(p.weight) + ((int64_t)t.expert * p.N + n0) * p.K, 0, min(kWideN, p.N - n0) * p.K, kRawBuffer);
+    const auto rows_m =
+        __builtin_amdgcn_make_buffer_rsrc(const_cast<int8_t*>(p.x) + (int64_t)t.row * p.K, 0, t.rows * p.K, kRawBuffer);
+    auto offset = [&](int32_t k) { return k + own < p.K ? first + (uint32_t)k : 0x80000000u; };
+    auto bring = [&](uint32_t from, i32x4* to, int i) {
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(i < kLoads / 2 ? rows_n : rows_m,
+                                               (LdsPlace*)(to + (i * kWaves + wid) * kWave), 16,
+                                               from + (uint32_t)(i % (kLoads / 2) * kWaves * 8 * p.K), 0, 0, 0);
+    };
+    i32x4 a[2][4], b[2][4];
+    auto take = [&](const i32x4* lds, int s, int into, int i) {
+      const int c = (2 * s + lane / 32) ^ turn;
+      if (i % 2 == 0) b[into][i / 2] = lds[at_m[i / 2] + c];
+      else a[into][i / 2] = lds[at_n[i / 2] + c];
+    };
+    i32x16 acc[4][4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) acc[i][j] = 0;
+    // 16 products; `also` comes before each, so that what it starts runs beside them
+    auto multiply = [&](int from, auto also) {
+#pragma unroll
+      for (int n = 0; n < 16; ++n) {
+        also(n);
+        acc[n / 4][n % 4] =
+            __builtin_amdgcn_mfma_i32_32x32x32_i8(a[from][n / 4], b[from][n % 4], acc[n / 4][n % 4], 0, 0, 0);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    };
+    auto step = [&](int32_t k, i32x4* here, i32x4* next) {
+#pragma unroll
+      for (int s = 0; s < 3; ++s)
+        multiply(s % 2, [&](int n) {
+          if (n % 2 == 0) take(here, s + 1, (s + 1) % 2, n / 2);
+          if (s == 0 && n % 2 == 1) bring(offset(k + kStep), next, kLoads / 2 + n / 2);
+        });
+      __builtin_amdgcn_s_waitcnt(kAllLoads);
+      __syncthreads();  // the next step's pieces are there, and nothing reads this one's any more
+      multiply(1, [&](int n) {
+        if (n % 2 == 0) take(next, 0, 0, n / 2);
+        else bring(offset(k + 2 * kStep), here, n / 2);
+      });
+    };
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) bring(offset(0), even, i);
+#pragma unroll
+    for (int i = 0; i < kLoads / 2; ++i) bring(offset(kStep), odd, i);
+    __builtin_amdgcn_s_waitcnt(kAllLoads);
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 8; ++i) take(even, 0, 0, i);
+    int32_t k = 0;
+    for (; k + kStep < p.K; k += 2 * kStep) {
+      step(k, even, odd);
+      step(k + kStep, odd, even);
+    }
+    if (k < p.K) step(k, even, odd);
+    __builtin_amdgcn_s_waitcnt(kAllLoads);  // what was brought last is of no use, but on its way
+    // the scales of this lane's channels and rows
+    const float* const sw = p.weight_scale + (int64_t)t.expert * p.N;
+    const bool whole = n0 + kWideN <= p.N;
+    f32x4 sn[4][4];
+    float sm[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const int32_t n = n0 + wn + 32 * i + 8 * q + 4 * (lane / 32);
+        if (whole) {
+          sn[i][q] = *reinterpret_cast<const f32x4_at*>(sw + n);
+        } else {
+#pragma unroll
+          for (int u = 0; u < 4; ++u) sn[i][q][u] = sw[min(n + u, p.N - 1)];
+        }
+      }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) sm[j] = p.scale[t.row + min(wm + 32 * j + lane % 32, t.rows - 1)];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int m = wm + 32 * j + lane % 32;
+      T* const to = out + (int64_t)(t.row + m) * p.N;
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int q = 0; q < 4; q += 2) {
+          float v[2][4];
+#pragma unroll
+          for (int u = 0; u < 8; ++u) v[u / 4][u % 4] = scaled(acc[i][j][4 * q + u], sm[j], sn[i][q + u / 4][u % 4]);
+          const int32_t n = n0 + wn + 32 * i + 8 * q;
+          if (whole) {
+            store16(to + n, v, lane / 32, m < t.rows);
+          } else if (m < t.rows) {
+            const int32_t at = n + 4 * (lane / 32);
+            if (at < p.N) store4(to + at, v[0], p.N - at);
+            if (at + 8 < p.N) store4(to + at + 8, v[1], p.N - at - 8);
+          }
         }
     }
   }
@@ -287,7 +498,7 @@ product_few_kernel(ProductArgs p, Work work, int32_t most) {
         float v[4];
 #pragma unroll
         for (int u = 0; u < 4; ++u)
-          v[u] = t.expert >= 0 ? (float)acc[u] * sx * p.weight_scale[(int64_t)t.expert * p.N + min(n + u, p.N - 1)] : 0.f;
+          v[u] = t.expert >= 0 ? scaled(acc[u], sx, p.weight_scale[(int64_t)t.expert * p.N + min(n + u, p.N - 1)]) : 0.f;
         store4(out + (int64_t)(t.row + m) * p.N + n, v, p.N - n);
       }
     }
@@ -322,16 +533,18 @@ taot_status product(const ProductArgs& p, void* ws, hipStream_t stream) {
     runs_kernel<<<1, kRunThreads, 0, stream>>>(p.offsets, p.experts, p.runs, p.G, p.M, rows, tiles, total);
     work = Work{tiles, total};
   }
-  auto go = [&](auto* kernel, int bn, int bm, int threads, size_t lds) {
+  auto go = [&](auto* kernel, int bn, int threads, size_t lds) {
     if (!allow_lds(reinterpret_cast<const void*>(kernel), lds)) return false;
-    const int64_t blocks = most * ((p.N + bn - 1) / bn);
+    const int64_t blocks = round_up(most * ((p.N + bn - 1) / bn), kDies);
     kernel<<<(unsigned)(blocks < kMaxBlocks ? blocks : kMaxBlocks), threads, lds, stream>>>(p, work, (int32_t)most);
     return true;
   };
   bool ok;
-  if (kind == kFew) ok = go(product_few_kernel<T>, 16, kFewRows, kWave * kFewWaves, 0);
-  else if (kind == kMiddle) ok = go(product_kernel<T, 128, 64, 2, 2>, 128, 64, 256, 2 * (128 + 64) * kStep);
-  else ok = go(product_kernel<T, 256, 256, 2, 4>, 256, 256, 512, 2 * (256 + 256) * kStep);
+  if (kind == kFew) ok = go(product_few_kernel<T>, 16, kWave * kFewWaves, 0);
+  else if (kind == kMiddle) ok = go(product_kernel<T, 128, 64, 2, 2>, 128, 256, 2 * (128 + 64) * kStep);
+  else if (p.K % 16 == 0 && reinterpret_cast<uintptr_t>(p.x) % 16 == 0 && reinterpret_cast<uintptr_t>(p.weight) % 16 == 0)
+    ok = go(product_wide_kernel<T>, kWideN, kWideThreads, 0);
+  else ok = go(product_kernel<T, 256, 256, 2, 4>, 256, 512, 2 * (256 + 256) * kStep);
   return ok && hipGetLastError() == hipSuccess ? TAOT_OK : TAOT_ERR_LAUNCH;
 }
 
