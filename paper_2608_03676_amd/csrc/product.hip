@@ -139,7 +139,7 @@ __device__ __forceinline__ Tile tile_of(const Work& w, int32_t i, int64_t M, int
 // turn; a die gets a contiguous part of the tiles, in groups of kGroup tiles of rows
 // by all channels, so that what its blocks read at a time is near a square and is
 // found in its L2 cache.
-constexpr int kDies = 8, kGroup = 4;
+constexpr int kDies = 8, kGroup = 4, kUnits = 256;  // compute units
 struct Walk {
   int64_t all, at, end, step;  // all tiles by channels, and the block's part of them
   int32_t across, tiles;
@@ -308,6 +308,7 @@ constexpr int kRawBuffer = 0x00027000;  // a buffer's description: untyped, chec
 constexpr int kAllLoads = 0x0F70;       // waits for memory alone
 
 typedef __attribute__((address_space(3))) void LdsPlace;
+typedef __amdgpu_buffer_rsrc_t Buffer;
 
 template <typename T>
 __global__ void __launch_bounds__(kWideThreads) __attribute__((amdgpu_waves_per_eu(1, 1)))
@@ -325,30 +326,51 @@ product_wide_kernel(ProductArgs p, Work work, int32_t most) {
     at_m[i] = (kWideN + wm + 32 * i + lane % 32) * kPieces;
   }
   const int turn = lane % kPieces;  // of the row's pieces
-  for (Walk walk(work, most, p.N, kWideN); walk.more(); walk.at += walk.step) {
+  auto bring = [&](Buffer rows_n, Buffer rows_m, uint32_t from, i32x4* to, int i) {
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(i < kLoads / 2 ? rows_n : rows_m,
+                                             (LdsPlace*)(to + (i * kWaves + wid) * kWave), 16,
+                                             from + (uint32_t)(i % (kLoads / 2) * kWaves * 8 * p.K), 0, 0, 0);
+  };
+  // A wave brings eight rows at a time, a lane the piece whose place is its own.  Rows and pieces behind the ends are
+  // out of the buffers' ranges, and come as zeros.
+  const int own = 16 * ((lane % kPieces) ^ (lane / kPieces));
+  const uint32_t first = (uint32_t)((wid * 8 + lane / kPieces) * p.K + own);
+  auto offset = [&](int32_t k) { return k + own < p.K ? first + (uint32_t)k : 0x80000000u; };
+  Walk walk(work, most, p.N, kWideN);
+  if (!walk.more()) return;
+  auto look = [&](int32_t& n0) {
     int32_t channels;
     const Tile t = tile_of(work, walk.place(channels), p.M, kWideM);
-    const int32_t n0 = channels * kWideN;
-    if (t.expert < 0) {
-      const int32_t wide = min(kWideN, p.N - n0);
-      for (int32_t i = tid; i < t.rows * kWideN; i += kWideThreads)
-        if (i % kWideN < wide) out[(int64_t)(t.row + i / kWideN) * p.N + n0 + i % kWideN] = (T)0.f;
-      continue;
-    }
-    // A wave brings eight rows at a time, a lane the piece whose place is its own.  Rows and pieces behind the ends are
-    // out of the buffers' ranges, and come as zeros.
-    const int own = 16 * ((lane % kPieces) ^ (lane / kPieces));
-    const uint32_t first = (uint32_t)((wid * 8 + lane / kPieces) * p.K + own);
-    const auto rows_n = __builtin_amdgcn_make_buffer_rsrc(
-        const_cast<int8_t*>(p.weight) + ((int64_t)t.expert * p.N + n0) * p.K, 0, min(kWideN, p.N - n0) * p.K, kRawBuffer);
-    const auto rows_m =
-        __builtin_amdgcn_make_buffer_rsrc(const_cast<int8_t*>(p.x) + (int64_t)t.row * p.K, 0, t.rows * p.K, kRawBuffer);
-    auto offset = [&](int32_t k) { return k + own < p.K ? first + (uint32_t)k : 0x80000000u; };
-    auto bring = [&](uint32_t from, i32x4* to, int i) {
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(i < kLoads / 2 ? rows_n : rows_m,
-                                               (LdsPlace*)(to + (i * kWaves + wid) * kWave), 16,
-                                               from + (uint32_t)(i % (kLoads / 2) * kWaves * 8 * p.K), 0, 0, 0);
-    };
+    n0 = channels * kWideN;
+    return t;
+  };
+  auto buffer_n = [&](const Tile& t, int32_t n0) {
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<int8_t*>(p.weight) + ((int64_t)max(t.expert, 0) * p.N + n0) * p.K, 0,
+                                             min(kWideN, p.N - n0) * p.K, kRawBuffer);
+  };
+  auto buffer_m = [&](const Tile& t) {
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<int8_t*>(p.x) + (int64_t)t.row * p.K, 0, t.rows * p.K, kRawBuffer);
+  };
+  auto begin = [&](Buffer rows_n, Buffer rows_m) {  // the first step's pieces, and half of the second's
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) bring(rows_n, rows_m, offset(0), even, i);
+#pragma unroll
+    for (int i = 0; i < kLoads / 2; ++i) bring(rows_n, rows_m, offset(kStep), odd, i);
+  };
+  int32_t n0;
+  Tile t = look(n0);
+  auto rows_n = buffer_n(t, n0), rows_m = buffer_m(t);
+  begin(rows_n, rows_m);
+  __builtin_amdgcn_s_waitcnt(kAllLoads);
+  for (bool more = true; more;) {
+    walk.at += walk.step;
+    more = walk.more();
+    int32_t next_n0 = n0;
+    Tile next = t;
+    if (more) next = look(next_n0);
+    const float* const sw = p.weight_scale + (int64_t)max(t.expert, 0) * p.N;
+    const bool whole = n0 + kWideN <= p.N;
+    const int32_t K = t.expert < 0 ? 0 : p.K;
     i32x4 a[2][4], b[2][4];
     auto take = [&](const i32x4* lds, int s, int into, int i) {
       const int c = (2 * s + lane / 32) ^ turn;
@@ -370,38 +392,34 @@ product_wide_kernel(ProductArgs p, Work work, int32_t most) {
         __builtin_amdgcn_sched_barrier(0);
       }
     };
-    auto step = [&](int32_t k, i32x4* here, i32x4* next) {
+    auto step = [&](int32_t k, i32x4* here, i32x4* there) {
 #pragma unroll
       for (int s = 0; s < 3; ++s)
         multiply(s % 2, [&](int n) {
-          if (n % 2 == 0) take(here, s + 1, (s + 1) % 2, n / 2);
-          if (s == 0 && n % 2 == 1) bring(offset(k + kStep), next, kLoads / 2 + n / 2);
+          if (n < 8) take(here, s + 1, (s + 1) % 2, n);
+          if (s == 0 && n % 2 == 1) bring(rows_n, rows_m, offset(k + kStep), there, kLoads / 2 + n / 2);
         });
       __builtin_amdgcn_s_waitcnt(kAllLoads);
       __syncthreads();  // the next step's pieces are there, and nothing reads this one's any more
       multiply(1, [&](int n) {
-        if (n % 2 == 0) take(next, 0, 0, n / 2);
-        else bring(offset(k + 2 * kStep), here, n / 2);
+        if (n < 8) take(there, 0, 0, n);
+        if (n % 2 == 1) bring(rows_n, rows_m, offset(k + 2 * kStep), here, n / 2);
       });
     };
-#pragma unroll
-    for (int i = 0; i < kLoads; ++i) bring(offset(0), even, i);
-#pragma unroll
-    for (int i = 0; i < kLoads / 2; ++i) bring(offset(kStep), odd, i);
-    __builtin_amdgcn_s_waitcnt(kAllLoads);
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < 8; ++i) take(even, 0, 0, i);
     int32_t k = 0;
-    for (; k + kStep < p.K; k += 2 * kStep) {
+    for (; k + kStep < K; k += 2 * kStep) {
       step(k, even, odd);
       step(k + kStep, odd, even);
     }
-    if (k < p.K) step(k, even, odd);
-    __builtin_amdgcn_s_waitcnt(kAllLoads);  // what was brought last is of no use, but on its way
-    // the scales of this lane's channels and rows
-    const float* const sw = p.weight_scale + (int64_t)t.expert * p.N;
-    const bool whole = n0 + kWideN <= p.N;
+    if (k < K) step(k, even, odd);
+    // What was brought last is of no use, but on its way.  No wave reads LDS any more (but for operands that it does
+    // not use), so the next tile's first pieces come while this one's results go.
+    __builtin_amdgcn_s_waitcnt(kAllLoads);
+    const auto next_rows_n = buffer_n(next, next_n0), next_rows_m = buffer_m(next);
+    if (more) begin(next_rows_n, next_rows_m);
     f32x4 sn[4][4];
     float sm[4];
 #pragma unroll
@@ -409,7 +427,9 @@ product_wide_kernel(ProductArgs p, Work work, int32_t most) {
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
         const int32_t n = n0 + wn + 32 * i + 8 * q + 4 * (lane / 32);
-        if (whole) {
+        if (t.expert < 0) {
+          sn[i][q] = 0.f;
+        } else if (whole) {
           sn[i][q] = *reinterpret_cast<const f32x4_at*>(sw + n);
         } else {
 #pragma unroll
@@ -417,7 +437,9 @@ product_wide_kernel(ProductArgs p, Work work, int32_t most) {
         }
       }
 #pragma unroll
-    for (int j = 0; j < 4; ++j) sm[j] = p.scale[t.row + min(wm + 32 * j + lane % 32, t.rows - 1)];
+    for (int j = 0; j < 4; ++j)
+      sm[j] = t.expert < 0 ? 0.f : p.scale[t.row + min(wm + 32 * j + lane % 32, t.rows - 1)];
+    __builtin_amdgcn_s_waitcnt(kAllLoads);  // the next tile's pieces too, and not for the results that go now
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       const int m = wm + 32 * j + lane % 32;
@@ -439,6 +461,10 @@ product_wide_kernel(ProductArgs p, Work work, int32_t most) {
           }
         }
     }
+    t = next;
+    n0 = next_n0;
+    rows_n = next_rows_n;
+    rows_m = next_rows_m;
   }
 }
 
@@ -533,17 +559,17 @@ taot_status product(const ProductArgs& p, void* ws, hipStream_t stream) {
     runs_kernel<<<1, kRunThreads, 0, stream>>>(p.offsets, p.experts, p.runs, p.G, p.M, rows, tiles, total);
     work = Work{tiles, total};
   }
-  auto go = [&](auto* kernel, int bn, int threads, size_t lds) {
+  auto go = [&](auto* kernel, int bn, int threads, size_t lds, int64_t most_blocks = kMaxBlocks) {
     if (!allow_lds(reinterpret_cast<const void*>(kernel), lds)) return false;
     const int64_t blocks = round_up(most * ((p.N + bn - 1) / bn), kDies);
-    kernel<<<(unsigned)(blocks < kMaxBlocks ? blocks : kMaxBlocks), threads, lds, stream>>>(p, work, (int32_t)most);
+    kernel<<<(unsigned)(blocks < most_blocks ? blocks : most_blocks), threads, lds, stream>>>(p, work, (int32_t)most);
     return true;
   };
   bool ok;
   if (kind == kFew) ok = go(product_few_kernel<T>, 16, kWave * kFewWaves, 0);
   else if (kind == kMiddle) ok = go(product_kernel<T, 128, 64, 2, 2>, 128, 256, 2 * (128 + 64) * kStep);
   else if (p.K % 16 == 0 && reinterpret_cast<uintptr_t>(p.x) % 16 == 0 && reinterpret_cast<uintptr_t>(p.weight) % 16 == 0)
-    ok = go(product_wide_kernel<T>, kWideN, kWideThreads, 0);
+    ok = go(product_wide_kernel<T>, kWideN, kWideThreads, 0, kUnits);
   else ok = go(product_kernel<T, 256, 256, 2, 4>, 256, 512, 2 * (256 + 256) * kStep);
   return ok && hipGetLastError() == hipSuccess ? TAOT_OK : TAOT_ERR_LAUNCH;
 }
