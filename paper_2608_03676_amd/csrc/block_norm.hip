@@ -16,6 +16,8 @@
 namespace taot {
 namespace {
 
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+
 // A norm's weights or a gate: null, of the rows' type, or floats.
 struct Vector {
   const void* p;
@@ -119,84 +121,115 @@ struct Rows {
   }
 };
 
+// Sums of three values over a row's waves, with one barrier: `slot` takes turns.
+struct Three {
+  float a, b, c;
+};
+__device__ __forceinline__ Three row_sums(Three v, f32x4 (*part)[16], int slot, int waves) {
+  v = {block_reduce<kWave>(v.a, SumOp()), block_reduce<kWave>(v.b, SumOp()), block_reduce<kWave>(v.c, SumOp())};
+  if (waves > 1) {
+    const int lane = threadIdx.x & (kWave - 1), wid = threadIdx.x / kWave;
+    if (lane == 0) part[slot][wid] = f32x4{v.a, v.b, v.c, 0.f};
+    __syncthreads();
+    const f32x4 w = lane % 16 < waves ? part[slot][lane % 16] : f32x4(0.f);
+    v = {block_reduce<16>(w[0], SumOp()), block_reduce<16>(w[1], SumOp()), block_reduce<16>(w[2], SumOp())};
+  }
+  return v;
+}
+
 // A worker (`waves` waves) keeps its share of dw and of S (MANY: of dpost) in
 // registers until it writes them as one row of the partial sums; a gate that a
-// worker has alone gets its gradient at once.  dresidual and dx may lie in an
-// input's memory: a row is read by its worker alone, each place by the lane that
-// writes it, before it does.
-template <typename T, bool FAR, bool MANY>
+// worker has alone gets its gradient at once.  The next row is on its way while
+// the present one is worked on.  dresidual and dx may lie in an input's memory: a row
+// is read by its worker alone, each place by the lane that writes it, before it does.
+//
+// With q = gate post, e = b dy w + dh and c = b^2 mean(dy w h) it is D = e - b c h, so
+// sum(D q x) = sum(e q x) - b c sum(h q x): all sums of a row are taken at once.
+template <typename T, bool FAR, bool MANY, bool WHOLE>
 __global__ void __launch_bounds__(1024)
 block_norm_backward_kernel(const T* dy, const T* dh, const T* x, const T* h, const float* __restrict__ rstd_x,
                            const float* __restrict__ rstd_h, Vector post, Vector gate, Share share, Vector weight,
                            int32_t H, float alpha, T* dx, T* dresidual, float* __restrict__ dgate,
                            float* __restrict__ part_w, float* __restrict__ part_s, int32_t workers, int waves) {
   using Raw = typename Row8<T>::vec;
-  __shared__ float part[2][16];
+  __shared__ f32x4 part[2][16];
   const int lane = waves == 1 ? threadIdx.x & (kWave - 1) : threadIdx.x;
   const int32_t worker = waves == 1 ? blockIdx.x * kRowsOfBlock + threadIdx.x / kWave : blockIdx.x;
   if (worker >= workers) return;
   const int col = 8 * lane, n = H - col;
+  constexpr bool kAhead = sizeof(T) == 2;  // the registers of 16 waves hold two rows of 16 bits
   const bool sums = post.p || gate.p;
   Rows<MANY> rows(share, worker, workers);
-  f32x8 dw = 0.f, S = 0.f, dp = 0.f;
-  Raw rx, rh, ry, rd, nx, nh, ny, nd;
-  auto fetch = [&](int64_t row, Raw& fx, Raw& fh, Raw& fy, Raw& fd) {
-    if (sums) fx = load_raw(x + row * H + col, n);
-    if (weight.p) {
-      fh = load_raw(h + row * H + col, n);
-      fy = load_raw(dy + row * H + col, n);
+  auto load = [&](const T* from, int64_t row, Raw& to) {  // lanes behind the row keep their zeros
+    if constexpr (WHOLE) {
+      if (n > 0) to = *reinterpret_cast<const typename Row8<T>::at*>(from + row * H + col);
+    } else {
+      to = load_raw(from + row * H + col, n);
     }
-    if (dh) fd = load_raw(dh + row * H + col, n);
   };
-  fetch(rows.row, rx, rh, ry, rd);
+  auto store = [&](T* to, f32x8 v) {
+    if (WHOLE ? n > 0 : true) store_row<FAR>(to, v, WHOLE ? 8 : n);
+  };
+  const f32x8 w = factor<T>(weight, col, n);
+  f32x8 q = factor<T>(gate, rows.seg * H + col, n) * factor<T>(post, col, n);
+  f32x8 dw = 0.f, S = 0.f, dp = 0.f;
+  Raw rx = {}, rh = {}, ry = {}, rd = {}, nx = {}, nh = {}, ny = {}, nd = {};
+  auto fetch = [&](int64_t row, Raw& fx, Raw& fh, Raw& fy, Raw& fd) {
+    if (sums) load(x, row, fx);
+    if (weight.p) {
+      load(h, row, fh);
+      load(dy, row, fy);
+    }
+    if (dh) load(dh, row, fd);
+  };
+  if (kAhead) fetch(rows.row, rx, rh, ry, rd);
   float a = post.p ? rstd_x[rows.row] : 1.f, b = weight.p ? rstd_h[rows.row] : 0.f;
   int slot = 0;
   for (; rows.left > 0; rows.next()) {
     const int64_t at = rows.row * H + col, gate_at = rows.seg * H + col, then = rows.then();
-    fetch(then, nx, nh, ny, nd);
+    if (kAhead) fetch(then, nx, nh, ny, nd);
+    else fetch(rows.row, rx, rh, ry, rd);
     const float next_a = post.p ? rstd_x[then] : 1.f, next_b = weight.p ? rstd_h[then] : 0.f;
-    f32x8 D = 0.f;
-    if (weight.p) {
-      const f32x8 w = factor<T>(weight, col, n), Hh = widen(rh), Y = widen(ry);
-      float dot = 0.f;
+    const f32x8 Y = widen(ry), Hh = widen(rh), X = widen(rx);
+    f32x8 e = widen(rd);
+    Three s = {0.f, 0.f, 0.f};
 #pragma unroll
-      for (int u = 0; u < 8; ++u) {
-        dw[u] = fmaf(Y[u], Hh[u] * b, dw[u]);
-        dot = fmaf(Y[u] * w[u], Hh[u], dot);
-      }
-      const float c = b * b * (row_reduce(dot, SumOp(), part, slot, waves) / (float)H);
-      slot ^= 1;
-      D = b * (Y * w - Hh * c);
+    for (int u = 0; u < 8; ++u) {
+      const float v = Y[u] * w[u], qx = q[u] * X[u];
+      e[u] = fmaf(b, v, e[u]);
+      dw[u] = fmaf(Y[u], Hh[u] * b, dw[u]);
+      s.a = fmaf(v, Hh[u], s.a);
+      s.b = fmaf(e[u], qx, s.b);
+      s.c = fmaf(Hh[u], qx, s.c);
     }
-    if (dh) D += widen(rd);
-    store_row<FAR>(dresidual + at, alpha * D, n);
-    if (sums) {
-      const f32x8 X = widen(rx);
+    s = row_sums(s, part, slot, waves);
+    slot ^= 1;
+    const float bc = b * b * b * (s.a / (float)H), m = a * a * (fmaf(-bc, s.c, s.b) / (float)H);
+    f32x8 D, t;
 #pragma unroll
-      for (int u = 0; u < 8; ++u) S[u] = fmaf(D[u], X[u] * a, S[u]);
-      if (gate.p) D = D * factor<T>(gate, gate_at, n);
-      if (post.p) {
-        float dot = 0.f;
-        D = D * factor<T>(post, col, n);
-#pragma unroll
-        for (int u = 0; u < 8; ++u) dot = fmaf(D[u], X[u], dot);
-        const float m = a * a * (row_reduce(dot, SumOp(), part, slot, waves) / (float)H);
-        slot ^= 1;
-        D = a * (D - X * m);
-      }
+    for (int u = 0; u < 8; ++u) {
+      D[u] = fmaf(-bc, Hh[u], e[u]);
+      S[u] = fmaf(D[u], X[u] * a, S[u]);
+      t[u] = D[u] * q[u];
+      if (post.p) t[u] = a * fmaf(-m, X[u], t[u]);
     }
-    store_row<FAR>(dx + at, D, n);
+    store(dresidual + at, alpha * D);
+    store(dx + at, t);
     if (MANY && rows.ends()) {
-      if (dgate) store_row(dgate + gate_at, S * factor<T>(post, col, n), n);
-      if (post.p) dp += S * factor<T>(gate, gate_at, n);
+      const f32x8 p = factor<T>(post, col, n);
+      if (dgate) store_row(dgate + gate_at, S * p, n);
+      dp += S * factor<T>(gate, gate_at, n);
       S = 0.f;
+      if (rows.left > 1) q = factor<T>(gate, gate_at + (int64_t)workers * H, n) * p;
     }
     a = next_a;
     b = next_b;
-    rx = nx;
-    rh = nh;
-    ry = ny;
-    rd = nd;
+    if constexpr (kAhead) {
+      rx = nx;
+      rh = nh;
+      ry = ny;
+      rd = nd;
+    }
   }
   if (part_w) store_row(part_w + (int64_t)worker * H + col, dw, n);
   if (part_s) store_row(part_s + (int64_t)worker * H + col, MANY ? dp : S, n);
@@ -293,13 +326,15 @@ __device__ __forceinline__ float column_sum(const float* __restrict__ partial, i
   return s;
 }
 
-// blockIdx.y < sets: S of that gate from its workers' rows (MANY: dpost itself);
-// the row of blocks behind them: dw.
+// blockIdx.y < sets: S of that gate from its workers' rows (MANY: dpost itself), or of
+// all gates where they are few, and with them dpost; the row of blocks behind: dw.
+constexpr int kFewGates = 32;
 template <typename T>
 __global__ void __launch_bounds__(1024)
 block_norm_sums_kernel(const float* __restrict__ part_w, const float* __restrict__ part_s, int64_t workers, bool many,
-                       int64_t sets, int64_t each, Vector post, Vector gate, int32_t H, float* __restrict__ dweight,
-                       float* __restrict__ dpost, float* __restrict__ dgate, float* __restrict__ S) {
+                       int64_t sets, int64_t gates, int64_t each, Vector post, Vector gate, int32_t H,
+                       float* __restrict__ dweight, float* __restrict__ dpost, float* __restrict__ dgate,
+                       float* __restrict__ S) {
   __shared__ float sum[32][33];
   const int c = threadIdx.x % 32, r = threadIdx.x / 32;
   const int32_t col = blockIdx.x * 32 + c;
@@ -310,18 +345,36 @@ block_norm_sums_kernel(const float* __restrict__ part_w, const float* __restrict
     if (r == 0 && col < H) dweight[col] = s;
     return;
   }
-  const float s = column_sum(part_s + set * each * H, many ? workers : each, H, col, r, c, sum);
-  if (r != 0 || col >= H) return;
   if (many) {
-    dpost[col] = s;
+    const float s = column_sum(part_s, workers, H, col, r, c, sum);
+    if (r == 0 && col < H) dpost[col] = s;
     return;
   }
-  const float p = factor<T>(post, col, 1)[0];
-  if (dgate) dgate[set * H + col] = s * p;
-  if (dpost) {
-    if (sets == 1) dpost[col] = s * factor<T>(gate, col, 1)[0];
-    else S[set * H + col] = s;
+  const float p = col < H ? factor<T>(post, col, 1)[0] : 0.f;
+  if (gates > kFewGates) {
+    const float s = column_sum(part_s + set * each * H, each, H, col, r, c, sum);
+    if (r != 0 || col >= H) return;
+    if (dgate) dgate[set * H + col] = s * p;
+    if (dpost) S[set * H + col] = s;
+    return;
   }
+  // thread r: gate r % gates, every `per`-th of its workers
+  const int n = (int)gates, mine = r % n, per = 32 / n;
+  float s = 0.f;
+  if (col < H && r < per * n)
+#pragma unroll 8
+    for (int64_t w = r / n; w < each; w += per) s += part_s[(mine * each + w) * H + col];
+  sum[r][c] = s;
+  __syncthreads();
+  if (r != 0 || col >= H) return;
+  float all = 0.f;
+  for (int g = 0; g < n; ++g) {
+    s = 0.f;
+    for (int k = 0; k < per; ++k) s += sum[k * n + g][c];
+    if (dgate) dgate[(int64_t)g * H + col] = s * p;
+    all = fmaf(s, gate.p ? factor<T>(gate, (int64_t)g * H + col, 1)[0] : 1.f, all);
+  }
+  if (dpost) dpost[col] = all;
 }
 
 // dpost = sum over the gates of g S_g.
@@ -358,10 +411,11 @@ struct Split {
   int32_t workers;
   bool many;
 };
-// Workers of the gradient: the same number on each compute unit, as many as 16 waves
-// make.  Gates of fewer rows than that are taken whole.
+// Workers of the gradient: as many on each compute unit as its registers hold, 16
+// waves.  Gates of fewer rows than that are taken whole.
 Split split_of(int64_t rows, int32_t H, int64_t gates) {
-  const int64_t most = 256 * ((16 + shape_of(H).waves - 1) / shape_of(H).waves), per = rows / gates;
+  const int waves = shape_of(H).waves;
+  const int64_t most = 256 * (16 / waves), per = rows / gates;
   if (gates >= most) return {{gates, per, 0}, (int32_t)most, true};
   int64_t each = (most + gates - 1) / gates;
   if (each > per) each = per;
@@ -378,7 +432,7 @@ Partial carve(void* ws, int64_t rows, int32_t H, int64_t gates) {
   Partial p;
   p.w = c.take<float>((size_t)s.workers * H);
   p.s = c.take<float>((size_t)s.workers * H);
-  p.S = c.take<float>(s.many || gates == 1 ? 0 : (size_t)gates * H);
+  p.S = c.take<float>(s.many || gates <= kFewGates ? 0 : (size_t)gates * H);
   p.bytes = c.off;
   return p;
 }
@@ -430,7 +484,11 @@ taot_status backward(const BlockNormGradArgs& a, void* ws, hipStream_t stream) {
     T *dx = static_cast<T*>(a.dx), *dr = static_cast<T*>(a.dresidual);
     float *part_w = a.dweight ? p.w : nullptr, *part_s = sums ? p.s : nullptr;
     if (s.cpl == 1) {
-      auto* kernel = sp.many ? block_norm_backward_kernel<T, far.value, true> : block_norm_backward_kernel<T, far.value, false>;
+      const bool whole = a.H % 8 == 0;
+      auto* kernel = sp.many ? whole ? block_norm_backward_kernel<T, far.value, true, true>
+                                     : block_norm_backward_kernel<T, far.value, true, false>
+                     : whole ? block_norm_backward_kernel<T, far.value, false, true>
+                             : block_norm_backward_kernel<T, far.value, false, false>;
       kernel<<<(unsigned)((sp.workers + per - 1) / per), kWave * s.waves * per, 0, stream>>>(
           dy, dh, x, h, a.rstd_x, a.rstd_h, post, gate, sp.share, weight, a.H, a.alpha, dx, dr, a.dgate, part_w, part_s,
           sp.workers, s.waves);
@@ -442,12 +500,12 @@ taot_status backward(const BlockNormGradArgs& a, void* ws, hipStream_t stream) {
     }
   });
   const unsigned cols = (unsigned)((a.H + 31) / 32);
-  const int64_t sets = !sums ? 0 : sp.many ? 1 : gates;
+  const int64_t sets = !sums ? 0 : sp.many || gates <= kFewGates ? 1 : gates;
   if (sets || a.dweight)
     block_norm_sums_kernel<T><<<dim3(cols, (unsigned)sets + 1), 1024, 0, stream>>>(
-        p.w, p.s, sp.workers, sp.many, sets, sp.share.each, post, gate, a.H, a.dweight, a.dpost,
+        p.w, p.s, sp.workers, sp.many, sets, gates, sp.share.each, post, gate, a.H, a.dweight, a.dpost,
         sp.many ? nullptr : a.dgate, p.S);
-  if (a.dpost && !sp.many && gates > 1)
+  if (a.dpost && !sp.many && gates > kFewGates)
     block_norm_post_kernel<T><<<cols, 1024, 0, stream>>>(p.S, gate, gates, a.H, a.dpost);
   return hipGetLastError() == hipSuccess ? TAOT_OK : TAOT_ERR_LAUNCH;
 }
