@@ -39,37 +39,51 @@ struct Group {
   }
 };
 
-template <bool SIGMOID, int L, int CPL>
+// exp(x) for x in [-150, 88]: the hardware's power of two of t = x log2(e), and what t's rounding takes away, which is
+// the larger part of the error for |x| above 1: 2^t (1 + (x - t ln 2)).
+__device__ __forceinline__ float exponential(float x) {
+  const float t = x * 1.44269504f, e = __builtin_amdgcn_exp2f(t);
+  return fmaf(e, fmaf(-t, 0.693147181f, x), e);
+}
+// x within [lo, hi], lo where it is NaN.
+__device__ __forceinline__ float within(float x, float lo, float hi) { return __builtin_amdgcn_fmed3f(x, lo, hi); }
+
+// FULL: all columns of the lanes are experts.
+template <bool SIGMOID, bool FULL, int L, int CPL>
 __device__ __forceinline__ void scores(Group<L>& g, int32_t E, f32x8 (&v)[CPL], float& total, float& lse, float& inv) {
   lse = 0.f;
   total = 0.f;
-  float top = -INFINITY;
+  if (!FULL) {
 #pragma unroll
-  for (int i = 0; i < CPL; ++i)
+    for (int i = 0; i < CPL; ++i)
 #pragma unroll
-    for (int u = 0; u < 8; ++u) {
-      const int col = 8 * (i * g.lanes + g.lane) + u;
-      const float x = v[i][u];
-      v[i][u] = col < E && x == x ? fminf(x, FLT_MAX) : -INFINITY;
-      if (!SIGMOID) top = fmaxf(top, v[i][u]);
-    }
+      for (int u = 0; u < 8; ++u)
+        if (8 * (i * g.lanes + g.lane) + u >= E) v[i][u] = -INFINITY;
+  }
   if (SIGMOID) {
 #pragma unroll
     for (int i = 0; i < CPL; ++i)
 #pragma unroll
       for (int u = 0; u < 8; ++u) {
-        v[i][u] = 1.f / (1.f + expf(-v[i][u]));
+        // below -87 the sigmoid is not a normal number, and 0 here; so is that of NaN
+        const float x = v[i][u], s = __builtin_amdgcn_rcpf(1.f + exponential(within(-x, -150.f, 88.f)));
+        v[i][u] = x >= -87.f ? s : 0.f;
         total += v[i][u];
       }
     total = g.reduce(total, SumOp()) + kTiny;
     inv = 1.f / total;
   } else {
-    top = fmaxf(g.reduce(top, MaxOp()), -FLT_MAX);
+    float top = -FLT_MAX;
+#pragma unroll
+    for (int i = 0; i < CPL; ++i)
+#pragma unroll
+      for (int u = 0; u < 8; ++u) top = fmaxf(top, v[i][u]);  // the number where one of the two is NaN
+    top = fminf(g.reduce(top, MaxOp()), FLT_MAX);
 #pragma unroll
     for (int i = 0; i < CPL; ++i)
 #pragma unroll
       for (int u = 0; u < 8; ++u) {
-        v[i][u] = expf(v[i][u] - top);
+        v[i][u] = exponential(within(v[i][u] - top, -150.f, 0.f));  // 0 at -150, where -infinity and NaN are
         total += v[i][u];
       }
     total = g.reduce(total, SumOp());
@@ -84,11 +98,11 @@ struct Tokens {
 };
 
 // Block (row, b) has tokens b * each .. of its row and writes its share of the sums.
-template <typename T, bool SIGMOID, int L, int CPL>
+template <typename T, bool SIGMOID, bool FULL, int L, int CPL>
 __global__ void __launch_bounds__(1024)
 balance_kernel(const T* __restrict__ logits, const int32_t* __restrict__ ids, const uint8_t* __restrict__ mask, Tokens s,
                int64_t each, float* __restrict__ part_p, int32_t* __restrict__ part_c, float* __restrict__ part_z,
-               int32_t* __restrict__ part_n) {
+               int32_t* __restrict__ part_n, int32_t* __restrict__ done) {
   extern __shared__ int32_t room[];
   __shared__ float part[2][16], zs[16];
   __shared__ int32_t ns;
@@ -99,7 +113,10 @@ balance_kernel(const T* __restrict__ logits, const int32_t* __restrict__ ids, co
   int32_t* hits = room;                                  // [E]
   float* sums = reinterpret_cast<float*>(room + s.E);    // [waves][E], not where the block holds a token
   for (int32_t e = tid; e < s.E; e += blockDim.x) hits[e] = 0;
-  if (tid == 0) ns = 0;
+  if (tid == 0) {
+    ns = 0;
+    if (block == 0) done[row] = 0;
+  }
   __syncthreads();
   Group<L> g;
   g.lanes = L == kWhole ? blockDim.x : L;
@@ -113,22 +130,18 @@ balance_kernel(const T* __restrict__ logits, const int32_t* __restrict__ ids, co
 #pragma unroll
   for (int i = 0; i < CPL; ++i) acc[i] = 0.f;
   const int64_t turns = (hi - lo + step - 1) / step;  // the same for all lanes: they work together
-  for (int64_t j = 0; j < turns; ++j) {
-    const int64_t t = first + j * step, at = row * s.tokens + t;
-    const bool in = t < hi && (!mask || mask[at]);
-    f32x8 v[CPL];
+  typename Row8<T>::vec raw[CPL];
+  bool in = false;
+  auto fetch = [&](int64_t t) {
+    const int64_t at = row * s.tokens + t;
+    in = t < hi && (!mask || mask[at]);
 #pragma unroll
     for (int i = 0; i < CPL; ++i) {
       const int col = 8 * (i * g.lanes + g.lane);
-      v[i] = load_row(logits + at * s.E + col, in ? s.E - col : 0);
+      raw[i] = load_raw(logits + at * s.E + col, t >= hi ? 0 : FULL ? 8 : s.E - col);
     }
-    float total, lse, inv;
-    scores<SIGMOID>(g, s.E, v, total, lse, inv);
-    if (!in) inv = lse = 0.f;
-#pragma unroll
-    for (int i = 0; i < CPL; ++i) acc[i] += v[i] * inv;
-    z = fmaf(lse, lse, z);
-  }
+  };
+  fetch(first);
   int32_t counted = 0;
   for (int64_t i = lo + tid; i < hi; i += blockDim.x) counted += !mask || mask[row * s.tokens + i];
   for (int64_t i = tid; i < (hi - lo) * s.k; i += blockDim.x) {
@@ -137,6 +150,21 @@ balance_kernel(const T* __restrict__ logits, const int32_t* __restrict__ ids, co
     if ((uint32_t)e < (uint32_t)s.E && (!mask || mask[at + i / s.k])) atomicAdd(&hits[e], 1);
   }
   if (counted) atomicAdd(&ns, counted);
+  for (int64_t j = 0; j < turns; ++j) {
+    f32x8 v[CPL];
+#pragma unroll
+    for (int i = 0; i < CPL; ++i) v[i] = widen(raw[i]);
+    const bool now = in;
+    if (j + 1 < turns) fetch(first + (j + 1) * step);
+    float total, lse, inv;
+    scores<SIGMOID, FULL>(g, s.E, v, total, lse, inv);
+    if (!now) inv = lse = 0.f;
+#pragma unroll
+    for (int i = 0; i < CPL; ++i)
+#pragma unroll
+      for (int u = 0; u < 8; ++u) acc[i][u] = fmaf(v[i][u], inv, acc[i][u]);
+    z = fmaf(lse, lse, z);
+  }
   if (L != kWhole && L < kWave) {  // a wave's tokens
 #pragma unroll
     for (int o = L; o < kWave; o *= 2) {
@@ -181,85 +209,110 @@ balance_kernel(const T* __restrict__ logits, const int32_t* __restrict__ ids, co
   }
 }
 
-// prob and counts of 32 experts of a row, 32 threads each.
+// prob and counts of kTile experts of a row, 32 threads each, and these experts' part
+// of the loss.  The last block of a row adds the parts up, in order.
+constexpr int kTile = 32;
+struct Part {
+  float loss;
+  int32_t choices;
+};
 __global__ void __launch_bounds__(1024)
-balance_sums_kernel(const float* __restrict__ part_p, const int32_t* __restrict__ part_c, const int32_t* __restrict__ part_n,
-                    int32_t blocks, int32_t E, float* __restrict__ prob, int32_t* __restrict__ counts) {
-  __shared__ float sum[32][33];
-  __shared__ int32_t cnt[32][33];
-  __shared__ int32_t ns;
-  const int c = threadIdx.x % 32, r = threadIdx.x / 32;
-  const int32_t tiles = (E + 31) / 32, e = (int32_t)(blockIdx.x % (uint32_t)tiles) * 32 + c;
+balance_sums_kernel(const float* __restrict__ part_p, const int32_t* __restrict__ part_c, const float* __restrict__ part_z,
+                    const int32_t* __restrict__ part_n, int32_t blocks, int32_t E, float* __restrict__ prob,
+                    int32_t* __restrict__ counts, uint64_t* parts, int32_t* done, float* __restrict__ loss,
+                    float* __restrict__ z, int32_t* __restrict__ counted) {
+  __shared__ float sum[16][kTile], zs[16];
+  __shared__ int32_t cnt[16][kTile], ns[16], all[16];
+  __shared__ int32_t last;
+  const int c = threadIdx.x % kTile, r = threadIdx.x / kTile, wid = threadIdx.x / kWave;
+  const int32_t tiles = (E + kTile - 1) / kTile, e = (int32_t)(blockIdx.x % (uint32_t)tiles) * kTile + c;
   const int64_t row = blockIdx.x / (uint32_t)tiles, at = row * blocks;
-  if (threadIdx.x == 0) ns = 0;
-  __syncthreads();
-  int32_t n = 0;
-  for (int32_t b = threadIdx.x; b < blocks; b += 1024) n += part_n[at + b];
-  if (n) atomicAdd(&ns, n);
-  float p = 0.f;
-  int32_t k = 0;
+  float p = 0.f, zz = 0.f;  // z is the last block's to write, but here its way is short
+  int32_t k = 0, n = 0;
+  for (int32_t b = threadIdx.x; b < blocks; b += 1024) {
+    n += part_n[at + b];
+    zz += part_z[at + b];
+  }
   if (e < E)
-#pragma unroll 4
-    for (int32_t b = r; b < blocks; b += 32) {
+#pragma unroll 8
+    for (int32_t b = r; b < blocks; b += 1024 / kTile) {
       p += part_p[(at + b) * E + e];
       k += part_c[(at + b) * E + e];
     }
-  sum[r][c] = p;
-  cnt[r][c] = k;
-  __syncthreads();
-  if (r == 0 && e < E) {
+  zz = wave_sum(zz);
+  for (int o = 32; o > 0; o >>= 1) n += __shfl_xor(n, o, kWave);
+  if (threadIdx.x % kWave == 0) {
+    ns[wid] = n;
+    zs[wid] = zz;
+  }
 #pragma unroll
-    for (int w = 1; w < 32; ++w) {
+  for (int o = kTile; o < kWave; o *= 2) {
+    p += __shfl_xor(p, o, kWave);
+    k += __shfl_xor(k, o, kWave);
+  }
+  if (threadIdx.x % kWave < kTile) {
+    sum[wid][c] = p;
+    cnt[wid][c] = k;
+  }
+  __syncthreads();
+  n = 0;
+  zz = 0.f;
+#pragma unroll
+  for (int w = 0; w < 16; ++w) {
+    n += ns[w];
+    zz += zs[w];
+  }
+  if (threadIdx.x < kTile) {
+    p = 0.f;
+    k = 0;
+#pragma unroll
+    for (int w = 0; w < 16; ++w) {
       p += sum[w][c];
       k += cnt[w][c];
     }
-    prob[row * E + e] = p / (float)max(ns, 1);
-    counts[row * E + e] = k;
+    p /= (float)max(n, 1);
+    if (e < E) {
+      prob[row * E + e] = p;
+      counts[row * E + e] = k;
+    }
+    float mine = block_reduce<kTile>((float)k * p, SumOp());  // the others have neither
+    for (int o = 1; o < kTile; o *= 2) k += __shfl_xor(k, o, kTile);
+    if (threadIdx.x == 0) {
+      // The part is written past the die's own cache, and is there when the wait is over; no other write has to be seen
+      // by the last block.
+      __hip_atomic_store(parts + blockIdx.x, __builtin_bit_cast(uint64_t, Part{mine, k}), __ATOMIC_RELAXED,
+                         __HIP_MEMORY_SCOPE_AGENT);
+      __atomic_signal_fence(__ATOMIC_SEQ_CST);
+      __builtin_amdgcn_s_waitcnt(0);
+      __atomic_signal_fence(__ATOMIC_SEQ_CST);
+      last = __hip_atomic_fetch_add(done + row, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == tiles - 1;
+    }
   }
-}
-
-// loss, z and the number of tokens of a row, a block each.
-__global__ void __launch_bounds__(256)
-balance_loss_kernel(const float* __restrict__ prob, const int32_t* __restrict__ counts, const float* __restrict__ part_z,
-                    const int32_t* __restrict__ part_n, int32_t blocks, int32_t E, float* __restrict__ loss,
-                    float* __restrict__ z, int32_t* __restrict__ counted) {
-  __shared__ float part[4][4];
-  const int64_t row = blockIdx.x;
-  float s = 0.f, zz = 0.f;
-  int32_t n = 0, all = 0;
-  for (int32_t e = threadIdx.x; e < E; e += 256) {
-    const int32_t k = counts[row * E + e];
-    s = fmaf((float)k, prob[row * E + e], s);
-    all += k;
+  __syncthreads();
+  if (!last) return;
+  float l = 0.f;
+  k = 0;
+  for (int32_t i = threadIdx.x; i < tiles; i += 1024) {
+    const Part q = __builtin_bit_cast(
+        Part, __hip_atomic_load(parts + row * tiles + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
+    l += q.loss;
+    k += q.choices;
   }
-  for (int32_t b = threadIdx.x; b < blocks; b += 256) {
-    zz += part_z[row * blocks + b];
-    n += part_n[row * blocks + b];
-  }
-  s = wave_sum(s);
-  zz = wave_sum(zz);
-  for (int o = 32; o > 0; o >>= 1) {
-    n += __shfl_xor(n, o, kWave);
-    all += __shfl_xor(all, o, kWave);
-  }
-  const int w = threadIdx.x / kWave;
+  l = wave_sum(l);
+  for (int o = 32; o > 0; o >>= 1) k += __shfl_xor(k, o, kWave);
   if (threadIdx.x % kWave == 0) {
-    part[0][w] = s;
-    part[1][w] = zz;
-    part[2][w] = __int_as_float(n);
-    part[3][w] = __int_as_float(all);
+    sum[wid][0] = l;
+    all[wid] = k;
   }
   __syncthreads();
   if (threadIdx.x != 0) return;
-  s = zz = 0.f;
-  n = all = 0;
-  for (int i = 0; i < 4; ++i) {
-    s += part[0][i];
-    zz += part[1][i];
-    n += __float_as_int(part[2][i]);
-    all += __float_as_int(part[3][i]);
+  l = 0.f;
+  k = 0;
+  for (int w = 0; w < 16; ++w) {
+    l += sum[w][0];
+    k += all[w];
   }
-  loss[row] = (float)E * (s / (float)max(all, 1));
+  loss[row] = (float)E * (l / (float)max(k, 1));
   if (z) z[row] = zz / (float)max(n, 1);
   if (counted) counted[row] = n;
 }
@@ -267,12 +320,13 @@ balance_loss_kernel(const float* __restrict__ prob, const int32_t* __restrict__ 
 // Block (row, b) as in balance_kernel; a lane holds its experts' a throughout.
 // dlogits may lie in the logits' or add's memory: a lane reads a token's columns
 // before it writes them.
-template <typename T, bool SIGMOID, int L, int CPL>
-__global__ void __launch_bounds__(1024)
+template <typename T, bool SIGMOID, bool FULL, int L, int CPL>
+__global__ void __launch_bounds__(L == kWhole ? 1024 : 256)
 balance_backward_kernel(const float* __restrict__ dloss, const float* __restrict__ dz, const T* logits,
                         const int32_t* __restrict__ counts, const int32_t* __restrict__ counted,
                         const uint8_t* __restrict__ mask, const T* add, Tokens s, int64_t each, T* dlogits) {
-  __shared__ float part[2][16];
+  extern __shared__ f32x8 table[];  // a of each expert, 0 behind the last
+  __shared__ float part[2][16], alls[16];
   constexpr int kLanes = L == kWhole ? kWave : L;
   const int waves = blockDim.x / kWave, tid = threadIdx.x;
   const int64_t row = blockIdx.x / (uint32_t)s.blocks, block = blockIdx.x % (uint32_t)s.blocks;
@@ -283,52 +337,68 @@ balance_backward_kernel(const float* __restrict__ dloss, const float* __restrict
   g.waves = waves;
   g.slot = 0;
   g.part = part;
-  const float n = (float)max(counted[row], 1);
-  f32x8 a[CPL];
-  float all = 0.f;
-#pragma unroll
-  for (int i = 0; i < CPL; ++i) {
-    const int col = 8 * (i * g.lanes + g.lane);
-#pragma unroll
-    for (int u = 0; u < 8; ++u) {
-      a[i][u] = col + u < s.E ? (float)counts[row * s.E + col + u] : 0.f;
-      all += a[i][u];
-    }
-  }
-  all = g.reduce(all, SumOp());
-  const float f = dloss[row] * (float)s.E / (fmaxf(all, 1.f) * n), fz = dz ? 2.f * dz[row] / n : 0.f;
-#pragma unroll
-  for (int i = 0; i < CPL; ++i) a[i] = a[i] * f;
   const int64_t first = L == kWhole ? lo : lo + tid / kLanes, step = L == kWhole ? 1 : waves * (kWave / kLanes);
   const int64_t turns = (hi - lo + step - 1) / step;
+  typename Row8<T>::vec raw[CPL], more[CPL];
+  bool in = false;
+  auto fetch = [&](int64_t t) {
+    const int64_t at = row * s.tokens + t;
+    in = t < hi && (!mask || mask[at]);
+#pragma unroll
+    for (int i = 0; i < CPL; ++i) {
+      const int col = 8 * (i * g.lanes + g.lane), m = t >= hi ? 0 : FULL ? 8 : s.E - col;
+      raw[i] = load_raw(logits + at * s.E + col, m);
+      if (add) more[i] = load_raw(add + at * s.E + col, m);
+    }
+  };
+  fetch(first);
+  float* const words = reinterpret_cast<float*>(table);
+  float all = 0.f;
+  for (int32_t e = tid; e < (s.E + 7) / 8 * 8; e += blockDim.x) {
+    const float c = e < s.E ? (float)counts[row * s.E + e] : 0.f;
+    words[e] = c;
+    all += c;
+  }
+  all = block_reduce<kWave>(all, SumOp());
+  if (tid % kWave == 0) alls[tid / kWave] = all;
+  const float n = (float)max(counted[row], 1), fz = dz ? 2.f * dz[row] / n : 0.f, fl = dloss[row];
+  __syncthreads();
+  all = 0.f;
+  for (int w = 0; w < waves; ++w) all += alls[w];
+  const float f = fl * (float)s.E / (fmaxf(all, 1.f) * n);
   for (int64_t j = 0; j < turns; ++j) {
     const int64_t t = first + j * step, at = row * s.tokens + t;
-    const bool is = t < hi, in = is && (!mask || mask[at]);
     f32x8 v[CPL];
+    typename Row8<T>::vec also[CPL];
 #pragma unroll
     for (int i = 0; i < CPL; ++i) {
-      const int col = 8 * (i * g.lanes + g.lane);
-      v[i] = load_row(logits + at * s.E + col, in ? s.E - col : 0);
+      v[i] = widen(raw[i]);
+      also[i] = more[i];
     }
+    const bool now = in;
+    if (j + 1 < turns) fetch(t + step);
     float total, lse, inv, dot = 0.f;
-    scores<SIGMOID>(g, s.E, v, total, lse, inv);
-#pragma unroll
-    for (int i = 0; i < CPL; ++i)
-#pragma unroll
-      for (int u = 0; u < 8; ++u) dot = fmaf(a[i][u], v[i][u], dot);
-    dot = g.reduce(dot, SumOp()) * inv;
-    const float up = SIGMOID ? 0.f : fz * lse;
+    scores<SIGMOID, FULL>(g, s.E, v, total, lse, inv);
+    const f32x8* const a = table + g.lane;
 #pragma unroll
     for (int i = 0; i < CPL; ++i) {
-      const int col = 8 * (i * g.lanes + g.lane), m = is ? s.E - col : 0;
-      f32x8 d = 0.f;
-      if (add) d = load_row(add + at * s.E + col, m);
-      if (in) {
+      const f32x8 c = FULL || 8 * (i * g.lanes + g.lane) < s.E ? a[i * g.lanes] : f32x8(0.f);
 #pragma unroll
-        for (int u = 0; u < 8; ++u) {
-          const float p = v[i][u];
-          d[u] += SIGMOID ? (a[i][u] - dot) * inv * p * (1.f - p) : p * inv * ((a[i][u] - dot) + up);
-        }
+      for (int u = 0; u < 8; ++u) dot = fmaf(c[u], v[i][u], dot);
+    }
+    dot = g.reduce(dot, SumOp()) * inv * f;
+    const float up = SIGMOID ? dot : dot - fz * lse, each_p = now ? inv : 0.f;
+#pragma unroll
+    for (int i = 0; i < CPL; ++i) {
+      const int col = 8 * (i * g.lanes + g.lane), m = t >= hi ? 0 : FULL ? 8 : s.E - col;
+      const f32x8 c = FULL || col < s.E ? a[i * g.lanes] : f32x8(0.f);
+      f32x8 d = 0.f;
+      if (add) d = widen(also[i]);
+#pragma unroll
+      for (int u = 0; u < 8; ++u) {
+        const float p = v[i][u] * each_p;
+        const float w = SIGMOID ? p - p * v[i][u] : p;
+        if (now) d[u] = fmaf(fmaf(c[u], f, -up), w, d[u]);
       }
       store_row(dlogits + at * s.E + col, d, m);
     }
@@ -341,12 +411,16 @@ struct Layout {
   int32_t blocks;
   int64_t each;
 };
-Layout layout_of(int64_t rows, int64_t tokens, int32_t E) {
+// Forward: blocks of 16 waves, one on each of the 256 compute units: more of them cost
+// more in the sums than they bring (65536 tokens of 256 in 32 bits, us by blocks of 16,
+// 8 and 8 waves: 256 22.5, 768 25.4, 1024 26.9).  Backward: what is resident at once
+// (32768 of 384 in 16 bits, 1280 blocks of four waves 18.2, 2048 21.0, 4096 21.0).
+Layout layout_of(int64_t rows, int64_t tokens, int32_t E, bool backward) {
   Layout l;
   if (E <= 512) {
-    l = {16, E <= 128 ? 1 : E <= 256 ? 2 : 4, 256, 0, 0};
+    l = {16, (E + 127) / 128, backward ? 256 : 1024, 0, 0};
   } else if (E <= 2048) {
-    l = {64, E <= 1024 ? 2 : 4, 256, 0, 0};
+    l = {64, E <= 1024 ? 2 : 4, backward ? 256 : 1024, 0, 0};
   } else {
     const int chunks = (E + 7) / 8;
     int cpl = 1;
@@ -354,7 +428,8 @@ Layout layout_of(int64_t rows, int64_t tokens, int32_t E) {
     l = {kWhole, cpl, (chunks + cpl * kWave - 1) / (cpl * kWave) * kWave, 0, 0};
   }
   const int64_t at_once = l.lanes == kWhole ? 1 : l.threads / l.lanes, most = (tokens + at_once - 1) / at_once;
-  int64_t blocks = (1024 + rows - 1) / rows;
+  const int64_t wanted = 256 * (backward && l.lanes != kWhole ? 5 : 1024 / l.threads);
+  int64_t blocks = (wanted + rows - 1) / rows;
   if (blocks > most) blocks = most;
   if (blocks < 1) blocks = 1;
   l.each = ((tokens + blocks - 1) / blocks + at_once - 1) / at_once * at_once;
@@ -368,7 +443,8 @@ struct Partial {
   float* p;
   int32_t* c;
   float* z;
-  int32_t* n;
+  int32_t *n, *done;
+  uint64_t* parts;
   size_t bytes;
 };
 Partial carve(void* ws, int64_t rows, int32_t E, int32_t blocks) {
@@ -378,25 +454,35 @@ Partial carve(void* ws, int64_t rows, int32_t E, int32_t blocks) {
   p.c = c.take<int32_t>((size_t)rows * blocks * E);
   p.z = c.take<float>((size_t)rows * blocks);
   p.n = c.take<int32_t>((size_t)rows * blocks);
+  p.done = c.take<int32_t>((size_t)rows);
+  p.parts = c.take<uint64_t>((size_t)rows * ((E + kTile - 1) / kTile));
   p.bytes = c.off;
   return p;
 }
 
-// f(lanes, chunks) as constants.
-template <typename F>
-void with_layout(const Layout& l, F f) {
+// f(lanes, chunks, whether they hold experts alone) as constants.
+template <int L, int CPL, typename F>
+void with_full(int32_t E, F f) {
   using std::integral_constant;
+  if constexpr (L == 16) {
+    if (E == 8 * L * CPL) return f(integral_constant<int, L>(), integral_constant<int, CPL>(), std::true_type());
+  }
+  f(integral_constant<int, L>(), integral_constant<int, CPL>(), std::false_type());
+}
+template <typename F>
+void with_layout(const Layout& l, int32_t E, F f) {
   if (l.lanes == 16) {
-    if (l.cpl == 1) f(integral_constant<int, 16>(), integral_constant<int, 1>());
-    else if (l.cpl == 2) f(integral_constant<int, 16>(), integral_constant<int, 2>());
-    else f(integral_constant<int, 16>(), integral_constant<int, 4>());
+    if (l.cpl == 1) with_full<16, 1>(E, f);
+    else if (l.cpl == 2) with_full<16, 2>(E, f);
+    else if (l.cpl == 3) with_full<16, 3>(E, f);
+    else with_full<16, 4>(E, f);
   } else if (l.lanes == 64) {
-    if (l.cpl == 2) f(integral_constant<int, 64>(), integral_constant<int, 2>());
-    else f(integral_constant<int, 64>(), integral_constant<int, 4>());
+    if (l.cpl == 2) with_full<64, 2>(E, f);
+    else with_full<64, 4>(E, f);
   } else {
-    if (l.cpl == 1) f(integral_constant<int, kWhole>(), integral_constant<int, 1>());
-    else if (l.cpl == 2) f(integral_constant<int, kWhole>(), integral_constant<int, 2>());
-    else f(integral_constant<int, kWhole>(), integral_constant<int, 4>());
+    if (l.cpl == 1) with_full<kWhole, 1>(E, f);
+    else if (l.cpl == 2) with_full<kWhole, 2>(E, f);
+    else with_full<kWhole, 4>(E, f);
   }
 }
 
@@ -407,19 +493,19 @@ bool by_type(int32_t dtype, F f) {
   return f(float());
 }
 
-constexpr int64_t kRowsAtOnce = kMaxBlocks / (TAOT_MAX_EXPERTS / 32);  // of a launch: up to a block for each 32 experts of a row
+constexpr int64_t kRowsAtOnce = kMaxBlocks / (TAOT_MAX_EXPERTS / kTile);  // of a launch: up to a block for each tile of a row
 
 }  // namespace
 
 size_t balance_loss_ws(int64_t rows, int64_t tokens, int32_t E) {
   const int64_t n = rows < kRowsAtOnce ? rows : kRowsAtOnce;
-  return carve(nullptr, n, E, layout_of(n, tokens, E).blocks).bytes;
+  return carve(nullptr, n, E, layout_of(n, tokens, E, false).blocks).bytes;
 }
 
 taot_status launch_balance_loss(const void* logits, const int32_t* ids, const uint8_t* mask, int64_t rows,
                                 int64_t tokens, int32_t E, int32_t k, uint32_t flags, int32_t dtype, float* loss,
                                 float* z, int32_t* counts, float* prob, int32_t* counted, void* ws, hipStream_t stream) {
-  const Layout l = layout_of(rows < kRowsAtOnce ? rows : kRowsAtOnce, tokens, E);
+  const Layout l = layout_of(rows < kRowsAtOnce ? rows : kRowsAtOnce, tokens, E, false);
   const Partial p = carve(ws, rows < kRowsAtOnce ? rows : kRowsAtOnce, E, l.blocks);
   const size_t lds = (size_t)E * 4 * (1 + (l.lanes == kWhole ? 0 : l.threads / kWave));
   for (int64_t r = 0; r < rows; r += kRowsAtOnce) {  // one after the other in the same workspace
@@ -428,22 +514,21 @@ taot_status launch_balance_loss(const void* logits, const int32_t* ids, const ui
     const bool ok = by_type(dtype, [&](auto type) {
       using T = decltype(type);
       bool fine = true;
-      with_layout(l, [&](auto lanes, auto cpl) {
-        auto* kernel = flags & TAOT_ROUTE_SIGMOID ? balance_kernel<T, true, lanes.value, cpl.value>
-                                                  : balance_kernel<T, false, lanes.value, cpl.value>;
+      with_layout(l, E, [&](auto lanes, auto cpl, auto full) {
+        auto* kernel = flags & TAOT_ROUTE_SIGMOID ? balance_kernel<T, true, full.value, lanes.value, cpl.value>
+                                                  : balance_kernel<T, false, full.value, lanes.value, cpl.value>;
         fine = allow_lds(reinterpret_cast<const void*>(kernel), lds);
         if (fine)
           kernel<<<(unsigned)(n * l.blocks), l.threads, lds, stream>>>(
               static_cast<const T*>(logits) + at * E, ids + at * k, mask ? mask + at : nullptr, s, l.each, p.p, p.c, p.z,
-              p.n);
+              p.n, p.done);
       });
       return fine;
     });
     if (!ok) return TAOT_ERR_LAUNCH;
-    balance_sums_kernel<<<(unsigned)(n * ((E + 31) / 32)), 1024, 0, stream>>>(p.p, p.c, p.n, l.blocks, E, prob + r * E,
-                                                                              counts + r * E);
-    balance_loss_kernel<<<(unsigned)n, 256, 0, stream>>>(prob + r * E, counts + r * E, p.z, p.n, l.blocks, E, loss + r,
-                                                         z ? z + r : nullptr, counted ? counted + r : nullptr);
+    balance_sums_kernel<<<(unsigned)(n * ((E + kTile - 1) / kTile)), 1024, 0, stream>>>(
+        p.p, p.c, p.z, p.n, l.blocks, E, prob + r * E, counts + r * E, p.parts, p.done, loss + r, z ? z + r : nullptr,
+        counted ? counted + r : nullptr);
   }
   return hipGetLastError() == hipSuccess ? TAOT_OK : TAOT_ERR_LAUNCH;
 }
@@ -452,22 +537,27 @@ taot_status launch_balance_loss_backward(const float* dloss, const float* dz, co
                                          const int32_t* counted, const uint8_t* mask, const void* add, int64_t rows,
                                          int64_t tokens, int32_t E, uint32_t flags, int32_t dtype, void* dlogits,
                                          hipStream_t stream) {
-  const Layout l = layout_of(rows < kRowsAtOnce ? rows : kRowsAtOnce, tokens, E);
+  const Layout l = layout_of(rows < kRowsAtOnce ? rows : kRowsAtOnce, tokens, E, true);
+  const size_t lds = (size_t)((E + 7) / 8) * sizeof(f32x8);
   for (int64_t r = 0; r < rows; r += kRowsAtOnce) {
     const int64_t n = rows - r < kRowsAtOnce ? rows - r : kRowsAtOnce, at = r * tokens;
     const Tokens s{n, tokens, E, 0, l.blocks};
-    by_type(dtype, [&](auto type) {
+    const bool ok = by_type(dtype, [&](auto type) {
       using T = decltype(type);
-      with_layout(l, [&](auto lanes, auto cpl) {
-        auto* kernel = flags & TAOT_ROUTE_SIGMOID ? balance_backward_kernel<T, true, lanes.value, cpl.value>
-                                                  : balance_backward_kernel<T, false, lanes.value, cpl.value>;
-        kernel<<<(unsigned)(n * l.blocks), l.threads, 0, stream>>>(
+      bool fine = true;
+      with_layout(l, E, [&](auto lanes, auto cpl, auto full) {
+        auto* kernel = flags & TAOT_ROUTE_SIGMOID ? balance_backward_kernel<T, true, full.value, lanes.value, cpl.value>
+                                                  : balance_backward_kernel<T, false, full.value, lanes.value, cpl.value>;
+        fine = allow_lds(reinterpret_cast<const void*>(kernel), lds);
+        if (!fine) return;
+        kernel<<<(unsigned)(n * l.blocks), l.threads, lds, stream>>>(
             dloss + r, dz ? dz + r : nullptr, static_cast<const T*>(logits) + at * E, counts + r * E, counted + r,
             mask ? mask + at : nullptr, add ? static_cast<const T*>(add) + at * E : nullptr, s, l.each,
             static_cast<T*>(dlogits) + at * E);
       });
-      return true;
+      return fine;
     });
+    if (!ok) return TAOT_ERR_LAUNCH;
   }
   return hipGetLastError() == hipSuccess ? TAOT_OK : TAOT_ERR_LAUNCH;
 }
