@@ -27,11 +27,11 @@ struct Tile {
 
 // Runs as they are worked on: [0, o_0), the given ones, [o_runs, M).  Offsets are
 // taken in [0, M], and each as at least the one before it.
-constexpr int kRunThreads = 1024;
+template <int kRunThreads>
 __global__ void __launch_bounds__(kRunThreads)
 runs_kernel(const int32_t* __restrict__ offsets, const int32_t* __restrict__ experts, int32_t runs, int32_t G, int64_t M,
             int32_t rows_of_tile, Tile* __restrict__ tiles, int32_t* __restrict__ total) {
-  __shared__ int32_t starts[kRunThreads + 1], firsts[kRunThreads + 1], part[16], whose[kRunThreads];
+  __shared__ int32_t starts[kRunThreads + 1], firsts[kRunThreads + 1], part[kRunThreads / kWave], whose[kRunThreads];
   const int tid = threadIdx.x, lane = tid % kWave, wid = tid / kWave;
   const int32_t V = runs + 2;
   int32_t start = 0, done = 0;  // of the next run, and tiles so far
@@ -84,16 +84,53 @@ runs_kernel(const int32_t* __restrict__ offsets, const int32_t* __restrict__ exp
   if (tid == 0) *total = done;
 }
 
-// Bytes k .. k + 15 of a row of K, zeros behind its end.
-__device__ __forceinline__ i32x4 bytes16(const int8_t* __restrict__ row, int32_t k, int32_t K) {
-  const int n = K - k;
-  if (n >= 16) return *reinterpret_cast<const i32x4_at*>(row + k);
-  i32x4 v = 0;
+// 16 P bytes of a row as the words that hold them.  SHIFT: they begin `shift` bytes
+// behind a word, and there is a word more (16 rows by 8192 channels of 8191: 69 us with
+// reads at the bytes' own addresses, 24 for 8192).  What is loaded is not touched before
+// it is needed, so that it may be on its way.
+template <bool SHIFT, int P>
+struct Words {
+  i32x4 w[P];
+  int last;
+  __device__ __forceinline__ void load(const int8_t* __restrict__ from, uint32_t shift) {
+    const int8_t* const at = from - (SHIFT ? shift : 0);
 #pragma unroll
-  for (int u = 0; u < 16; ++u)
-    if (u < n) v[u / 4] |= (int)((uint32_t)(uint8_t)row[k + u] << (8 * (u % 4)));
-  return v;
-}
+    for (int s = 0; s < P; ++s) w[s] = *reinterpret_cast<const i32x4_at*>(at + 16 * s);
+    if (SHIFT) last = *reinterpret_cast<const int*>(at + 16 * P);
+  }
+  // The words that hold one of the next n bytes of the row, zeros for others.
+  __device__ __forceinline__ void load_end(const int8_t* __restrict__ from, uint32_t shift, int n) {
+    const int* const at = reinterpret_cast<const int*>(from - (SHIFT ? shift : 0));
+    const int m = n > 0 ? n + (SHIFT ? (int)shift : 0) : 0;
+#pragma unroll
+    for (int u = 0; u < 4 * P; ++u) {
+      w[u / 4][u % 4] = 0;
+      if (4 * u < m) w[u / 4][u % 4] = at[u];
+    }
+    last = 0;
+    if (SHIFT && 16 * P < m) last = at[4 * P];
+  }
+  __device__ __forceinline__ i32x4 bytes(int s, uint32_t shift) const {
+    if constexpr (!SHIFT) return w[s];
+    i32x4 v;
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int next = u < 3 ? w[s][u + 1] : s < P - 1 ? w[s + 1 < P ? s + 1 : s][0] : last;
+      v[u] = (int)__builtin_amdgcn_alignbyte((uint32_t)next, (uint32_t)w[s][u], shift);
+    }
+    return v;
+  }
+  // As many as n of them, zeros behind.
+  __device__ __forceinline__ i32x4 bytes_end(int s, uint32_t shift, int n) const {
+    i32x4 v = bytes(s, shift);
+    if constexpr (SHIFT) {
+#pragma unroll
+      for (int u = 0; u < 4; ++u) v[u] &= (int)((1ull << (8 * min(max(n - 16 * s - 4 * u, 0), 4))) - 1);
+    }
+    return v;
+  }
+};
+__device__ __forceinline__ uint32_t within_word(const int8_t* p) { return (uint32_t)reinterpret_cast<uintptr_t>(p) & 3; }
 
 // A sum with its scales, rounded to a float: without the empty statement the last
 // product and the rounding to 16 bits become one instruction in some kernels and not in
@@ -138,16 +175,19 @@ __device__ __forceinline__ Tile tile_of(const Work& w, int32_t i, int64_t M, int
 // Which tiles a block works on, and in which order.  Blocks go to the eight dies in
 // turn; a die gets a contiguous part of the tiles, in groups of kGroup tiles of rows
 // by all channels, so that what its blocks read at a time is near a square and is
-// found in its L2 cache.
+// found in its L2 cache.  Or all blocks take the tiles in order: where each weight is
+// read by one block, memory is read from one end to the other (64 rows of 128 runs, 31
+// of them not empty, 2048 x 2048: 28 us, 35 by dies).
+constexpr int kStep = 128;  // bytes of the inner dimension that a step has
 constexpr int kDies = 8, kGroup = 4, kUnits = 256;  // compute units
 struct Walk {
-  int64_t all, at, end, step;  // all tiles by channels, and the block's part of them
-  int32_t across, tiles;
-  __device__ __forceinline__ Walk(const Work& w, int32_t most, int32_t N, int bn) {
+  int64_t at, end, step;  // the block's part of the tiles by channels
+  int32_t across, tiles, group;
+  __device__ __forceinline__ Walk(const Work& w, int32_t most, int32_t N, int bn, int32_t of_group = kGroup)
+      : group(of_group) {
     across = (N + bn - 1) / bn;
     tiles = w.tiles ? __builtin_amdgcn_readfirstlane(min(*w.total, most)) : most;
-    all = (int64_t)tiles * across;
-    const int64_t per = (all + kDies - 1) / kDies, die = blockIdx.x % kDies;
+    const int64_t all = (int64_t)tiles * across, per = (all + kDies - 1) / kDies, die = blockIdx.x % kDies;
     at = die * per + blockIdx.x / kDies;
     end = min(die * per + per, all);
     step = gridDim.x / kDies;
@@ -155,123 +195,13 @@ struct Walk {
   __device__ __forceinline__ bool more() const { return at < end; }
   // The tile of rows and the tile of channels.
   __device__ __forceinline__ int32_t place(int32_t& channels) const {
-    const int64_t group = at / (kGroup * (int64_t)across);
-    const int32_t in = (int32_t)(at - group * kGroup * across), first = (int32_t)group * kGroup;
-    const int32_t rows = min(kGroup, tiles - first);
+    const int64_t which = at / (group * (int64_t)across);
+    const int32_t in = (int32_t)(at - which * group * across), first = (int32_t)which * group;
+    const int32_t rows = min(group, tiles - first);
     channels = in / rows;
     return first + in % rows;
   }
 };
-
-// BN channels by BM rows of a tile, by WN x WM waves; kStep bytes of the inner
-// dimension at a time, the next ones on their way in registers while the present
-// ones are worked on out of LDS.  16-byte pieces of a row of LDS change places by
-// the row's number, so that lanes of neighbouring rows read other banks.
-constexpr int kStep = 128;
-template <typename T, int BN, int BM, int WN, int WM>
-__global__ void __launch_bounds__(kWave * WN * WM)
-product_kernel(ProductArgs p, Work work, int32_t most) {
-  constexpr int kThreads = kWave * WN * WM, TN = BN / WN / 32, TM = BM / WM / 32, kPieces = kStep / 16;
-  constexpr int LN = BN * kPieces / kThreads, LM = BM * kPieces / kThreads;
-  extern __shared__ i32x4 room[];
-  const int tid = threadIdx.x, lane = tid % kWave, wid = tid / kWave;
-  const int wn = wid % WN * (BN / WN), wm = wid / WN * (BM / WM);
-  T* const out = static_cast<T*>(p.out);
-  for (Walk walk(work, most, p.N, BN); walk.more(); walk.at += walk.step) {
-    int32_t channels;
-    const Tile t = tile_of(work, walk.place(channels), p.M, BM);
-    const int32_t n0 = channels * BN;
-    if (t.expert < 0) {
-      const int32_t wide = min(BN, p.N - n0);
-      for (int32_t i = tid; i < t.rows * BN; i += kThreads)
-        if (i % BN < wide) out[(int64_t)(t.row + i / BN) * p.N + n0 + i % BN] = (T)0.f;
-      continue;
-    }
-    const int8_t* const W = p.weight + (int64_t)t.expert * p.N * p.K;
-    const int8_t *from_n[LN], *from_m[LM];
-    int to_n[LN], to_m[LM];
-    const int piece = tid % kPieces;
-#pragma unroll
-    for (int i = 0; i < LN; ++i) {
-      const int r = tid / kPieces + i * (kThreads / kPieces);
-      from_n[i] = W + (int64_t)min(n0 + r, p.N - 1) * p.K;
-      to_n[i] = r * kPieces + (piece ^ (r % kPieces));
-    }
-#pragma unroll
-    for (int i = 0; i < LM; ++i) {
-      const int r = tid / kPieces + i * (kThreads / kPieces);
-      from_m[i] = p.x + (int64_t)(t.row + min(r, t.rows - 1)) * p.K;
-      to_m[i] = BN * kPieces + r * kPieces + (piece ^ (r % kPieces));
-    }
-    i32x4 next_n[LN], next_m[LM];
-    auto fetch = [&](int32_t k) {
-#pragma unroll
-      for (int i = 0; i < LN; ++i) next_n[i] = bytes16(from_n[i], k + 16 * piece, p.K);
-#pragma unroll
-      for (int i = 0; i < LM; ++i) next_m[i] = bytes16(from_m[i], k + 16 * piece, p.K);
-    };
-    auto put = [&](i32x4* to) {
-#pragma unroll
-      for (int i = 0; i < LN; ++i) to[to_n[i]] = next_n[i];
-#pragma unroll
-      for (int i = 0; i < LM; ++i) to[to_m[i]] = next_m[i];
-    };
-    i32x16 acc[TN][TM];
-#pragma unroll
-    for (int i = 0; i < TN; ++i)
-#pragma unroll
-      for (int j = 0; j < TM; ++j) acc[i][j] = 0;
-    fetch(0);
-    put(room);
-    __syncthreads();
-    int buf = 0;
-    for (int32_t k = 0; k < p.K; k += kStep, buf ^= 1) {
-      const i32x4* const lds = room + buf * (BN + BM) * kPieces;
-      const bool more = k + kStep < p.K;
-      if (more) fetch(k + kStep);
-#pragma unroll
-      for (int s = 0; s < kStep / 32; ++s) {
-        i32x4 a[TN], b[TM];
-        const int c = 2 * s + lane / 32;
-#pragma unroll
-        for (int i = 0; i < TN; ++i) {
-          const int r = wn + 32 * i + lane % 32;
-          a[i] = lds[r * kPieces + (c ^ (r % kPieces))];
-        }
-#pragma unroll
-        for (int j = 0; j < TM; ++j) {
-          const int r = wm + 32 * j + lane % 32;
-          b[j] = lds[BN * kPieces + r * kPieces + (c ^ (r % kPieces))];
-        }
-#pragma unroll
-        for (int i = 0; i < TN; ++i)
-#pragma unroll
-          for (int j = 0; j < TM; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(a[i], b[j], acc[i][j], 0, 0, 0);
-      }
-      if (more) put(room + (buf ^ 1) * (BN + BM) * kPieces);
-      __syncthreads();
-    }
-    const float* const sw = p.weight_scale + (int64_t)t.expert * p.N;
-#pragma unroll
-    for (int j = 0; j < TM; ++j) {
-      const int m = wm + 32 * j + lane % 32;
-      if (m >= t.rows) continue;
-      const float sx = p.scale[t.row + m];
-      T* const to = out + (int64_t)(t.row + m) * p.N;
-#pragma unroll
-      for (int i = 0; i < TN; ++i)
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          const int32_t n = n0 + wn + 32 * i + 8 * q + 4 * (lane / 32);
-          if (n >= p.N) continue;
-          float v[4];
-#pragma unroll
-          for (int u = 0; u < 4; ++u) v[u] = scaled(acc[i][j][4 * q + u], sx, sw[min(n + u, p.N - 1)]);
-          store4(to + n, v, p.N - n);
-        }
-    }
-  }
-}
 
 // 16 neighbouring channels of a row, of which the lane has 4 half .. + 3 and 8 + 4 half
 // .. + 3 and the lane 32 further the others.  16-bit values change lanes first, so
@@ -299,6 +229,175 @@ __device__ __forceinline__ void store16(T* p, const float (&v)[2][4], int half, 
   }
 }
 
+// The scales of a lane's channels and rows, and its results with them: TN x TM blocks of
+// 32 channels by 32 rows from channel n0 and row m0 of the tile.
+template <typename T, int TN, int TM>
+struct Results {
+  f32x4 sn[TN][4];
+  float sm[TM];
+  bool whole;
+  __device__ __forceinline__ void scales(const ProductArgs& p, const Tile& t, int32_t n0, int m0) {
+    const int lane = threadIdx.x % kWave;
+    const float* const sw = p.weight_scale + (int64_t)max(t.expert, 0) * p.N;
+    whole = n0 + 32 * TN <= p.N;
+#pragma unroll
+    for (int i = 0; i < TN; ++i)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const int32_t n = n0 + 32 * i + 8 * q + 4 * (lane / 32);
+        if (t.expert < 0) {
+          sn[i][q] = 0.f;
+        } else if (whole) {
+          sn[i][q] = *reinterpret_cast<const f32x4_at*>(sw + n);
+        } else {
+#pragma unroll
+          for (int u = 0; u < 4; ++u) sn[i][q][u] = sw[min(n + u, p.N - 1)];
+        }
+      }
+#pragma unroll
+    for (int j = 0; j < TM; ++j)
+      sm[j] = t.expert < 0 ? 0.f : p.scale[t.row + min(m0 + 32 * j + lane % 32, t.rows - 1)];
+  }
+  __device__ __forceinline__ void store(const ProductArgs& p, const Tile& t, int32_t n0, int m0,
+                                        const i32x16 (&acc)[TN][TM]) const {
+    const int lane = threadIdx.x % kWave;
+#pragma unroll
+    for (int j = 0; j < TM; ++j) {
+      const int m = m0 + 32 * j + lane % 32;
+      T* const to = static_cast<T*>(p.out) + (int64_t)(t.row + m) * p.N;
+#pragma unroll
+      for (int i = 0; i < TN; ++i)
+#pragma unroll
+        for (int q = 0; q < 4; q += 2) {
+          float v[2][4];
+#pragma unroll
+          for (int u = 0; u < 8; ++u) v[u / 4][u % 4] = scaled(acc[i][j][4 * q + u], sm[j], sn[i][q + u / 4][u % 4]);
+          const int32_t n = n0 + 32 * i + 8 * q;
+          if (whole) {
+            store16(to + n, v, lane / 32, m < t.rows);
+          } else if (m < t.rows) {
+            const int32_t at = n + 4 * (lane / 32);
+            if (at < p.N) store4(to + at, v[0], p.N - at);
+            if (at + 8 < p.N) store4(to + at + 8, v[1], p.N - at - 8);
+          }
+        }
+    }
+  }
+};
+
+// BN channels by BM rows of a tile, by WN x WM waves; kStep bytes of the inner
+// dimension at a time, those of the next AHEAD steps on their way in registers while
+// the present ones are worked on out of LDS.  16-byte pieces of a row of LDS change
+// places by the row's number, so that lanes of neighbouring rows read other banks.
+template <typename T, int BN, int BM, int WN, int WM, int AHEAD, bool SHIFT>
+__global__ void __launch_bounds__(kWave * WN * WM) __attribute__((amdgpu_waves_per_eu(AHEAD > 1 ? 3 : 2)))
+product_kernel(ProductArgs p, Work work, int32_t most) {
+  constexpr int kThreads = kWave * WN * WM, TN = BN / WN / 32, TM = BM / WM / 32, kPieces = kStep / 16;
+  constexpr int LN = BN * kPieces / kThreads, LM = BM * kPieces / kThreads;
+  extern __shared__ i32x4 room[];
+  const int tid = threadIdx.x, lane = tid % kWave, wid = tid / kWave;
+  const int wn = wid % WN * (BN / WN), wm = wid / WN * (BM / WM);
+  for (Walk walk(work, most, p.N, BN); walk.more(); walk.at += walk.step) {
+    int32_t channels;
+    const Tile t = tile_of(work, walk.place(channels), p.M, BM);
+    const int32_t n0 = channels * BN, K = t.expert < 0 ? 0 : p.K;
+    const int8_t* const W = p.weight + (int64_t)max(t.expert, 0) * p.N * p.K;
+    const int8_t *from_n[LN], *from_m[LM];
+    int to_n[LN], to_m[LM];
+    const int piece = tid % kPieces;
+#pragma unroll
+    for (int i = 0; i < LN; ++i) {
+      const int r = tid / kPieces + i * (kThreads / kPieces);
+      from_n[i] = W + (int64_t)min(n0 + r, p.N - 1) * p.K;
+      to_n[i] = r * kPieces + (piece ^ (r % kPieces));
+    }
+#pragma unroll
+    for (int i = 0; i < LM; ++i) {
+      const int r = tid / kPieces + i * (kThreads / kPieces);
+      from_m[i] = p.x + (int64_t)(t.row + min(r, t.rows - 1)) * p.K;
+      to_m[i] = BN * kPieces + r * kPieces + (piece ^ (r % kPieces));
+    }
+    Words<SHIFT, 1> next_n[AHEAD][LN], next_m[AHEAD][LM];
+    auto fetch = [&](int32_t k, int s) {
+      const int n = K - k - 16 * piece;
+      if (n >= (SHIFT ? 20 : 16)) {
+#pragma unroll
+        for (int i = 0; i < LN; ++i) next_n[s][i].load(from_n[i] + k + 16 * piece, within_word(from_n[i]));
+#pragma unroll
+        for (int i = 0; i < LM; ++i) next_m[s][i].load(from_m[i] + k + 16 * piece, within_word(from_m[i]));
+      } else {
+#pragma unroll
+        for (int i = 0; i < LN; ++i) next_n[s][i].load_end(from_n[i] + k + 16 * piece, within_word(from_n[i]), n);
+#pragma unroll
+        for (int i = 0; i < LM; ++i) next_m[s][i].load_end(from_m[i] + k + 16 * piece, within_word(from_m[i]), n);
+      }
+    };
+    auto put = [&](int32_t k, i32x4* to, int s) {
+      if (k + kStep <= K) {
+#pragma unroll
+        for (int i = 0; i < LN; ++i) to[to_n[i]] = next_n[s][i].bytes(0, within_word(from_n[i]));
+#pragma unroll
+        for (int i = 0; i < LM; ++i) to[to_m[i]] = next_m[s][i].bytes(0, within_word(from_m[i]));
+      } else {
+        const int n = K - k - 16 * piece;
+#pragma unroll
+        for (int i = 0; i < LN; ++i) to[to_n[i]] = next_n[s][i].bytes_end(0, within_word(from_n[i]), n);
+#pragma unroll
+        for (int i = 0; i < LM; ++i) to[to_m[i]] = next_m[s][i].bytes_end(0, within_word(from_m[i]), n);
+      }
+    };
+#pragma unroll
+    for (int s = 0; s < AHEAD; ++s) fetch(s * kStep, s);
+    Results<T, TN, TM> results;
+    if (AHEAD > 1) results.scales(p, t, n0 + wn, wm);
+    i32x16 acc[TN][TM];
+#pragma unroll
+    for (int i = 0; i < TN; ++i)
+#pragma unroll
+      for (int j = 0; j < TM; ++j) acc[i][j] = 0;
+    put(0, room, 0);
+    fetch(AHEAD * kStep, 0);
+    __syncthreads();
+    int buf = 0;
+    for (int32_t k0 = 0; k0 < K; k0 += AHEAD * kStep) {
+#pragma unroll
+      for (int u = 0; u < AHEAD; ++u) {
+        const int32_t k = k0 + u * kStep;
+        if (k >= K) break;
+        const i32x4* const lds = room + buf * (BN + BM) * kPieces;
+#pragma unroll
+        for (int s = 0; s < kStep / 32; ++s) {
+          i32x4 a[TN], b[TM];
+          const int c = 2 * s + lane / 32;
+#pragma unroll
+          for (int i = 0; i < TN; ++i) {
+            const int r = wn + 32 * i + lane % 32;
+            a[i] = lds[r * kPieces + (c ^ (r % kPieces))];
+          }
+#pragma unroll
+          for (int j = 0; j < TM; ++j) {
+            const int r = wm + 32 * j + lane % 32;
+            b[j] = lds[BN * kPieces + r * kPieces + (c ^ (r % kPieces))];
+          }
+#pragma unroll
+          for (int i = 0; i < TN; ++i)
+#pragma unroll
+            for (int j = 0; j < TM; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(a[i], b[j], acc[i][j], 0, 0, 0);
+        }
+        buf ^= 1;
+        if (k + kStep < K) {
+          put(k + kStep, room + buf * (BN + BM) * kPieces, (u + 1) % AHEAD);
+          fetch(k + (AHEAD + 1) * kStep, (u + 1) % AHEAD);
+        }
+        __syncthreads();
+      }
+    }
+    if (AHEAD == 1) results.scales(p, t, n0 + wn, wm);  // many results: no registers for them before
+    results.store(p, t, n0 + wn, wm, acc);
+    __syncthreads();  // a run of no expert waits nowhere else
+  }
+}
+
 // Many rows, whole 16-byte pieces: a wave on each SIMD holds 128 x 128 results, and
 // pieces go from memory to LDS without passing through registers.  The operands of
 // the next 32 bytes are read out of LDS while the present ones are multiplied, and
@@ -317,7 +416,6 @@ product_wide_kernel(ProductArgs p, Work work, int32_t most) {
   __shared__ i32x4 even[(kWideN + kWideM) * kPieces], odd[(kWideN + kWideM) * kPieces];
   const int tid = threadIdx.x, lane = tid % kWave, wid = __builtin_amdgcn_readfirstlane(tid / kWave);
   const int wn = wid % 2 * 128, wm = wid / 2 * 128;
-  T* const out = static_cast<T*>(p.out);
   // where this lane's operands lie in a step's room
   int at_n[4], at_m[4];
 #pragma unroll
@@ -368,8 +466,6 @@ product_wide_kernel(ProductArgs p, Work work, int32_t most) {
     int32_t next_n0 = n0;
     Tile next = t;
     if (more) next = look(next_n0);
-    const float* const sw = p.weight_scale + (int64_t)max(t.expert, 0) * p.N;
-    const bool whole = n0 + kWideN <= p.N;
     const int32_t K = t.expert < 0 ? 0 : p.K;
     i32x4 a[2][4], b[2][4];
     auto take = [&](const i32x4* lds, int s, int into, int i) {
@@ -420,47 +516,10 @@ product_wide_kernel(ProductArgs p, Work work, int32_t most) {
     __builtin_amdgcn_s_waitcnt(kAllLoads);
     const auto next_rows_n = buffer_n(next, next_n0), next_rows_m = buffer_m(next);
     if (more) begin(next_rows_n, next_rows_m);
-    f32x4 sn[4][4];
-    float sm[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-#pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        const int32_t n = n0 + wn + 32 * i + 8 * q + 4 * (lane / 32);
-        if (t.expert < 0) {
-          sn[i][q] = 0.f;
-        } else if (whole) {
-          sn[i][q] = *reinterpret_cast<const f32x4_at*>(sw + n);
-        } else {
-#pragma unroll
-          for (int u = 0; u < 4; ++u) sn[i][q][u] = sw[min(n + u, p.N - 1)];
-        }
-      }
-#pragma unroll
-    for (int j = 0; j < 4; ++j)
-      sm[j] = t.expert < 0 ? 0.f : p.scale[t.row + min(wm + 32 * j + lane % 32, t.rows - 1)];
+    Results<T, 4, 4> results;
+    results.scales(p, t, n0 + wn, wm);
     __builtin_amdgcn_s_waitcnt(kAllLoads);  // the next tile's pieces too, and not for the results that go now
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int m = wm + 32 * j + lane % 32;
-      T* const to = out + (int64_t)(t.row + m) * p.N;
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int q = 0; q < 4; q += 2) {
-          float v[2][4];
-#pragma unroll
-          for (int u = 0; u < 8; ++u) v[u / 4][u % 4] = scaled(acc[i][j][4 * q + u], sm[j], sn[i][q + u / 4][u % 4]);
-          const int32_t n = n0 + wn + 32 * i + 8 * q;
-          if (whole) {
-            store16(to + n, v, lane / 32, m < t.rows);
-          } else if (m < t.rows) {
-            const int32_t at = n + 4 * (lane / 32);
-            if (at < p.N) store4(to + at, v[0], p.N - at);
-            if (at + 8 < p.N) store4(to + at + 8, v[1], p.N - at - 8);
-          }
-        }
-    }
+    results.store(p, t, n0 + wn, wm, acc);
     t = next;
     n0 = next_n0;
     rows_n = next_rows_n;
@@ -468,77 +527,183 @@ product_wide_kernel(ProductArgs p, Work work, int32_t most) {
   }
 }
 
-// Few rows: all that counts is the weights' way from memory.  A block has 16
-// channels and up to 16 rows, its waves share the inner dimension; nothing passes
-// through LDS but the waves' sums.  A lane reads 32 neighbouring bytes of its row, a
-// wave whole lines of 128; which bytes meet in a step is the same for both operands.
-constexpr int kFewRows = 16, kFewWaves = 4, kFewAhead = 4;
-template <typename T>
+// A few rows of each run: tiles of 16 rows by 16 channels, whose four waves share the
+// inner dimension.  A lane reads 32 neighbouring bytes of its row, a wave whole lines.
+constexpr int kFewRows = 16, kFewN = 16, kFewWaves = 4, kFewAhead = 4;
+template <typename T, bool SHIFT>
 __global__ void __launch_bounds__(kWave * kFewWaves)
 product_few_kernel(ProductArgs p, Work work, int32_t most) {
-  __shared__ i32x4 part[kFewWaves][kWave];
-  const int lane = threadIdx.x % kWave, wid = threadIdx.x / kWave;
-  const int32_t across = (p.N + 15) / 16;
-  const int64_t all = (int64_t)(work.tiles ? min(*work.total, most) : most) * across;
-  T* const out = static_cast<T*>(p.out);
-  for (int64_t at = blockIdx.x; at < all; at += gridDim.x) {
-    const Tile t = tile_of(work, (int32_t)(at / across), p.M, kFewRows);
-    const int32_t n0 = (int32_t)(at % across) * 16;
+  __shared__ i32x4 part[2][kFewWaves][kWave];
+  const int lane = threadIdx.x % kWave, wid = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  int slot = 0;
+  for (Walk walk(work, most, p.N, kFewN, 1); walk.more(); walk.at += walk.step, slot ^= 1) {
+    int32_t channels;
+    const Tile t = tile_of(work, walk.place(channels), p.M, kFewRows);
+    const int32_t n0 = channels * kFewN, n = n0 + lane / 16 * 4, K = t.expert < 0 ? 0 : p.K;
+    const int m = min(lane % 16, t.rows - 1);
+    const int8_t* const w = p.weight + ((int64_t)max(t.expert, 0) * p.N + min(n0 + lane % 16, p.N - 1)) * p.K;
+    const int8_t* const x = p.x + (int64_t)(t.row + m) * p.K;
+    const uint32_t shift_w = within_word(w), shift_x = within_word(x);
+    constexpr int32_t kAll = kStep * kFewWaves, kNeeds = kStep + (SHIFT ? 4 : 0);
+    const int32_t mine = lane / 16 * 32;
     i32x4 acc = 0;
-    if (t.expert >= 0) {
-      const int8_t* const w = p.weight + ((int64_t)t.expert * p.N + min(n0 + lane % 16, p.N - 1)) * p.K;
-      const int8_t* const x = p.x + (int64_t)(t.row + min(lane % 16, t.rows - 1)) * p.K;
-      int32_t k = wid * kStep;
-      constexpr int32_t kAll = kStep * kFewWaves;
-      const int32_t mine = lane / 16 * 32;
-      for (; k + (kFewAhead - 1) * kAll + kStep <= p.K; k += kFewAhead * kAll) {
-        i32x4 a[kFewAhead][2], b[kFewAhead][2];
+    Words<SHIFT, 2> a[kFewAhead], b[kFewAhead];
+    auto fetch = [&](int32_t k, int u) {
+      if (k + kNeeds > K) return;
+      a[u].load(w + k + mine, shift_w);
+      b[u].load(x + k + mine, shift_x);
+    };
+    int32_t k = wid * kStep;
 #pragma unroll
-        for (int u = 0; u < kFewAhead; ++u)
+    for (int u = 0; u < kFewAhead; ++u) fetch(k + u * kAll, u);
+    float sx = 0.f, sn[4] = {};
+    if (wid == 0 && t.expert >= 0) {
+      sx = p.scale[t.row + m];
 #pragma unroll
-          for (int s = 0; s < 2; ++s) a[u][s] = *reinterpret_cast<const i32x4_at*>(w + k + u * kAll + mine + 16 * s);
+      for (int u = 0; u < 4; ++u) sn[u] = p.weight_scale[(int64_t)t.expert * p.N + min(n + u, p.N - 1)];
+    }
+    while (k + kNeeds <= K) {
 #pragma unroll
-        for (int u = 0; u < kFewAhead; ++u)
-#pragma unroll
-          for (int s = 0; s < 2; ++s) b[u][s] = *reinterpret_cast<const i32x4_at*>(x + k + u * kAll + mine + 16 * s);
-#pragma unroll
-        for (int u = 0; u < kFewAhead; ++u)
-#pragma unroll
-          for (int s = 0; s < 2; ++s) acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(a[u][s], b[u][s], acc, 0, 0, 0);
-      }
-      for (; k < p.K; k += kAll)
+      for (int u = 0; u < kFewAhead; ++u) {
+        if (k + kNeeds > K) break;
 #pragma unroll
         for (int s = 0; s < 2; ++s)
-          acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(bytes16(w, k + mine + 16 * s, p.K), bytes16(x, k + mine + 16 * s, p.K),
-                                                      acc, 0, 0, 0);
-    }
-    part[wid][lane] = acc;
-    __syncthreads();
-    const int m = lane % 16;
-    if (wid == 0 && m < t.rows) {
-#pragma unroll
-      for (int w = 1; w < kFewWaves; ++w) acc += part[w][lane];
-      const int32_t n = n0 + lane / 16 * 4;
-      if (n < p.N) {
-        const float sx = t.expert >= 0 ? p.scale[t.row + m] : 0.f;
-        float v[4];
-#pragma unroll
-        for (int u = 0; u < 4; ++u)
-          v[u] = t.expert >= 0 ? scaled(acc[u], sx, p.weight_scale[(int64_t)t.expert * p.N + min(n + u, p.N - 1)]) : 0.f;
-        store4(out + (int64_t)(t.row + m) * p.N + n, v, p.N - n);
+          acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(a[u].bytes(s, shift_w), b[u].bytes(s, shift_x), acc, 0, 0, 0);
+        fetch(k + kFewAhead * kAll, u);
+        k += kAll;
       }
+    }
+    if (k < K) {  // the row's end: one wave has it
+      const int left = K - k - mine;
+      a[0].load_end(w + k + mine, shift_w, left);
+      b[0].load_end(x + k + mine, shift_x, left);
+#pragma unroll
+      for (int s = 0; s < 2; ++s)
+        acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(a[0].bytes_end(s, shift_w, left), b[0].bytes_end(s, shift_x, left), acc, 0, 0, 0);
+    }
+    part[slot][wid][lane] = acc;
+    __syncthreads();  // the two sets of sums take turns
+    if (wid == 0 && lane % 16 < t.rows && n < p.N) {
+#pragma unroll
+      for (int i = 1; i < kFewWaves; ++i) acc += part[slot][i][lane];
+      float v[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) v[u] = scaled(acc[u], sx, sn[u]);
+      store4(static_cast<T*>(p.out) + (int64_t)(t.row + m) * p.N + n, v, p.N - n);
+    }
+  }
+}
+
+// Fewer rows than fill the matrix units: all that counts is the weights' way from
+// memory.  A block has 32 channels and up to 32 TM rows, and its waves share the inner
+// dimension: operands go from memory to registers, the next step's while the present
+// one's are multiplied, and meet as sums in LDS, which are whole numbers and have no
+// order.  A lane reads 64 neighbouring bytes of its row, a wave whole lines of 128 of
+// each; which bytes meet in a product is the same for both operands.  Blocks of 32 rows
+// that a tile does not have are left out.
+constexpr int kSomeN = 32, kSomeWaves = 8, kSomeThreads = kSomeWaves * kWave;
+
+template <typename T, int TM, bool SHIFT>
+__global__ void __launch_bounds__(kSomeThreads)
+product_some_kernel(ProductArgs p, Work work, int32_t most) {
+  constexpr int kRows = 32 * TM, kPitch = kRows + 1, kTasks = kRows * kSomeN / 4, kMine = (kTasks + kSomeThreads - 1) / kSomeThreads;
+  __shared__ int sum[kSomeN * kPitch];
+  const int tid = threadIdx.x, lane = tid % kWave, wid = __builtin_amdgcn_readfirstlane(tid / kWave);
+  for (Walk walk(work, most, p.N, kSomeN); walk.more(); walk.at += walk.step) {
+    int32_t channels;
+    const Tile t = tile_of(work, walk.place(channels), p.M, kRows);
+    const int32_t n0 = channels * kSomeN, K = t.expert < 0 ? 0 : p.K;
+    const int8_t* const w = p.weight + ((int64_t)max(t.expert, 0) * p.N + min(n0 + lane % 32, p.N - 1)) * p.K;
+    const int8_t* x[TM];
+#pragma unroll
+    for (int j = 0; j < TM; ++j) x[j] = p.x + (int64_t)(t.row + min(32 * j + lane % 32, t.rows - 1)) * p.K;
+    const int32_t mine = 64 * (lane / 32);
+    const uint32_t shift_w = within_word(w);
+    uint32_t shift_x[TM];
+#pragma unroll
+    for (int j = 0; j < TM; ++j) shift_x[j] = within_word(x[j]);
+    Words<SHIFT, 4> a, b[TM], next_a, next_b[TM];
+    auto fetch = [&](int32_t k, Words<SHIFT, 4>& to_a, Words<SHIFT, 4>(&to_b)[TM]) {
+      to_a.load(w + k + mine, shift_w);
+#pragma unroll
+      for (int j = 0; j < TM; ++j)
+        if (32 * j < t.rows) to_b[j].load(x[j] + k + mine, shift_x[j]);
+    };
+    constexpr int32_t kAll = kStep * kSomeWaves, kNeeds = kStep + (SHIFT ? 4 : 0);
+    int32_t k = wid * kStep;
+    if (k + kNeeds <= K) fetch(k, a, b);
+    // the results that this thread gives: four channels of a row each
+    const int32_t n = n0 + tid % 8 * 4;
+    float sx[kMine], sn[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+      sn[u] = t.expert < 0 ? 0.f : p.weight_scale[(int64_t)t.expert * p.N + min(n + u, p.N - 1)];
+#pragma unroll
+    for (int i = 0; i < kMine; ++i)
+      sx[i] = t.expert < 0 ? 0.f : p.scale[t.row + min((tid + i * kSomeThreads) / 8, t.rows - 1)];
+    for (int i = tid; i < kSomeN * kPitch; i += kSomeThreads) sum[i] = 0;
+    i32x16 acc[TM];
+#pragma unroll
+    for (int j = 0; j < TM; ++j) acc[j] = 0;
+    __syncthreads();
+    for (; k + kNeeds <= K; k += kAll) {
+      if (k + kAll + kNeeds <= K) fetch(k + kAll, next_a, next_b);
+#pragma unroll
+      for (int s = 0; s < 4; ++s) {
+        const i32x4 ws = a.bytes(s, shift_w);
+#pragma unroll
+        for (int j = 0; j < TM; ++j)
+          if (32 * j < t.rows)
+            acc[j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(ws, b[j].bytes(s, shift_x[j]), acc[j], 0, 0, 0);
+      }
+      a = next_a;
+#pragma unroll
+      for (int j = 0; j < TM; ++j) b[j] = next_b[j];
+    }
+    if (k < K) {  // the row's end: one wave has it
+      const int left = K - k - mine;
+      a.load_end(w + k + mine, shift_w, left);
+#pragma unroll
+      for (int j = 0; j < TM; ++j)
+        if (32 * j < t.rows) {
+          b[j].load_end(x[j] + k + mine, shift_x[j], left);
+#pragma unroll
+          for (int s = 0; s < 4; ++s)
+            acc[j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(a.bytes_end(s, shift_w, left), b[j].bytes_end(s, shift_x[j], left),
+                                                           acc[j], 0, 0, 0);
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < TM; ++j)
+      if (32 * j < t.rows)
+#pragma unroll
+        for (int q = 0; q < 16; ++q) {
+          const int c = 8 * (q / 4) + 4 * (lane / 32) + q % 4;
+          __hip_atomic_fetch_add(&sum[c * kPitch + 32 * j + lane % 32], acc[j][q], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+        }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kMine; ++i) {
+      const int m = (tid + i * kSomeThreads) / 8;
+      if (m >= t.rows || n >= p.N) continue;
+      float v[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) v[u] = scaled(sum[(tid % 8 * 4 + u) * kPitch + m], sx[i], sn[u]);
+      store4(static_cast<T*>(p.out) + (int64_t)(t.row + m) * p.N + n, v, p.N - n);
     }
     __syncthreads();
   }
 }
 
-// Rows of a tile, by how many a run has on average.
-enum Kind { kFew, kMiddle, kLarge };
-Kind kind_of(int64_t M, int32_t runs) {
-  const int64_t each = M / (runs > 0 ? runs : 1);
-  return each <= 16 ? kFew : each < 128 ? kMiddle : kLarge;
+enum Kind { kFew, kSome, kMiddle, kLarge };
+Kind kind_of(int64_t M, int32_t N, int32_t runs) {
+  const int64_t sets = runs > 0 ? runs : 1, each = M / sets;
+  auto tiles = [&](int rows, int channels) { return (M / rows + sets) * ((N + channels - 1) / channels); };
+  if (each <= kFewRows) return kFew;
+  if (each >= 64 && tiles(256, 256) >= 96) return kLarge;
+  return tiles(64, 128) <= 128 ? kSome : kMiddle;
 }
-int32_t rows_of(Kind k) { return k == kFew ? kFewRows : k == kMiddle ? 64 : 256; }
+int32_t rows_of(Kind k) { return k == kFew ? kFewRows : k == kSome ? 64 : k == kMiddle ? 64 : 256; }
 
 // Tiles of all runs, at most.
 int64_t most_tiles(int64_t M, int32_t runs, bool listed, int32_t rows) {
@@ -548,7 +713,7 @@ int64_t most_tiles(int64_t M, int32_t runs, bool listed, int32_t rows) {
 
 template <typename T>
 taot_status product(const ProductArgs& p, void* ws, hipStream_t stream) {
-  const Kind kind = kind_of(p.M, p.runs);
+  const Kind kind = kind_of(p.M, p.N, p.runs);
   const int32_t rows = rows_of(kind);
   const int64_t most = most_tiles(p.M, p.runs, p.offsets, rows);
   Work work{nullptr, nullptr};
@@ -556,7 +721,9 @@ taot_status product(const ProductArgs& p, void* ws, hipStream_t stream) {
     Carver c{static_cast<char*>(ws)};
     int32_t* total = c.take<int32_t>(1);
     Tile* tiles = c.take<Tile>((size_t)most);
-    runs_kernel<<<1, kRunThreads, 0, stream>>>(p.offsets, p.experts, p.runs, p.G, p.M, rows, tiles, total);
+    // a block of 256 starts and ends sooner
+    auto* kernel = p.runs + 2 <= 256 ? runs_kernel<256> : runs_kernel<1024>;
+    kernel<<<1, p.runs + 2 <= 256 ? 256 : 1024, 0, stream>>>(p.offsets, p.experts, p.runs, p.G, p.M, rows, tiles, total);
     work = Work{tiles, total};
   }
   auto go = [&](auto* kernel, int bn, int threads, size_t lds, int64_t most_blocks = kMaxBlocks) {
@@ -566,11 +733,16 @@ taot_status product(const ProductArgs& p, void* ws, hipStream_t stream) {
     return true;
   };
   bool ok;
-  if (kind == kFew) ok = go(product_few_kernel<T>, 16, kWave * kFewWaves, 0);
-  else if (kind == kMiddle) ok = go(product_kernel<T, 128, 64, 2, 2>, 128, 256, 2 * (128 + 64) * kStep);
+  const bool words = (p.K | (int32_t)reinterpret_cast<uintptr_t>(p.x) | (int32_t)reinterpret_cast<uintptr_t>(p.weight)) % 4 == 0;
+  if (kind == kFew)
+    ok = go(words ? product_few_kernel<T, false> : product_few_kernel<T, true>, kFewN, kWave * kFewWaves, 0);
+  else if (kind == kSome)
+    ok = go(words ? product_some_kernel<T, 2, false> : product_some_kernel<T, 2, true>, kSomeN, kSomeThreads, 0);
+  else if (kind == kMiddle)
+    ok = go(words ? product_kernel<T, 128, 64, 2, 2, 2, false> : product_kernel<T, 128, 64, 2, 2, 2, true>, 128, 256, 2 * (128 + 64) * kStep);
   else if (p.K % 16 == 0 && reinterpret_cast<uintptr_t>(p.x) % 16 == 0 && reinterpret_cast<uintptr_t>(p.weight) % 16 == 0)
     ok = go(product_wide_kernel<T>, kWideN, kWideThreads, 0, kUnits);
-  else ok = go(product_kernel<T, 256, 256, 2, 4>, 256, 512, 2 * (256 + 256) * kStep);
+  else ok = go(words ? product_kernel<T, 256, 256, 2, 4, 1, false> : product_kernel<T, 256, 256, 2, 4, 1, true>, 256, 512, 2 * (256 + 256) * kStep);
   return ok && hipGetLastError() == hipSuccess ? TAOT_OK : TAOT_ERR_LAUNCH;
 }
 
@@ -579,7 +751,7 @@ taot_status product(const ProductArgs& p, void* ws, hipStream_t stream) {
 size_t matmul_i8_ws(int64_t M, int32_t runs) {
   Carver c{nullptr};
   c.take<int32_t>(1);
-  c.take<Tile>((size_t)most_tiles(M, runs, true, rows_of(kind_of(M, runs))));
+  c.take<Tile>((size_t)most_tiles(M, runs, true, rows_of(kFew)));  // the smallest tiles: the number of channels is not known
   return c.off;
 }
 
