@@ -39,15 +39,6 @@ struct Group {
   }
 };
 
-// exp(x) for x in [-150, 88]: the hardware's power of two of t = x log2(e), and what t's rounding takes away, which is
-// the larger part of the error for |x| above 1: 2^t (1 + (x - t ln 2)).
-__device__ __forceinline__ float exponential(float x) {
-  const float t = x * 1.44269504f, e = __builtin_amdgcn_exp2f(t);
-  return fmaf(e, fmaf(-t, 0.693147181f, x), e);
-}
-// x within [lo, hi], lo where it is NaN.
-__device__ __forceinline__ float within(float x, float lo, float hi) { return __builtin_amdgcn_fmed3f(x, lo, hi); }
-
 // FULL: all columns of the lanes are experts.
 template <bool SIGMOID, bool FULL, int L, int CPL>
 __device__ __forceinline__ void scores(Group<L>& g, int32_t E, f32x8 (&v)[CPL], float& total, float& lse, float& inv) {

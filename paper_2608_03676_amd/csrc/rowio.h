@@ -143,6 +143,16 @@ __device__ __forceinline__ float block_max(float v, int lanes) {
   return v;
 }
 
+// ---- functions ----------------------------------------------------------------
+// exp(x) for x in [-150, 88]: the hardware's power of two of t = x log2(e), and what t's rounding takes away, which is
+// the larger part of the error for |x| above 1: 2^t (1 + (x - t ln 2)).
+__device__ __forceinline__ float exponential(float x) {
+  const float t = x * 1.44269504f, e = __builtin_amdgcn_exp2f(t);
+  return fmaf(e, fmaf(-t, 0.693147181f, x), e);
+}
+// x within [lo, hi], lo where it is NaN.
+__device__ __forceinline__ float within(float x, float lo, float hi) { return __builtin_amdgcn_fmed3f(x, lo, hi); }
+
 // ---- rows held by waves -------------------------------------------------------
 constexpr int kRowsOfBlock = 4;  // where a wave holds a row
 
