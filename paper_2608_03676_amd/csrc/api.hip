@@ -276,7 +276,7 @@ taot_status taot_block_norm(const void* x, const void* residual, const void* pos
     return TAOT_ERR_INVALID_ARG;
   if (H > TAOT_MAX_WIDTH || T > kMaxGrid) return TAOT_ERR_UNSUPPORTED;
   if (T == 0) return TAOT_OK;
-  if (!x || !residual || (weight && !y)) return TAOT_ERR_INVALID_ARG;
+  if (!x || !residual) return TAOT_ERR_INVALID_ARG;
   return launch_block_norm(BlockNormArgs{x, residual, post, gate, weight, T, gate ? gates : 1, H, weight_dtype == TAOT_F32,
                                          gate_dtype == TAOT_F32, eps, alpha, h, y, rstd_x, rstd_h},
                            dtype, static_cast<hipStream_t>(stream));

@@ -378,7 +378,8 @@ balance_backward_kernel(const float* __restrict__ dloss, const float* __restrict
       for (int u = 0; u < 8; ++u) dot = fmaf(c[u], v[i][u], dot);
     }
     dot = g.reduce(dot, SumOp()) * inv * f;
-    const float up = SIGMOID ? dot : dot - fz * lse, each_p = now ? inv : 0.f;
+    // finite, so that experts of p = 0 get 0
+    const float up = SIGMOID ? dot : dot - within(fz * lse, -FLT_MAX, FLT_MAX), each_p = now ? inv : 0.f;
 #pragma unroll
     for (int i = 0; i < CPL; ++i) {
       const int col = 8 * (i * g.lanes + g.lane), m = t >= hi ? 0 : FULL ? 8 : s.E - col;

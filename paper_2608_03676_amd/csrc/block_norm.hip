@@ -76,7 +76,7 @@ block_norm_kernel(const T* x, const T* residual, Vector post, Vector gate, int64
 #pragma unroll
   for (int i = 0; i < CPL; ++i) {
     const int col = 8 * (i * lanes + lane), n = H - col;
-    store_row<FAR>(y + at + col, v[i] * b * factor<T>(weight, col, n), n);
+    if (y) store_row<FAR>(y + at + col, v[i] * b * factor<T>(weight, col, n), n);
   }
 }
 

@@ -529,7 +529,7 @@ product_wide_kernel(ProductArgs p, Work work, int32_t most) {
 
 // A few rows of each run: tiles of 16 rows by 16 channels, whose four waves share the
 // inner dimension.  A lane reads 32 neighbouring bytes of its row, a wave whole lines.
-constexpr int kFewRows = 16, kFewN = 16, kFewWaves = 4, kFewAhead = 4;
+constexpr int kFewRows = 16, kFewN = 16, kFewWaves = 4, kFewAhead = 2;
 template <typename T, bool SHIFT>
 __global__ void __launch_bounds__(kWave * kFewWaves)
 product_few_kernel(ProductArgs p, Work work, int32_t most) {

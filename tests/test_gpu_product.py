@@ -177,6 +177,42 @@ def test_offsets_that_are_wrong(gpu):
         _grouped(gpu, M, 70, 100, 2, [0, 20, 10, 30, M], [0, 1, 0, 2 ** 31 - 1])
 
 
+# Tiles of 256 by 256 (from 96 of them and 64 rows a run on), with pieces straight to LDS where rows begin at multiples
+# of 16 bytes and by way of registers where they do not.
+@pytest.mark.parametrize("K", [16, 128, 144, 256, 400, 1024, 1, 17, 132, 333])
+@pytest.mark.parametrize("dtype", TYPES)
+def test_many_tiles_of_many_rows(gpu, K, dtype):
+    print(f"[large] {dtype} K {K}", flush=True)
+    x, sx, w, sw = _operands(gpu, 4000, 1601, K)
+    out = taot.matmul_i8(x, sx, w, sw, dtype=dtype)
+    assert _near(out, _dense(x, sx, w, sw))
+    assert torch.equal(taot.matmul_i8(_shifted(x, 3), sx, _shifted(w, 5), sw, dtype=dtype), out)
+    g = torch.Generator().manual_seed(K)
+    sizes = torch.randint(0, 200, (40,), generator=g)
+    sizes[7], sizes[8], sizes[9] = 256, 257, 511
+    offsets = [3] + (3 + sizes.cumsum(0)).tolist()
+    experts = torch.randint(-1, 4, (40,), generator=g).tolist()
+    _grouped(gpu, offsets[-1] + 30, 520, K, 3, offsets, experts, dtype)
+
+
+# Tiles of 64 rows by 128 channels (from 129 of them on), and fewer, whose waves share the inner dimension.
+@pytest.mark.parametrize("K", [4, 64, 128, 255, 256, 388, 1024, 1030, 2050, 1, 131])
+def test_middling_runs(gpu, K):
+    for M, N in ((2000, 600), (2001, 521), (100, 512), (33, 70)):
+        for dtype in (torch.bfloat16, torch.float32):
+            x, sx, w, sw = _operands(gpu, M, N, K)
+            out = taot.matmul_i8(x, sx, w, sw, dtype=dtype)
+            assert _near(out, _dense(x, sx, w, sw)), (M, N)
+            assert torch.equal(taot.matmul_i8(_shifted(x, 1), sx, _shifted(w, 2), sw, dtype=dtype), out), (M, N)
+    _grouped(gpu, 1250, 700, K, 24, [0, 466, 655, 767, 844, 901, 946, 984] + list(range(1000, 1170, 10)))
+    _grouped(gpu, 300, 100, K, 2, [10, 150, 290], [1, 0])
+
+
+def test_wrong_offsets_of_large_runs(gpu):
+    M = 9000
+    _grouped(gpu, M, 520, 48, 40, [-7, 300, 200, 5000, 4000, 10 ** 9, 5] + [6000 + 75 * i for i in range(34)])
+
+
 @pytest.mark.parametrize("runs", [1022, 1023, 1024, 1025, 3000])
 def test_many_runs(gpu, runs):
     g = torch.Generator().manual_seed(runs)

@@ -41,7 +41,7 @@ def product(x=P, s=P, w=P, ws_=P, off=P, e=P, M=4, N=8, K=16, runs=2, G=2, dt=0,
 @pytest.mark.parametrize("call,code,cases", [
     (block_norm, 1, [dict(T=-1), dict(H=0), dict(dt=3), dict(wdt=1), dict(gdt=1), dict(gdt=7), dict(eps=-1.0), dict(eps=NAN),
                      dict(eps=INF), dict(alpha=NAN), dict(alpha=INF), dict(gates=0), dict(gates=3), dict(gates=-2),
-                     dict(w=None), dict(y=None), dict(x=None), dict(r=None)]),
+                     dict(w=None), dict(x=None), dict(r=None)]),
     (block_norm, 2, [dict(H=32769), dict(T=1 << 31)]),
     (block_norm, 0, [dict(T=0), dict(T=0, x=None)]),
     (block_norm_backward, 1, [dict(T=-1), dict(H=0), dict(dt=3), dict(wdt=1), dict(gdt=1), dict(alpha=NAN), dict(gates=3),
