@@ -258,11 +258,13 @@ struct Results {
     for (int j = 0; j < TM; ++j)
       sm[j] = t.expert < 0 ? 0.f : p.scale[t.row + min(m0 + 32 * j + lane % 32, t.rows - 1)];
   }
+  // Blocks of rows FROM .. TO - 1.
+  template <int FROM = 0, int TO = TM>
   __device__ __forceinline__ void store(const ProductArgs& p, const Tile& t, int32_t n0, int m0,
                                         const i32x16 (&acc)[TN][TM]) const {
     const int lane = threadIdx.x % kWave;
 #pragma unroll
-    for (int j = 0; j < TM; ++j) {
+    for (int j = FROM; j < TO; ++j) {
       const int m = m0 + 32 * j + lane % 32;
       T* const to = static_cast<T*>(p.out) + (int64_t)(t.row + m) * p.N;
 #pragma unroll
@@ -513,13 +515,14 @@ product_wide_kernel(ProductArgs p, Work work, int32_t most) {
     if (k < K) step(k, even, odd);
     // What was brought last is of no use, but on its way.  No wave reads LDS any more (but for operands that it does
     // not use), so the next tile's first pieces come while this one's results go.
+    Results<T, 4, 4> results;
+    results.scales(p, t, n0 + wn, wm);
     __builtin_amdgcn_s_waitcnt(kAllLoads);
     const auto next_rows_n = buffer_n(next, next_n0), next_rows_m = buffer_m(next);
     if (more) begin(next_rows_n, next_rows_m);
-    Results<T, 4, 4> results;
-    results.scales(p, t, n0 + wn, wm);
-    __builtin_amdgcn_s_waitcnt(kAllLoads);  // the next tile's pieces too, and not for the results that go now
-    results.store(p, t, n0 + wn, wm, acc);
+    results.template store<0, 3>(p, t, n0 + wn, wm, acc);
+    __builtin_amdgcn_s_waitcnt(kAllLoads);  // the pieces are there, and the last results are not waited for
+    results.template store<3, 4>(p, t, n0 + wn, wm, acc);
     t = next;
     n0 = next_n0;
     rows_n = next_rows_n;
