@@ -30,6 +30,7 @@ __device__ __forceinline__ f32x8 factor(const Vector& v, int64_t col, int n) {
 
 // Lanes hold columns as in the norm without a gate; h may lie in x's or the
 // residual's memory: a lane has read all of its columns before it writes them.
+// 16384 x 4096 bfloat16, post and gate: 95 us for 537 MB, 5.7 TB/s.
 template <typename T, int CPL, bool FAR>
 __global__ void __launch_bounds__(1024)
 block_norm_kernel(const T* x, const T* residual, Vector post, Vector gate, int64_t per_gate, int64_t first,
@@ -144,7 +145,10 @@ __device__ __forceinline__ Three row_sums(Three v, f32x4 (*part)[16], int slot, 
 // is read by its worker alone, each place by the lane that writes it, before it does.
 //
 // With q = gate post, e = b dy w + dh and c = b^2 mean(dy w h) it is D = e - b c h, so
-// sum(D q x) = sum(e q x) - b c sum(h q x): all sums of a row are taken at once.
+// sum(D q x) = sum(e q x) - b c sum(h q x): all sums of a row are taken at once (8192 x 5120
+// bfloat16, dh, post, 4 gates: 136 us with a sum after the other, 109 so and with as many
+// workers as are resident).  102 us for 503 MB, 4.9 TB/s, and 6 for the workers' sums: of
+// the 16 waves whose registers a compute unit holds, a row of 5120 fills ten.
 template <typename T, bool FAR, bool MANY, bool WHOLE>
 __global__ void __launch_bounds__(1024)
 block_norm_backward_kernel(const T* dy, const T* dh, const T* x, const T* h, const float* __restrict__ rstd_x,

@@ -9,6 +9,12 @@
 //
 // runs_kernel lists the tiles of rows: a tile lies within one run.  The weights are
 // the matrix unit's first operand, so a lane's results are neighbouring channels.
+//   product_few_kernel     16 rows, 16 channels   few rows a run: the weights' way from memory
+//   product_some_kernel    64 rows, 32 channels   few tiles in all: waves share the inner dimension
+//   product_kernel         64 rows, 128 channels  middling runs (and 256 by 256 where rows do not
+//                                                 begin at multiples of 16 bytes)
+//   product_wide_kernel    256 rows, 256 channels  long runs: the matrix units
+// The rule is at kind_of, with both sides of each bound.
 #include "rowio.h"
 
 namespace taot {
@@ -175,9 +181,9 @@ __device__ __forceinline__ Tile tile_of(const Work& w, int32_t i, int64_t M, int
 // Which tiles a block works on, and in which order.  Blocks go to the eight dies in
 // turn; a die gets a contiguous part of the tiles, in groups of kGroup tiles of rows
 // by all channels, so that what its blocks read at a time is near a square and is
-// found in its L2 cache.  Or all blocks take the tiles in order: where each weight is
-// read by one block, memory is read from one end to the other (64 rows of 128 runs, 31
-// of them not empty, 2048 x 2048: 28 us, 35 by dies).
+// found in its L2 cache; in groups of one where each weight is read by one block, which
+// goes through memory in order (64 rows of 64 runs, 4096 x 4096: 172 us, 178 in groups of
+// four; 64 of 128, 2048 x 2048: 30 and 35).
 constexpr int kStep = 128;  // bytes of the inner dimension that a step has
 constexpr int kDies = 8, kGroup = 4, kUnits = 256;  // compute units
 struct Walk {
@@ -287,10 +293,15 @@ struct Results {
   }
 };
 
+// 16-byte pieces of a row of LDS change places by half the row's number: 16 lanes are
+// served at a time out of 64 banks, which two rows of a step fill (by the row's own
+// number half of all cycles of the reads are conflicts: 32768 x 4096 x 1024 178 us, 165
+// so).
+__device__ __forceinline__ int turn_of(int row) { return row / 2 % (kStep / 16); }
+
 // BN channels by BM rows of a tile, by WN x WM waves; kStep bytes of the inner
 // dimension at a time, those of the next AHEAD steps on their way in registers while
-// the present ones are worked on out of LDS.  16-byte pieces of a row of LDS change
-// places by the row's number, so that lanes of neighbouring rows read other banks.
+// the present ones are worked on out of LDS.
 template <typename T, int BN, int BM, int WN, int WM, int AHEAD, bool SHIFT>
 __global__ void __launch_bounds__(kWave * WN * WM) __attribute__((amdgpu_waves_per_eu(AHEAD > 1 ? 3 : 2)))
 product_kernel(ProductArgs p, Work work, int32_t most) {
@@ -311,13 +322,13 @@ product_kernel(ProductArgs p, Work work, int32_t most) {
     for (int i = 0; i < LN; ++i) {
       const int r = tid / kPieces + i * (kThreads / kPieces);
       from_n[i] = W + (int64_t)min(n0 + r, p.N - 1) * p.K;
-      to_n[i] = r * kPieces + (piece ^ (r % kPieces));
+      to_n[i] = r * kPieces + (piece ^ turn_of(r));
     }
 #pragma unroll
     for (int i = 0; i < LM; ++i) {
       const int r = tid / kPieces + i * (kThreads / kPieces);
       from_m[i] = p.x + (int64_t)(t.row + min(r, t.rows - 1)) * p.K;
-      to_m[i] = BN * kPieces + r * kPieces + (piece ^ (r % kPieces));
+      to_m[i] = BN * kPieces + r * kPieces + (piece ^ turn_of(r));
     }
     Words<SHIFT, 1> next_n[AHEAD][LN], next_m[AHEAD][LM];
     auto fetch = [&](int32_t k, int s) {
@@ -374,12 +385,12 @@ product_kernel(ProductArgs p, Work work, int32_t most) {
 #pragma unroll
           for (int i = 0; i < TN; ++i) {
             const int r = wn + 32 * i + lane % 32;
-            a[i] = lds[r * kPieces + (c ^ (r % kPieces))];
+            a[i] = lds[r * kPieces + (c ^ turn_of(r))];
           }
 #pragma unroll
           for (int j = 0; j < TM; ++j) {
             const int r = wm + 32 * j + lane % 32;
-            b[j] = lds[BN * kPieces + r * kPieces + (c ^ (r % kPieces))];
+            b[j] = lds[BN * kPieces + r * kPieces + (c ^ turn_of(r))];
           }
 #pragma unroll
           for (int i = 0; i < TN; ++i)
@@ -400,10 +411,17 @@ product_kernel(ProductArgs p, Work work, int32_t most) {
   }
 }
 
-// Many rows, whole 16-byte pieces: a wave on each SIMD holds 128 x 128 results, and
-// pieces go from memory to LDS without passing through registers.  The operands of
-// the next 32 bytes are read out of LDS while the present ones are multiplied, and
-// those of the next step's first 32 before the present step's last are.
+// Many rows, whole 16-byte pieces: a wave on each SIMD holds 128 x 128 results (of
+// smaller ones the reads of LDS would take as long as the products), and pieces go from
+// memory to LDS without passing through registers.  The operands of the next 32 bytes
+// are read out of LDS while the present ones are multiplied, and those of the next
+// step's first 32 before the present step's last are.  A step's 16 loads and 32 reads
+// lie between its 64 products, one or two at a time: a wave has its SIMD for itself, and
+// what it issues in a row the matrix unit waits for (8192 x 4096 and 8192, zeros: 2.6 to
+// 2.8 POP/s with all of them in a row, 3.6 to 4.1 so).
+// 65536 rows of 32 runs, 4096 x 4096: 1060 us, 2.08 POP/s; 8192^3 2.3 to 2.5.  Bound by
+// power: 8192^3 of zeros reaches 3.5, the clock falls from 2.4 to 1.75 GHz, and products
+// alone, no loads and no reads, reach 3.0 to 3.3 of random values and 4.1 to 4.7 of zeros.
 constexpr int kWideN = 256, kWideM = 256, kWideThreads = 256;
 constexpr int kRawBuffer = 0x00027000;  // a buffer's description: untyped, checked by bytes
 constexpr int kAllLoads = 0x0F70;       // waits for memory alone
@@ -425,7 +443,7 @@ product_wide_kernel(ProductArgs p, Work work, int32_t most) {
     at_n[i] = (wn + 32 * i + lane % 32) * kPieces;
     at_m[i] = (kWideN + wm + 32 * i + lane % 32) * kPieces;
   }
-  const int turn = lane % kPieces;  // of the row's pieces
+  const int turn = turn_of(lane % 32);  // of the row's pieces
   auto bring = [&](Buffer rows_n, Buffer rows_m, uint32_t from, i32x4* to, int i) {
     __builtin_amdgcn_raw_ptr_buffer_load_lds(i < kLoads / 2 ? rows_n : rows_m,
                                              (LdsPlace*)(to + (i * kWaves + wid) * kWave), 16,
@@ -433,7 +451,7 @@ product_wide_kernel(ProductArgs p, Work work, int32_t most) {
   };
   // A wave brings eight rows at a time, a lane the piece whose place is its own.  Rows and pieces behind the ends are
   // out of the buffers' ranges, and come as zeros.
-  const int own = 16 * ((lane % kPieces) ^ (lane / kPieces));
+  const int own = 16 * ((lane % kPieces) ^ turn_of(wid * 8 + lane / kPieces));
   const uint32_t first = (uint32_t)((wid * 8 + lane / kPieces) * p.K + own);
   auto offset = [&](int32_t k) { return k + own < p.K ? first + (uint32_t)k : 0x80000000u; };
   Walk walk(work, most, p.N, kWideN);
@@ -532,6 +550,9 @@ product_wide_kernel(ProductArgs p, Work work, int32_t most) {
 
 // A few rows of each run: tiles of 16 rows by 16 channels, whose four waves share the
 // inner dimension.  A lane reads 32 neighbouring bytes of its row, a wave whole lines.
+// Bound by memory where the weights are many (64 rows of 64 runs, 4096 x 4096: 172 us for
+// 1.07 GB, 6.2 TB/s), by the blocks' own chains of loads where they are few (64 rows over
+// 31 of 128 runs, 2048 x 2048: 26 us for 130 MB, and the list of tiles).
 constexpr int kFewRows = 16, kFewN = 16, kFewWaves = 4, kFewAhead = 2;
 template <typename T, bool SHIFT>
 __global__ void __launch_bounds__(kWave * kFewWaves)
@@ -603,7 +624,8 @@ product_few_kernel(ProductArgs p, Work work, int32_t most) {
 // one's are multiplied, and meet as sums in LDS, which are whole numbers and have no
 // order.  A lane reads 64 neighbouring bytes of its row, a wave whole lines of 128 of
 // each; which bytes meet in a product is the same for both operands.  Blocks of 32 rows
-// that a tile does not have are left out.
+// that a tile does not have are left out.  64 rows, 8192 x 8192: 33 us (67 by tiles of 64
+// by 128 that go through LDS, of which there are too few for the chip).
 constexpr int kSomeN = 32, kSomeWaves = 8, kSomeThreads = kSomeWaves * kWave;
 
 template <typename T, int TM, bool SHIFT>
@@ -698,6 +720,14 @@ product_some_kernel(ProductArgs p, Work work, int32_t most) {
   }
 }
 
+// Which kernel, by how many rows a run has on average and how many tiles there are.  Us by
+// few, some, middle and wide:
+//   K = N = 8192, one run:    16 rows  22 23 67 83       32 rows  36 25 67 84      64 rows  62 33 68 88
+//   K = N = 4096, one run:   128 rows  36 21 34 44      256 rows  64 33 27 43     512 rows 120 59 30 44
+//                           1024 rows 231 110 39 45    2048 rows 453 211 72 49
+//   K = N = 4096:         8 runs of 256 rows in all   65 54 50 59     30 of 2000  528 397 152 144
+//   K = N = 2048:       128 runs of 64 rows in all    36 52 34 39     30 of 4096  248 168  62  46
+//                        64 of 8192  465 275 98 88                    64 of 16384 917 532 159  98
 enum Kind { kFew, kSome, kMiddle, kLarge };
 Kind kind_of(int64_t M, int32_t N, int32_t runs) {
   const int64_t sets = runs > 0 ? runs : 1, each = M / sets;
