@@ -6,8 +6,8 @@
 //   With a_e = dloss E c_e / (n sum c):
 //   softmax:  dx = p (a - <a, p> + 2 dz / n lse);  sigmoid s with sum V:  dx = (a - <a, p>) / V s (1 - s).
 //
-// A token's logits are read once and held in registers, by 16 lanes (E to 512), a wave
-// (to 2048) or a block.  Sums over tokens are taken by lane, then over a block's waves,
+// A token's logits are read once and held in registers, by 2, 8 or 16 lanes (E to 16,
+// 64 and 512), a wave (to 2048) or a block.  Sums over tokens are taken by lane, then over a block's waves,
 // then over the blocks, always in the same order; choices are whole numbers, counted in LDS.
 // A logit of -infinity or NaN is an expert with p = 0, +infinity counts as the
 // largest float; a token of such experts alone has p = 0 everywhere and lse = 0.
@@ -20,6 +20,9 @@ namespace {
 
 constexpr float kTiny = 1e-20f;  // added to a sum of sigmoids before it divides
 constexpr int kWhole = 0;        // lanes of a token: all of the block
+// Counters of rows lie in cache lines of their own: atomics on one line wait for one
+// another (32 rows of 128 tokens of 4096 experts, the sums' kernel: 49 us in a line, 10 so).
+constexpr int kLine = 32;
 
 // A token's scores.  L lanes hold it (kWhole: the block's waves), lane l columns
 // 8 (i L + l) .. + 7.  v: p;  total: the sum that p was divided by.
@@ -108,7 +111,7 @@ balance_kernel(const T* __restrict__ logits, const int32_t* __restrict__ ids, co
   for (int32_t e = tid; e < s.E; e += blockDim.x) hits[e] = 0;
   if (tid == 0) {
     ns = 0;
-    if (block == 0) done[row] = 0;
+    if (block == 0) done[row * kLine] = 0;
   }
   __syncthreads();
   Group<L> g;
@@ -202,33 +205,35 @@ balance_kernel(const T* __restrict__ logits, const int32_t* __restrict__ ids, co
   }
 }
 
-// prob and counts of kTile experts of a row, 32 threads each, and these experts' part
-// of the loss.  The last block of a row adds the parts up, in order.
+// prob and counts of kTile experts of a row, up to 32 threads each, and these experts'
+// part of the loss.  The last block of a row adds the parts up, in order.
 constexpr int kTile = 32;
 struct Part {
   float loss;
   int32_t choices;
 };
-__global__ void __launch_bounds__(1024)
+template <int THREADS>
+__global__ void __launch_bounds__(THREADS)
 balance_sums_kernel(const float* __restrict__ part_p, const int32_t* __restrict__ part_c, const float* __restrict__ part_z,
                     const int32_t* __restrict__ part_n, int32_t blocks, int32_t E, float* __restrict__ prob,
                     int32_t* __restrict__ counts, uint64_t* parts, int32_t* done, float* __restrict__ loss,
                     float* __restrict__ z, int32_t* __restrict__ counted) {
-  __shared__ float sum[16][kTile], zs[16];
-  __shared__ int32_t cnt[16][kTile], ns[16], all[16];
+  constexpr int kWaves = THREADS / kWave;
+  __shared__ float sum[kWaves][kTile], zs[kWaves];
+  __shared__ int32_t cnt[kWaves][kTile], ns[kWaves], all[kWaves];
   __shared__ int32_t last;
   const int c = threadIdx.x % kTile, r = threadIdx.x / kTile, wid = threadIdx.x / kWave;
   const int32_t tiles = (E + kTile - 1) / kTile, e = (int32_t)(blockIdx.x % (uint32_t)tiles) * kTile + c;
   const int64_t row = blockIdx.x / (uint32_t)tiles, at = row * blocks;
   float p = 0.f, zz = 0.f;  // z is the last block's to write, but here its way is short
   int32_t k = 0, n = 0;
-  for (int32_t b = threadIdx.x; b < blocks; b += 1024) {
+  for (int32_t b = threadIdx.x; b < blocks; b += THREADS) {
     n += part_n[at + b];
     zz += part_z[at + b];
   }
   if (e < E)
 #pragma unroll 8
-    for (int32_t b = r; b < blocks; b += 1024 / kTile) {
+    for (int32_t b = r; b < blocks; b += THREADS / kTile) {
       p += part_p[(at + b) * E + e];
       k += part_c[(at + b) * E + e];
     }
@@ -251,7 +256,7 @@ balance_sums_kernel(const float* __restrict__ part_p, const int32_t* __restrict_
   n = 0;
   zz = 0.f;
 #pragma unroll
-  for (int w = 0; w < 16; ++w) {
+  for (int w = 0; w < kWaves; ++w) {
     n += ns[w];
     zz += zs[w];
   }
@@ -259,7 +264,7 @@ balance_sums_kernel(const float* __restrict__ part_p, const int32_t* __restrict_
     p = 0.f;
     k = 0;
 #pragma unroll
-    for (int w = 0; w < 16; ++w) {
+    for (int w = 0; w < kWaves; ++w) {
       p += sum[w][c];
       k += cnt[w][c];
     }
@@ -278,14 +283,14 @@ balance_sums_kernel(const float* __restrict__ part_p, const int32_t* __restrict_
       __atomic_signal_fence(__ATOMIC_SEQ_CST);
       __builtin_amdgcn_s_waitcnt(0);
       __atomic_signal_fence(__ATOMIC_SEQ_CST);
-      last = __hip_atomic_fetch_add(done + row, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == tiles - 1;
+      last = __hip_atomic_fetch_add(done + row * kLine, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == tiles - 1;
     }
   }
   __syncthreads();
   if (!last) return;
   float l = 0.f;
   k = 0;
-  for (int32_t i = threadIdx.x; i < tiles; i += 1024) {
+  for (int32_t i = threadIdx.x; i < tiles; i += THREADS) {
     const Part q = __builtin_bit_cast(
         Part, __hip_atomic_load(parts + row * tiles + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
     l += q.loss;
@@ -301,7 +306,7 @@ balance_sums_kernel(const float* __restrict__ part_p, const int32_t* __restrict_
   if (threadIdx.x != 0) return;
   l = 0.f;
   k = 0;
-  for (int w = 0; w < 16; ++w) {
+  for (int w = 0; w < kWaves; ++w) {
     l += sum[w][0];
     k += all[w];
   }
@@ -413,7 +418,11 @@ struct Layout {
 // (32768 of 384 in 16 bits, 1280 blocks of four waves 18.2, 2048 21.0, 4096 21.0).
 Layout layout_of(int64_t rows, int64_t tokens, int32_t E, bool backward) {
   Layout l;
-  if (E <= 512) {
+  if (E <= 16) {
+    l = {2, 1, backward ? 256 : 1024, 0, 0};
+  } else if (E <= 64) {
+    l = {8, 1, backward ? 256 : 1024, 0, 0};
+  } else if (E <= 512) {
     l = {16, (E + 127) / 128, backward ? 256 : 1024, 0, 0};
   } else if (E <= 2048) {
     l = {64, E <= 1024 ? 2 : 4, backward ? 256 : 1024, 0, 0};
@@ -450,7 +459,7 @@ Partial carve(void* ws, int64_t rows, int32_t E, int32_t blocks) {
   p.c = c.take<int32_t>((size_t)rows * blocks * E);
   p.z = c.take<float>((size_t)rows * blocks);
   p.n = c.take<int32_t>((size_t)rows * blocks);
-  p.done = c.take<int32_t>((size_t)rows);
+  p.done = c.take<int32_t>((size_t)rows * kLine);
   p.parts = c.take<uint64_t>((size_t)rows * ((E + kTile - 1) / kTile));
   p.bytes = c.off;
   return p;
@@ -460,14 +469,16 @@ Partial carve(void* ws, int64_t rows, int32_t E, int32_t blocks) {
 template <int L, int CPL, typename F>
 void with_full(int32_t E, F f) {
   using std::integral_constant;
-  if constexpr (L == 16) {
+  if constexpr (L >= 2 && L <= 16) {
     if (E == 8 * L * CPL) return f(integral_constant<int, L>(), integral_constant<int, CPL>(), std::true_type());
   }
   f(integral_constant<int, L>(), integral_constant<int, CPL>(), std::false_type());
 }
 template <typename F>
 void with_layout(const Layout& l, int32_t E, F f) {
-  if (l.lanes == 16) {
+  if (l.lanes == 2) with_full<2, 1>(E, f);
+  else if (l.lanes == 8) with_full<8, 1>(E, f);
+  else if (l.lanes == 16) {
     if (l.cpl == 1) with_full<16, 1>(E, f);
     else if (l.cpl == 2) with_full<16, 2>(E, f);
     else if (l.cpl == 3) with_full<16, 3>(E, f);
@@ -522,7 +533,9 @@ taot_status launch_balance_loss(const void* logits, const int32_t* ids, const ui
       return fine;
     });
     if (!ok) return TAOT_ERR_LAUNCH;
-    balance_sums_kernel<<<(unsigned)(n * ((E + kTile - 1) / kTile)), 1024, 0, stream>>>(
+    const bool few = l.blocks <= 2 * 256 / kTile;
+    auto* const sums = few ? balance_sums_kernel<256> : balance_sums_kernel<1024>;
+    sums<<<(unsigned)(n * ((E + kTile - 1) / kTile)), few ? 256 : 1024, 0, stream>>>(
         p.p, p.c, p.z, p.n, l.blocks, E, prob + r * E, counts + r * E, p.parts, p.done, loss + r, z ? z + r : nullptr,
         counted ? counted + r : nullptr);
   }
