@@ -28,14 +28,41 @@ __device__ __forceinline__ f32x8 factor(const Vector& v, int64_t col, int n) {
   return v.p ? load_row_either<T>(v.p, v.f32, col, n) : f32x8(1.f);
 }
 
+// A row's odd end.  Its lane takes the row's last eight columns, some of which the lane
+// before it has too: both work the same out and write it, and one of them adds it to the
+// row's sums.  (With single loads there, for which the others of the row wait: 16384 x
+// 4095 141 us, 127 so, gradient of 8192 x 5119 195 and 133.)
+enum Edge { kWholeRows, kOddRows, kAnyRows };  // H % 8 == 0; other H from 8 on; any H, with single loads
+template <Edge EDGE>
+struct Place {
+  int col, n, back;  // first column, how many (8 or 0, kAnyRows: up to the row's end), how many the lane before has too
+  __device__ __forceinline__ Place(int chunk, int32_t H) : col(8 * chunk), n(EDGE == kAnyRows ? H - col : col < H ? 8 : 0), back(0) {
+    if (EDGE == kOddRows && n && H - col < 8) {
+      back = 8 - (H - col);
+      col -= back;
+    }
+  }
+  __device__ __forceinline__ bool adds(int u) const { return EDGE != kOddRows || u >= back; }
+  template <typename T>
+  __device__ __forceinline__ void load(const T* from, typename Row8<T>::vec& to) const {  // `to` is 0 if there are no columns
+    if (EDGE == kAnyRows) to = load_raw(from + col, n);
+    else if (n) to = *reinterpret_cast<const typename Row8<T>::at*>(from + col);
+  }
+  template <bool FAR, typename T>
+  __device__ __forceinline__ void store(T* to, f32x8 v) const {
+    if (EDGE == kAnyRows || n) store_row<FAR>(to + col, v, n);
+  }
+};
+
 // Lanes hold columns as in the norm without a gate; h may lie in x's or the
-// residual's memory: a lane has read all of its columns before it writes them.
+// residual's memory: all of a lane's columns are read before they are written.
 // 16384 x 4096 bfloat16, post and gate: 95 us for 537 MB, 5.7 TB/s.
-template <typename T, int CPL, bool FAR>
+template <typename T, int CPL, bool FAR, Edge EDGE>
 __global__ void __launch_bounds__(1024)
 block_norm_kernel(const T* x, const T* residual, Vector post, Vector gate, int64_t per_gate, int64_t first,
                   Vector weight, int64_t rows, int32_t H, float eps, float alpha, T* h, T* y,
                   float* __restrict__ rstd_x, float* __restrict__ rstd_h, int waves) {
+  using At = Place<EDGE>;
   __shared__ float part[2][16];
   const int lanes = waves * kWave;
   const int lane = waves == 1 ? threadIdx.x & (kWave - 1) : threadIdx.x;
@@ -43,12 +70,13 @@ block_norm_kernel(const T* x, const T* residual, Vector post, Vector gate, int64
   if (row >= rows) return;  // whole waves, and only where no wave waits for another
   const int64_t at = row * H, gate_at = gate.p ? (first + row) / per_gate * H : 0;
   f32x8 v[CPL];
-  typename Row8<T>::vec r[CPL];
+  typename Row8<T>::vec raw[CPL], r[CPL];
 #pragma unroll
   for (int i = 0; i < CPL; ++i) {
-    const int col = 8 * (i * lanes + lane), n = H - col;
-    v[i] = load_row(x + at + col, n);
-    r[i] = load_raw(residual + at + col, n);
+    raw[i] = r[i] = (T)0.f;
+    At(i * lanes + lane, H).load(x + at, raw[i]);
+    v[i] = widen(raw[i]);
+    At(i * lanes + lane, H).load(residual + at, r[i]);
   }
   float a = 1.f;
   if (post.p) {
@@ -56,28 +84,30 @@ block_norm_kernel(const T* x, const T* residual, Vector post, Vector gate, int64
 #pragma unroll
     for (int i = 0; i < CPL; ++i)
 #pragma unroll
-      for (int u = 0; u < 8; ++u) ss = fmaf(v[i][u], v[i][u], ss);
+      for (int u = 0; u < 8; ++u) ss = At(i * lanes + lane, H).adds(u) ? fmaf(v[i][u], v[i][u], ss) : ss;
     a = 1.f / sqrtf(row_reduce(ss, SumOp(), part, 0, waves) / (float)H + eps);
     if (lane == 0 && rstd_x) rstd_x[row] = a;
+  } else if (EDGE == kOddRows && waves > 1) {
+    __syncthreads();  // the lane before may be another wave's, and write where this one reads
   }
   float ss = 0.f;
 #pragma unroll
   for (int i = 0; i < CPL; ++i) {
-    const int col = 8 * (i * lanes + lane), n = H - col;
-    if (post.p) v[i] = v[i] * a * factor<T>(post, col, n);
-    if (gate.p) v[i] = v[i] * factor<T>(gate, gate_at + col, n);
+    const At p(i * lanes + lane, H);
+    if (post.p) v[i] = v[i] * a * factor<T>(post, p.col, p.n);
+    if (gate.p) v[i] = v[i] * factor<T>(gate, gate_at + p.col, p.n);
     v[i] = alpha * widen(r[i]) + v[i];
 #pragma unroll
-    for (int u = 0; u < 8; ++u) ss = fmaf(v[i][u], v[i][u], ss);
-    if (h) store_row<FAR>(h + at + col, v[i], n);
+    for (int u = 0; u < 8; ++u) ss = p.adds(u) ? fmaf(v[i][u], v[i][u], ss) : ss;
+    if (h) p.template store<FAR>(h + at, v[i]);
   }
   if (!weight.p) return;
   const float b = 1.f / sqrtf(row_reduce(ss, SumOp(), part, 1, waves) / (float)H + eps);
   if (lane == 0 && rstd_h) rstd_h[row] = b;
 #pragma unroll
   for (int i = 0; i < CPL; ++i) {
-    const int col = 8 * (i * lanes + lane), n = H - col;
-    if (y) store_row<FAR>(y + at + col, v[i] * b * factor<T>(weight, col, n), n);
+    const At p(i * lanes + lane, H);
+    if (y) p.template store<FAR>(y + at, v[i] * b * factor<T>(weight, p.col, p.n));
   }
 }
 
@@ -142,14 +172,14 @@ __device__ __forceinline__ Three row_sums(Three v, f32x4 (*part)[16], int slot, 
 // registers until it writes them as one row of the partial sums; a gate that a
 // worker has alone gets its gradient at once.  The next row is on its way while
 // the present one is worked on.  dresidual and dx may lie in an input's memory: a row
-// is read by its worker alone, each place by the lane that writes it, before it does.
+// is read by its worker alone, and all of it before any of it is written.
 //
 // With q = gate post, e = b dy w + dh and c = b^2 mean(dy w h) it is D = e - b c h, so
 // sum(D q x) = sum(e q x) - b c sum(h q x): all sums of a row are taken at once (8192 x 5120
 // bfloat16, dh, post, 4 gates: 136 us with a sum after the other, 109 so and with as many
 // workers as are resident).  102 us for 503 MB, 4.9 TB/s, and 6 for the workers' sums: of
 // the 16 waves whose registers a compute unit holds, a row of 5120 fills ten.
-template <typename T, bool FAR, bool MANY, bool WHOLE>
+template <typename T, bool FAR, bool MANY, Edge EDGE>
 __global__ void __launch_bounds__(1024)
 block_norm_backward_kernel(const T* dy, const T* dh, const T* x, const T* h, const float* __restrict__ rstd_x,
                            const float* __restrict__ rstd_h, Vector post, Vector gate, Share share, Vector weight,
@@ -160,20 +190,12 @@ block_norm_backward_kernel(const T* dy, const T* dh, const T* x, const T* h, con
   const int lane = waves == 1 ? threadIdx.x & (kWave - 1) : threadIdx.x;
   const int32_t worker = waves == 1 ? blockIdx.x * kRowsOfBlock + threadIdx.x / kWave : blockIdx.x;
   if (worker >= workers) return;
-  const int col = 8 * lane, n = H - col;
+  const Place<EDGE> place(lane, H);
+  const int col = place.col, n = place.n;
   constexpr bool kAhead = sizeof(T) == 2;  // the registers of 16 waves hold two rows of 16 bits
   const bool sums = post.p || gate.p;
   Rows<MANY> rows(share, worker, workers);
-  auto load = [&](const T* from, int64_t row, Raw& to) {  // lanes behind the row keep their zeros
-    if constexpr (WHOLE) {
-      if (n > 0) to = *reinterpret_cast<const typename Row8<T>::at*>(from + row * H + col);
-    } else {
-      to = load_raw(from + row * H + col, n);
-    }
-  };
-  auto store = [&](T* to, f32x8 v) {
-    if (WHOLE ? n > 0 : true) store_row<FAR>(to, v, WHOLE ? 8 : n);
-  };
+  auto load = [&](const T* from, int64_t row, Raw& to) { place.load(from + row * H, to); };
   const f32x8 w = factor<T>(weight, col, n);
   f32x8 q = factor<T>(gate, rows.seg * H + col, n) * factor<T>(post, col, n);
   f32x8 dw = 0.f, S = 0.f, dp = 0.f;
@@ -190,7 +212,7 @@ block_norm_backward_kernel(const T* dy, const T* dh, const T* x, const T* h, con
   float a = post.p ? rstd_x[rows.row] : 1.f, b = weight.p ? rstd_h[rows.row] : 0.f;
   int slot = 0;
   for (; rows.left > 0; rows.next()) {
-    const int64_t at = rows.row * H + col, gate_at = rows.seg * H + col, then = rows.then();
+    const int64_t at = rows.row * H, gate_at = rows.seg * H + col, then = rows.then();
     if (kAhead) fetch(then, nx, nh, ny, nd);
     else fetch(rows.row, rx, rh, ry, rd);
     const float next_a = post.p ? rstd_x[then] : 1.f, next_b = weight.p ? rstd_h[then] : 0.f;
@@ -202,9 +224,10 @@ block_norm_backward_kernel(const T* dy, const T* dh, const T* x, const T* h, con
       const float v = Y[u] * w[u], qx = q[u] * X[u];
       e[u] = fmaf(b, v, e[u]);
       dw[u] = fmaf(Y[u], Hh[u] * b, dw[u]);
-      s.a = fmaf(v, Hh[u], s.a);
-      s.b = fmaf(e[u], qx, s.b);
-      s.c = fmaf(Hh[u], qx, s.c);
+      const bool mine = place.adds(u);
+      s.a = mine ? fmaf(v, Hh[u], s.a) : s.a;
+      s.b = mine ? fmaf(e[u], qx, s.b) : s.b;
+      s.c = mine ? fmaf(Hh[u], qx, s.c) : s.c;
     }
     s = row_sums(s, part, slot, waves);
     slot ^= 1;
@@ -217,8 +240,8 @@ block_norm_backward_kernel(const T* dy, const T* dh, const T* x, const T* h, con
       t[u] = D[u] * q[u];
       if (post.p) t[u] = a * fmaf(-m, X[u], t[u]);
     }
-    store(dresidual + at, alpha * D);
-    store(dx + at, t);
+    place.template store<FAR>(dresidual + at, alpha * D);
+    place.template store<FAR>(dx + at, t);
     if (MANY && rows.ends()) {
       const f32x8 p = factor<T>(post, col, n);
       if (dgate) store_row(dgate + gate_at, S * p, n);
@@ -240,7 +263,7 @@ block_norm_backward_kernel(const T* dy, const T* dh, const T* x, const T* h, con
 }
 
 // The same for rows wider than the registers hold beside the sums (more than 8192
-// columns): the 16 waves read a row's inputs three times, the later ones out of the
+// columns), and for those of less than eight: the 16 waves read a row's inputs three times, the later ones out of the
 // L2 cache, and keep their sums in memory, each lane its own columns.  A gate that a
 // worker has alone is summed where its gradient goes.
 template <typename T, bool FAR, bool MANY>
@@ -420,11 +443,12 @@ struct Split {
   bool many;
 };
 // Workers of the gradient: as many on each compute unit as its registers hold, 16
-// waves.  Gates of fewer rows than that are taken whole.
+// waves.  Gates that are as many, or have one row each, are taken whole (1753 x 511 in
+// 32 bits, a gate a row: 98 us where each gate's sums are a launch's blocks, 28 so).
 Split split_of(int64_t rows, int32_t H, int64_t gates) {
   const int waves = shape_of(H).waves;
   const int64_t most = 256 * (16 / waves), per = rows / gates;
-  if (gates >= most) return {{gates, per, 0}, (int32_t)most, true};
+  if (gates >= most || (gates > 1 && per == 1)) return {{gates, per, 0}, (int32_t)(gates < most ? gates : most), true};
   int64_t each = (most + gates - 1) / gates;
   if (each > per) each = per;
   return {{gates, per, each}, (int32_t)(each * gates), false};
@@ -456,8 +480,9 @@ taot_status forward(const BlockNormArgs& a, hipStream_t stream) {
   const Vector post{a.post, a.weight_f32}, gate{a.gate, a.gate_f32}, weight{a.weight, a.weight_f32};
   const int64_t per_gate = a.gate ? a.rows / a.gates : 1;
   const bool ok = with_chunks(s.cpl, [&](auto C) {
-    auto* kernel = with_far(a.rows * a.H * ((a.h != nullptr) + (a.y != nullptr)) * (int64_t)sizeof(T), [](auto far) {
-      return block_norm_kernel<T, decltype(C)::value, far.value>;
+    auto* kernel = with_far(a.rows * a.H * ((a.h != nullptr) + (a.y != nullptr)) * (int64_t)sizeof(T), [&](auto far) {
+      return a.H % 8 && a.H >= 8 ? block_norm_kernel<T, decltype(C)::value, far.value, kOddRows>
+                                 : block_norm_kernel<T, decltype(C)::value, far.value, kAnyRows>;
     });
     for (int64_t r = 0; r < a.rows; r += kMaxBlocks * per) {
       const int64_t n = a.rows - r < kMaxBlocks * per ? a.rows - r : kMaxBlocks * per, at = r * a.H;
@@ -491,12 +516,12 @@ taot_status backward(const BlockNormGradArgs& a, void* ws, hipStream_t stream) {
             *h = static_cast<const T*>(a.h);
     T *dx = static_cast<T*>(a.dx), *dr = static_cast<T*>(a.dresidual);
     float *part_w = a.dweight ? p.w : nullptr, *part_s = sums ? p.s : nullptr;
-    if (s.cpl == 1) {
+    if (s.cpl == 1 && a.H >= 8) {
       const bool whole = a.H % 8 == 0;
-      auto* kernel = sp.many ? whole ? block_norm_backward_kernel<T, far.value, true, true>
-                                     : block_norm_backward_kernel<T, far.value, true, false>
-                     : whole ? block_norm_backward_kernel<T, far.value, false, true>
-                             : block_norm_backward_kernel<T, far.value, false, false>;
+      auto* kernel = sp.many ? whole ? block_norm_backward_kernel<T, far.value, true, kWholeRows>
+                                     : block_norm_backward_kernel<T, far.value, true, kOddRows>
+                     : whole ? block_norm_backward_kernel<T, far.value, false, kWholeRows>
+                             : block_norm_backward_kernel<T, far.value, false, kOddRows>;
       kernel<<<(unsigned)((sp.workers + per - 1) / per), kWave * s.waves * per, 0, stream>>>(
           dy, dh, x, h, a.rstd_x, a.rstd_h, post, gate, sp.share, weight, a.H, a.alpha, dx, dr, a.dgate, part_w, part_s,
           sp.workers, s.waves);

@@ -237,6 +237,26 @@ def test_odd_addresses_and_in_place(gpu, dtype):
         assert torch.equal(a.dx, b.dx) and torch.equal(a.dresidual, b.dresidual) and torch.equal(a.dgate, b.dgate)
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("H", [9, 513, 1025, 1031, 2049, 4097, 5003, 8191])
+def test_odd_widths_in_place(gpu, dtype, H):  # the end of a row is read by two lanes, of two waves at some of these
+    c = _case(gpu, 700, H, dtype, gates=700)
+    for post in (None, c["post"]):
+        args = (c["weight"], 1e-6)
+        want = taot.block_norm(c["x"], c["residual"], *args, post=post, gate=c["gate"])
+        for over in ("x", "residual"):
+            v = {n: c[n].clone() for n in ("x", "residual")}
+            o = taot.block_norm(v["x"], v["residual"], *args, post=post, gate=c["gate"], out=taot.BlockNorm(h=v[over]))
+            assert torch.equal(o.h, want.h) and torch.equal(o.y, want.y)
+        kw = dict(rstd_x=want.rstd_x, post=post, gate=c["gate"])
+        a = taot.block_norm_backward(c["dy"], c["x"], want.h, want.rstd_h, c["weight"], dh=c["dh"], **kw)
+        dy, dh = c["dy"].clone(), c["dh"].clone()
+        b = taot.block_norm_backward(dy, c["x"], want.h, want.rstd_h, c["weight"], dh=dh, **kw,
+                                     out=taot.BlockNormGrad(dx=dy, dresidual=dh))
+        for f in ("dx", "dresidual", "dweight", "dgate"):
+            assert torch.equal(getattr(a, f), getattr(b, f)), f
+
+
 def test_shapes_of_gates_and_empty(gpu):
     c = _case(gpu, 24, 40, torch.float16, gates=4)
     flat = taot.block_norm(c["x"], c["residual"], c["weight"], 1e-6, post=c["post"], gate=c["gate"])
