@@ -702,8 +702,8 @@ def block_norm(x: torch.Tensor, residual: torch.Tensor, weight: Optional[torch.T
                out: Optional[BlockNorm] = None, stream=None) -> BlockNorm:
     """h = alpha * residual + gate * norm(x) * post, y = norm(h) * weight over the last dimension (taot_block_norm): x is
     a block's output, h the new residual, y the next block's input.  post None: x without a norm; gate [H], or one for
-    equal runs of rows: [gates, H] for x [T, H], else [..., H] over the first of x's dimensions; weight None: no y.  Vectors are of x's type or
-    float32.  out: tensors to write to, or an earlier call's result."""
+    equal runs of rows: [gates, H] for x [T, H], else [..., H] over the first of x's dimensions; weight None: no y.
+    Vectors are of x's type or float32.  out: tensors to write to, or an earlier call's result."""
     _rows(x, "x")
     H = x.shape[-1] if x.dim() else 0
     _shape(_rows(residual, "residual", x), "residual", x.shape)
