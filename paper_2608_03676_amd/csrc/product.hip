@@ -13,6 +13,7 @@
 //   product_some_kernel    64 rows, 32 channels   few tiles in all: waves share the inner dimension
 //   product_kernel         64 rows, 128 channels  middling runs (and 256 by 256 where rows do not
 //                                                 begin at multiples of 16 bytes)
+//   product_half_kernel    128 rows, 128 channels  runs that are too few for the next
 //   product_wide_kernel    256 rows, 256 channels  long runs: the matrix units
 // The rule is at kind_of, with both sides of each bound.
 #include "rowio.h"
@@ -419,7 +420,7 @@ product_kernel(ProductArgs p, Work work, int32_t most) {
 // lie between its 64 products, one or two at a time: a wave has its SIMD for itself, and
 // what it issues in a row the matrix unit waits for (8192 x 4096 and 8192, zeros: 2.6 to
 // 2.8 POP/s with all of them in a row, 3.6 to 4.1 so).
-// 65536 rows of 32 runs, 4096 x 4096: 1060 us, 2.08 POP/s; 8192^3 2.3 to 2.5.  Bound by
+// 65536 rows of 32 runs, 4096 x 4096: 1060 to 1110 us by the card, 2.0 POP/s; 8192^3 2.3 to 2.5.  Bound by
 // power: 8192^3 of zeros reaches 3.5, the clock falls from 2.4 to 1.75 GHz, and products
 // alone, no loads and no reads, reach 3.0 to 3.3 of random values and 4.1 to 4.7 of zeros.
 constexpr int kWideN = 256, kWideM = 256, kWideThreads = 256;
@@ -548,6 +549,114 @@ product_wide_kernel(ProductArgs p, Work work, int32_t most) {
   }
 }
 
+// The same for tiles of 128 by 128, where those of 256 are too few for the chip: a wave
+// holds 64 x 64 results, and as a step is over in a quarter of the time, four of them are
+// on their way.  The barrier waits for the step that is next alone.  512 rows, 8192 x 8192:
+// 37 us, 1.85 POP/s (58 by tiles of 64 by 128 through registers, 76 by those of 256); 128
+// rows, 4096 x 4096: 14.  A step's 16 reads of 1 KB by each of four waves, and its pieces,
+// keep LDS busy for longer than the matrix units (768 and 512 cycles), and 64 steps of
+// 8192 take 23 us however few the rows.
+constexpr int kHalfTile = 128, kHalfThreads = 256;
+constexpr int kAllButTwo = 0x4070;  // waits for LDS, and for memory but for the last 16 loads
+
+template <typename T>
+__global__ void __launch_bounds__(kHalfThreads) __attribute__((amdgpu_waves_per_eu(1, 1)))
+product_half_kernel(ProductArgs p, Work work, int32_t most) {
+  constexpr int kPieces = kStep / 16, kWaves = kHalfThreads / kWave, kRoom = 2 * kHalfTile * kPieces;
+  constexpr int kLoads = kRoom / kHalfThreads;
+  static_assert(2 * kLoads == 16, "kAllButTwo counts two steps' loads");
+  __shared__ i32x4 room0[kRoom], room1[kRoom], room2[kRoom], room3[kRoom];
+  const int tid = threadIdx.x, lane = tid % kWave, wid = __builtin_amdgcn_readfirstlane(tid / kWave);
+  const int wn = wid % 2 * 64, wm = wid / 2 * 64, turn = turn_of(lane % 32);
+  int at_n[2], at_m[2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    at_n[i] = (wn + 32 * i + lane % 32) * kPieces;
+    at_m[i] = (kHalfTile + wm + 32 * i + lane % 32) * kPieces;
+  }
+  const int own = 16 * ((lane % kPieces) ^ turn_of(wid * 8 + lane / kPieces));
+  const uint32_t first = (uint32_t)((wid * 8 + lane / kPieces) * p.K + own);
+  for (Walk walk(work, most, p.N, kHalfTile); walk.more(); walk.at += walk.step) {
+    int32_t channels;
+    const Tile t = tile_of(work, walk.place(channels), p.M, kHalfTile);
+    const int32_t n0 = channels * kHalfTile, K = t.expert < 0 ? 0 : p.K;
+    const Buffer rows_n = __builtin_amdgcn_make_buffer_rsrc(
+        const_cast<int8_t*>(p.weight) + ((int64_t)max(t.expert, 0) * p.N + n0) * p.K, 0, min(kHalfTile, p.N - n0) * p.K,
+        kRawBuffer);
+    const Buffer rows_m =
+        __builtin_amdgcn_make_buffer_rsrc(const_cast<int8_t*>(p.x) + (int64_t)t.row * p.K, 0, t.rows * p.K, kRawBuffer);
+    auto bring = [&](int32_t k, i32x4* to, int i) {
+      const uint32_t from = k + own < p.K ? first + (uint32_t)k : 0x80000000u;
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(i < kLoads / 2 ? rows_n : rows_m,
+                                               (LdsPlace*)(to + (i * kWaves + wid) * kWave), 16,
+                                               from + (uint32_t)(i % (kLoads / 2) * kWaves * 8 * p.K), 0, 0, 0);
+    };
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) bring(0, room0, i);
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) bring(kStep, room1, i);
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) bring(2 * kStep, room2, i);
+    i32x4 a[2][2], b[2][2];
+    auto take = [&](const i32x4* lds, int s, int into, int i) {
+      const int c = (2 * s + lane / 32) ^ turn;
+      if (i % 2 == 0) b[into][i / 2] = lds[at_m[i / 2] + c];
+      else a[into][i / 2] = lds[at_n[i / 2] + c];
+    };
+    i32x16 acc[2][2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int j = 0; j < 2; ++j) acc[i][j] = 0;
+    auto multiply = [&](int from, auto also) {
+#pragma unroll
+      for (int n = 0; n < 4; ++n) {
+        also(n);
+        acc[n / 2][n % 2] =
+            __builtin_amdgcn_mfma_i32_32x32x32_i8(a[from][n / 2], b[from][n % 2], acc[n / 2][n % 2], 0, 0, 0);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    };
+    // The next step's pieces are there for all waves, and nothing reads this one's any more: __syncthreads would
+    // wait for all loads.
+    auto meet = [] {
+      __atomic_signal_fence(__ATOMIC_SEQ_CST);
+      __builtin_amdgcn_s_waitcnt(kAllButTwo);
+      __builtin_amdgcn_s_barrier();
+      __atomic_signal_fence(__ATOMIC_SEQ_CST);
+    };
+    // `free`: the room of the step before, which all waves have read
+    auto step = [&](int32_t k, i32x4* here, i32x4* there, i32x4* free) {
+#pragma unroll
+      for (int s = 0; s < 3; ++s)
+        multiply(s % 2, [&](int n) {
+          take(here, s + 1, (s + 1) % 2, n);
+          if (s < 2) bring(k + 3 * kStep, free, 4 * s + n);
+        });
+      meet();
+      multiply(1, [&](int n) { take(there, 0, 0, n); });
+    };
+    meet();
+#pragma unroll
+    for (int i = 0; i < 4; ++i) take(room0, 0, 0, i);
+    int32_t k = 0;
+    for (; k + 3 * kStep < K; k += 4 * kStep) {
+      step(k, room0, room1, room3);
+      step(k + kStep, room1, room2, room0);
+      step(k + 2 * kStep, room2, room3, room1);
+      step(k + 3 * kStep, room3, room0, room2);
+    }
+    if (k < K) step(k, room0, room1, room3);
+    if (k + kStep < K) step(k + kStep, room1, room2, room0);
+    if (k + 2 * kStep < K) step(k + 2 * kStep, room2, room3, room1);
+    Results<T, 2, 2> results;
+    results.scales(p, t, n0 + wn, wm);
+    results.store(p, t, n0 + wn, wm, acc);
+    __builtin_amdgcn_s_waitcnt(kAllLoads);  // what was brought last is of no use, but on its way
+    __syncthreads();
+  }
+}
+
 // A few rows of each run: tiles of 16 rows by 16 channels, whose four waves share the
 // inner dimension.  A lane reads 32 neighbouring bytes of its row, a wave whole lines.
 // Bound by memory where the weights are many (64 rows of 64 runs, 4096 x 4096: 172 us for
@@ -624,8 +733,8 @@ product_few_kernel(ProductArgs p, Work work, int32_t most) {
 // one's are multiplied, and meet as sums in LDS, which are whole numbers and have no
 // order.  A lane reads 64 neighbouring bytes of its row, a wave whole lines of 128 of
 // each; which bytes meet in a product is the same for both operands.  Blocks of 32 rows
-// that a tile does not have are left out.  64 rows, 8192 x 8192: 33 us (67 by tiles of 64
-// by 128 that go through LDS, of which there are too few for the chip).
+// that a tile does not have are left out.  32 rows, 8192 x 8192: 19 us, 3.6 TB/s (39 by tiles
+// of 64 by 128 that go through LDS, of which there are too few for the chip).
 constexpr int kSomeN = 32, kSomeWaves = 8, kSomeThreads = kSomeWaves * kWave;
 
 template <typename T, int TM, bool SHIFT>
@@ -721,22 +830,26 @@ product_some_kernel(ProductArgs p, Work work, int32_t most) {
 }
 
 // Which kernel, by how many rows a run has on average and how many tiles there are.  Us by
-// few, some, middle and wide:
-//   K = N = 8192, one run:    16 rows  22 23 67 83       32 rows  36 25 67 84      64 rows  62 33 68 88
-//   K = N = 4096, one run:   128 rows  36 21 34 44      256 rows  64 33 27 43     512 rows 120 59 30 44
-//                           1024 rows 231 110 39 45    2048 rows 453 211 72 49
-//   K = N = 4096:         8 runs of 256 rows in all   65 54 50 59     30 of 2000  528 397 152 144
-//   K = N = 2048:       128 runs of 64 rows in all    36 52 34 39     30 of 4096  248 168  62  46
-//                        64 of 8192  465 275 98 88                    64 of 16384 917 532 159  98
-enum Kind { kFew, kSome, kMiddle, kLarge };
-Kind kind_of(int64_t M, int32_t N, int32_t runs) {
+// few, some, middle, half and wide (rows in all, runs; K = N):
+//   16    1 8192  17.0 16.1  38  23  67      32  1 8192    31 18.6  39 23.4  67      64 1 8192   59 25.9  39 23.7  67
+//   64    1 4096  17.6 14.4  21 13.9 37     128  1 4096    32 15.1  22 14.2  37     512 1 8192  190 189.7  58 37  76
+//   1024  1 8192   -   376  118  73  87    1536  1 8192   1334 562 167 107   98    2048 1 4096   -  213   60 43.9  52
+//   3000  1 4096  659  314   83  64  56    4096  1 4096   894  417 113  85   65    256  8 4096   73  55   29 27.5  46
+//   512   8 4096  137   86   37  29  47    2048  8 4096    -   248  73  62   58    1024 32 2048  75  63   27  31   35
+//   2000 30 4096   -   334  121 120 133    4096 30 2048    -   161  44  46   39    6000 64 2048 365 260   80  84   83
+//   8192 64 2048   -   333   99 103  90   16384 64 2048   932  579 163 147  121    25180 8 5120 x 256 - 234  85  69  76
+// Rows that do not begin at multiples of 16 bytes have no half, and their 256 by 256 go
+// through registers.
+enum Kind { kFew, kSome, kMiddle, kHalf, kLarge };
+Kind kind_of(int64_t M, int32_t N, int32_t runs, bool pieces) {
   const int64_t sets = runs > 0 ? runs : 1, each = M / sets;
   auto tiles = [&](int rows, int channels) { return (M / rows + sets) * ((N + channels - 1) / channels); };
   if (each <= kFewRows) return kFew;
-  if (each >= 64 && tiles(256, 256) >= 96) return kLarge;
+  if (pieces && each >= 48) return each >= 96 && tiles(256, 256) >= 176 ? kLarge : kHalf;
+  if (!pieces && each >= 64 && tiles(256, 256) >= 96) return kLarge;
   return tiles(64, 128) <= 128 ? kSome : kMiddle;
 }
-int32_t rows_of(Kind k) { return k == kFew ? kFewRows : k == kSome ? 64 : k == kMiddle ? 64 : 256; }
+int32_t rows_of(Kind k) { return k == kFew ? kFewRows : k == kSome ? 64 : k == kMiddle ? 64 : k == kHalf ? kHalfTile : 256; }
 
 // Tiles of all runs, at most.
 int64_t most_tiles(int64_t M, int32_t runs, bool listed, int32_t rows) {
@@ -746,7 +859,9 @@ int64_t most_tiles(int64_t M, int32_t runs, bool listed, int32_t rows) {
 
 template <typename T>
 taot_status product(const ProductArgs& p, void* ws, hipStream_t stream) {
-  const Kind kind = kind_of(p.M, p.N, p.runs);
+  const bool pieces =
+      p.K % 16 == 0 && reinterpret_cast<uintptr_t>(p.x) % 16 == 0 && reinterpret_cast<uintptr_t>(p.weight) % 16 == 0;
+  const Kind kind = kind_of(p.M, p.N, p.runs, pieces);
   const int32_t rows = rows_of(kind);
   const int64_t most = most_tiles(p.M, p.runs, p.offsets, rows);
   Work work{nullptr, nullptr};
@@ -773,7 +888,8 @@ taot_status product(const ProductArgs& p, void* ws, hipStream_t stream) {
     ok = go(words ? product_some_kernel<T, 2, false> : product_some_kernel<T, 2, true>, kSomeN, kSomeThreads, 0);
   else if (kind == kMiddle)
     ok = go(words ? product_kernel<T, 128, 64, 2, 2, 2, false> : product_kernel<T, 128, 64, 2, 2, 2, true>, 128, 256, 2 * (128 + 64) * kStep);
-  else if (p.K % 16 == 0 && reinterpret_cast<uintptr_t>(p.x) % 16 == 0 && reinterpret_cast<uintptr_t>(p.weight) % 16 == 0)
+  else if (kind == kHalf) ok = go(product_half_kernel<T>, kHalfTile, kHalfThreads, 0);
+  else if (pieces)
     ok = go(product_wide_kernel<T>, kWideN, kWideThreads, 0, kUnits);
   else ok = go(words ? product_kernel<T, 256, 256, 2, 4, 1, false> : product_kernel<T, 256, 256, 2, 4, 1, true>, 256, 512, 2 * (256 + 256) * kStep);
   return ok && hipGetLastError() == hipSuccess ? TAOT_OK : TAOT_ERR_LAUNCH;

@@ -177,8 +177,27 @@ def test_offsets_that_are_wrong(gpu):
         _grouped(gpu, M, 70, 100, 2, [0, 20, 10, 30, M], [0, 1, 0, 2 ** 31 - 1])
 
 
-# Tiles of 256 by 256 (from 96 of them and 64 rows a run on), with pieces straight to LDS where rows begin at multiples
-# of 16 bytes and by way of registers where they do not.
+# Where rows begin at multiples of 16 bytes, pieces go straight to LDS: tiles of 128 by 128 from 48 rows a run on, and of
+# 256 by 256 from 96 rows a run and 176 of them on.
+@pytest.mark.parametrize("K", [16, 128, 144, 256, 272, 384, 400, 512, 528, 640, 768, 896, 1024, 2064])
+def test_tiles_of_whole_pieces(gpu, K):
+    print(f"[pieces] K {K}", flush=True)
+    for M, N in ((48, 64), (128, 128), (129, 1000), (700, 300), (257, 2049), (6001, 2305)):
+        x, sx, w, sw = _operands(gpu, M, N, K)
+        for dtype in TYPES:
+            out = torch.full((M + 1, N), 7.0, dtype=dtype, device=gpu)
+            taot.matmul_i8(x, sx, w, sw, dtype=dtype, out=out[:M])
+            assert _near(out[:M], _dense(x, sx, w, sw)) and (out[M] == 7).all(), (M, N)
+            assert torch.equal(taot.matmul_i8(_shifted(x, 3), sx, _shifted(w, 5), sw, dtype=dtype), out[:M]), (M, N)
+    _grouped(gpu, 1200, 260, K, 4, [0, 0, 5, 133, 300, 555, 811, 812, 940, 1190], [0, 3, -1, 2, 2, 4, 1, 0, 3])
+    sizes = [0, 900, 1, 255, 256, 257, 512, 700, 3, 900]
+    offsets = [7]
+    for n in sizes:
+        offsets.append(offsets[-1] + n)
+    _grouped(gpu, offsets[-1] + 9, 3001, K, 3, offsets, [1, 0, 2, 1, -1, 2, 0, 3, 1, 2])
+
+
+# Tiles of 256 by 256 by way of registers (from 96 of them and 64 rows a run on) where rows begin elsewhere.
 @pytest.mark.parametrize("K", [16, 128, 144, 256, 400, 1024, 1, 17, 132, 333])
 @pytest.mark.parametrize("dtype", TYPES)
 def test_many_tiles_of_many_rows(gpu, K, dtype):
