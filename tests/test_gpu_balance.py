@@ -136,6 +136,24 @@ def test_backward(gpu, dtype, shape):
                 assert r is into and torch.equal(r, got)
 
 
+# A token's experts in two lanes (to 16), eight (to 64) or more; rows of few and of many blocks.
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("shape", [(1, 70001, 16, 2), (3, 4000, 9, 1), (2, 3001, 33, 4), (5, 2000, 64, 8), (2, 9000, 8, 2),
+                                   (9, 600, 17, 3), (32, 128, 4096, 8), (40, 70, 65, 8)])
+def test_few_experts_and_many_blocks(gpu, dtype, shape):
+    print(f"[balance] {dtype} {shape}", flush=True)
+    x, ids, mask = _case(gpu, *shape, dtype, True)
+    for flags in (0, SIGMOID):
+        b = taot.balance_loss(x, ids, mask=mask, flags=flags)
+        _check(b, x, ids, mask, flags != 0)
+        g = torch.Generator(device=gpu).manual_seed(3)
+        dloss, dz = (torch.randn(shape[0], device=gpu, generator=g) for _ in range(2))
+        add = torch.randn(x.shape, device=gpu, generator=g).to(dtype)
+        dz = None if flags else dz
+        got = taot.balance_loss_backward(dloss, x, b.counts, b.tokens, mask=mask, dz=dz, add=add, flags=flags)
+        _grad_check(got, x, ids, b.counts, b.tokens, mask, dloss, dz, add, flags != 0)
+
+
 @pytest.mark.parametrize("flags", [0, SIGMOID])
 def test_against_differences(gpu, flags):
     """The loss's directional derivative in 64 bits by central differences (error about 1e-9 here)."""
