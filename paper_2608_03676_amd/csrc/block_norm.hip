@@ -35,8 +35,10 @@ __device__ __forceinline__ f32x8 factor(const Vector& v, int64_t col, int n) {
 enum Edge { kWholeRows, kOddRows, kAnyRows };  // H % 8 == 0; other H from 8 on; any H, with single loads
 template <Edge EDGE>
 struct Place {
-  int col, n, back;  // first column, how many (8 or 0, kAnyRows: up to the row's end), how many the lane before has too
-  __device__ __forceinline__ Place(int chunk, int32_t H) : col(8 * chunk), n(EDGE == kAnyRows ? H - col : col < H ? 8 : 0), back(0) {
+  // first column, how many (8 or 0, kAnyRows: up to the row's end), how many of them the lane before has too
+  int col, n, back;
+  __device__ __forceinline__ Place(int chunk, int32_t H)
+      : col(8 * chunk), n(EDGE == kAnyRows ? H - col : col < H ? 8 : 0), back(0) {
     if (EDGE == kOddRows && n && H - col < 8) {
       back = 8 - (H - col);
       col -= back;
@@ -263,9 +265,9 @@ block_norm_backward_kernel(const T* dy, const T* dh, const T* x, const T* h, con
 }
 
 // The same for rows wider than the registers hold beside the sums (more than 8192
-// columns), and for those of less than eight: the 16 waves read a row's inputs three times, the later ones out of the
-// L2 cache, and keep their sums in memory, each lane its own columns.  A gate that a
-// worker has alone is summed where its gradient goes.
+// columns), and for those of less than eight: the 16 waves read a row's inputs three
+// times, the later ones out of the L2 cache, and keep their sums in memory, each lane its
+// own columns.  A gate that a worker has alone is summed where its gradient goes.
 template <typename T, bool FAR, bool MANY>
 __global__ void __launch_bounds__(1024)
 block_norm_backward_wide_kernel(const T* dy, const T* dh, const T* x, const T* h, const float* __restrict__ rstd_x,
