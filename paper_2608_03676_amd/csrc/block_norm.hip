@@ -176,8 +176,9 @@ __device__ __forceinline__ Three row_sums(Three v, f32x4 (*part)[16], int slot, 
 // the present one is worked on.  dresidual and dx may lie in an input's memory: a row
 // is read by its worker alone, and all of it before any of it is written.
 //
-// With q = gate post, e = b dy w + dh and c = b^2 mean(dy w h) it is D = e - b c h, so
-// sum(D q x) = sum(e q x) - b c sum(h q x): all sums of a row are taken at once (8192 x 5120
+// With H = b h, X = a x, q = gate post, e = b dy w + dh and c = b mean(dy w H) it is
+// D = e - c H, so sum(D q X) = sum(e q X) - c sum(H q X): all sums of a row are taken at
+// once, of normed rows, for powers of b and a leave 32 bits where D and dx do not (8192 x 5120
 // bfloat16, dh, post, 4 gates: 136 us with a sum after the other, 109 so and with as many
 // workers as are resident).  102 us for 503 MB, 4.9 TB/s, and 6 for the workers' sums: of
 // the 16 waves whose registers a compute unit holds, a row of 5120 fills ten.
@@ -218,14 +219,14 @@ block_norm_backward_kernel(const T* dy, const T* dh, const T* x, const T* h, con
     if (kAhead) fetch(then, nx, nh, ny, nd);
     else fetch(rows.row, rx, rh, ry, rd);
     const float next_a = post.p ? rstd_x[then] : 1.f, next_b = weight.p ? rstd_h[then] : 0.f;
-    const f32x8 Y = widen(ry), Hh = widen(rh), X = widen(rx);
+    const f32x8 Y = widen(ry), Hh = widen(rh) * b, X = widen(rx) * a;
     f32x8 e = widen(rd);
     Three s = {0.f, 0.f, 0.f};
 #pragma unroll
     for (int u = 0; u < 8; ++u) {
       const float v = Y[u] * w[u], qx = q[u] * X[u];
       e[u] = fmaf(b, v, e[u]);
-      dw[u] = fmaf(Y[u], Hh[u] * b, dw[u]);
+      dw[u] = fmaf(Y[u], Hh[u], dw[u]);
       const bool mine = place.adds(u);
       s.a = mine ? fmaf(v, Hh[u], s.a) : s.a;
       s.b = mine ? fmaf(e[u], qx, s.b) : s.b;
@@ -233,12 +234,12 @@ block_norm_backward_kernel(const T* dy, const T* dh, const T* x, const T* h, con
     }
     s = row_sums(s, part, slot, waves);
     slot ^= 1;
-    const float bc = b * b * b * (s.a / (float)H), m = a * a * (fmaf(-bc, s.c, s.b) / (float)H);
+    const float c = b * (s.a / (float)H), m = fmaf(-c, s.c, s.b) / (float)H;
     f32x8 D, t;
 #pragma unroll
     for (int u = 0; u < 8; ++u) {
-      D[u] = fmaf(-bc, Hh[u], e[u]);
-      S[u] = fmaf(D[u], X[u] * a, S[u]);
+      D[u] = fmaf(-c, Hh[u], e[u]);
+      S[u] = fmaf(D[u], X[u], S[u]);
       t[u] = D[u] * q[u];
       if (post.p) t[u] = a * fmaf(-m, X[u], t[u]);
     }
@@ -292,14 +293,14 @@ block_norm_backward_wide_kernel(const T* dy, const T* dh, const T* x, const T* h
     if (weight.p) {
       for (int col = 8 * (int)threadIdx.x; col < H; col += 8 * kWaves * kWave) {
         const int n = H - col;
-        const f32x8 w = factor<T>(weight, col, n), Y = load_row(dy + at + col, n), Hh = load_row(h + at + col, n);
+        const f32x8 w = factor<T>(weight, col, n), Y = load_row(dy + at + col, n), Hh = load_row(h + at + col, n) * b;
 #pragma unroll
         for (int u = 0; u < 8; ++u) dot = fmaf(Y[u] * w[u], Hh[u], dot);
       }
       dot = row_reduce(dot, SumOp(), part, slot, kWaves) / (float)H;
       slot ^= 1;
     }
-    const float c = b * b * dot;
+    const float c = b * dot;
     auto D_of = [&](int col, int n) {
       f32x8 D = 0.f;
       if (weight.p) D = b * (load_row(dy + at + col, n) * factor<T>(weight, col, n) - load_row(h + at + col, n) * c);
@@ -312,24 +313,24 @@ block_norm_backward_wide_kernel(const T* dy, const T* dh, const T* x, const T* h
       for (int col = 8 * (int)threadIdx.x; col < H; col += 8 * kWaves * kWave) {
         const int n = H - col;
         const f32x8 t = D_of(col, n) * factor<T>(gate, gate_at + col, n) * factor<T>(post, col, n);
-        const f32x8 X = load_row(x + at + col, n);
+        const f32x8 X = load_row(x + at + col, n) * a;
 #pragma unroll
         for (int u = 0; u < 8; ++u) dot = fmaf(t[u], X[u], dot);
       }
-      m = a * a * (row_reduce(dot, SumOp(), part, slot, kWaves) / (float)H);
+      m = row_reduce(dot, SumOp(), part, slot, kWaves) / (float)H;
       slot ^= 1;
     }
     for (int col = 8 * (int)threadIdx.x; col < H; col += 8 * kWaves * kWave) {
       const int n = H - col;
       const f32x8 D = D_of(col, n), g = factor<T>(gate, gate_at + col, n), p = factor<T>(post, col, n);
       f32x8 X = 0.f;
-      if (sums) X = load_row(x + at + col, n);
+      if (sums) X = load_row(x + at + col, n) * a;
       if (part_w) add(part_w + (int64_t)worker * H + col, load_row(dy + at + col, n) * load_row(h + at + col, n) * b, n, first);
       if (MANY) {
-        if (dgate) add(dgate + gate_at + col, D * X * a * p, n, rows.in_seg == 0);
-        if (part_s) add(part_s + (int64_t)worker * H + col, D * X * a * g, n, first);
+        if (dgate) add(dgate + gate_at + col, D * X * p, n, rows.in_seg == 0);
+        if (part_s) add(part_s + (int64_t)worker * H + col, D * X * g, n, first);
       } else if (part_s) {
-        add(part_s + (int64_t)worker * H + col, D * X * a, n, first);
+        add(part_s + (int64_t)worker * H + col, D * X, n, first);
       }
       f32x8 t = D * g;
       if (post.p) t = a * (t * p - X * m);
