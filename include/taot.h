@@ -459,7 +459,9 @@ taot_status taot_balance_loss(const void* logits, const int32_t* ids, const uint
  *   dloss [rows], dz [rows] float (nullable; null with SIGMOID); counts, counted as given
  *   add      [rows][tokens][E] dtype, nullable: what reaches the logits otherwise
  * Output: dlogits [rows][tokens][E] dtype, add alone for tokens of mask 0 (it may be the
- * logits' or add's own storage, with the same pointer). */
+ * logits' or add's own storage, with the same pointer).  A dloss or dz that is NaN or
+ * infinite makes its row's gradients so, as the formula has it (0 times it is NaN);
+ * 2 dz / n lse of a finite dz is held within the finite floats. */
 taot_status taot_balance_loss_backward(const float* dloss, const float* dz, const void* logits, const int32_t* counts,
                                        const int32_t* counted, const uint8_t* mask, const void* add, int64_t rows,
                                        int64_t tokens, int32_t E, uint32_t flags, int32_t dtype, void* dlogits,

@@ -387,8 +387,10 @@ balance_backward_kernel(const float* __restrict__ dloss, const float* __restrict
       for (int u = 0; u < 8; ++u) dot = fmaf(c[u], v[i][u], dot);
     }
     dot = g.reduce(dot, SumOp()) * inv * f;
-    // finite, so that experts of p = 0 get 0
-    const float up = SIGMOID ? dot : dot - within(fz * lse, -FLT_MAX, FLT_MAX), each_p = now ? inv : 0.f;
+    // A finite dz has a finite term, also where lse is the largest float: experts of p = 0 get 0.  A dz that is not
+    // finite has none, so that who looks for it in the gradient finds it.
+    const float zl = fz * lse, term = fabsf(fz) <= FLT_MAX ? within(zl, -FLT_MAX, FLT_MAX) : zl;
+    const float up = SIGMOID ? dot : dot - term, each_p = now ? inv : 0.f;
 #pragma unroll
     for (int i = 0; i < CPL; ++i) {
       const int col = 8 * (i * g.lanes + g.lane), m = t >= hi ? 0 : FULL ? 8 : s.E - col;
