@@ -361,11 +361,11 @@ balance_backward_kernel(const float* __restrict__ dloss, const float* __restrict
   }
   all = block_reduce<kWave>(all, SumOp());
   if (tid % kWave == 0) alls[tid / kWave] = all;
-  const float n = (float)max(counted[row], 1), fz = dz ? 2.f * dz[row] / n : 0.f, fl = dloss[row];
+  const float n = (float)max(counted[row], 1), fz = dz ? 2.f * (dz[row] / n) : 0.f, fl = dloss[row];
   __syncthreads();
   all = 0.f;
   for (int w = 0; w < waves; ++w) all += alls[w];
-  const float f = fl * (float)s.E / (fmaxf(all, 1.f) * n);
+  const float f = fl * ((float)s.E / (fmaxf(all, 1.f) * n));  // fl E may be no float where f is one
   for (int64_t j = 0; j < turns; ++j) {
     const int64_t t = first + j * step, at = row * s.tokens + t;
     f32x8 v[CPL];

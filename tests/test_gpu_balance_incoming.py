@@ -1,10 +1,10 @@
 """Gradients that reach balance_loss from outside its usual range.  One that is not finite has to be seen in what leaves:
-the step that it belongs to is not to be taken."""
+the step that it belongs to is not to be taken.  A large one whose results are finite may not leave 32 bits on the way."""
 import pytest
 import torch
 
 import paper_2608_03676_amd as taot
-from test_gpu_balance import E, SIGMOID, TYPES, _case, _scores
+from test_gpu_balance import E, SIGMOID, TYPES, _case, _grad_check, _scores
 
 pytestmark = pytest.mark.gpu
 NAN, INF = float("nan"), float("inf")
@@ -68,3 +68,17 @@ def test_a_logit_of_infinity_with_a_finite_dz(gpu):
         assert abs(float(got[0, 9, 4]) / (0.3 * top) - 1) < 16 * E and got[1, 7, 5] == -top  # 50 times the largest float
         for r, t in ((0, 9), (1, 7)):
             assert (got[r, t] != 0).sum() == 1
+
+
+@pytest.mark.parametrize("flags", [0, SIGMOID])
+@pytest.mark.parametrize("experts,size", [(16, 3e37), (160, 5e36), (600, 3e36), (4096, 3e36)])
+def test_large_incoming_gradients(gpu, experts, size, flags):
+    """dloss E is no float, dloss E / n is; 2 dz is none, 2 dz / n is."""
+    x, ids, _ = _case(gpu, 3, 64, experts, 8, torch.float32)
+    x *= 0.3
+    b = taot.balance_loss(x, ids, flags=flags)
+    dloss = torch.tensor([size, -size, 1.0], device=gpu)
+    dz = None if flags else torch.tensor([2e38, -2e38, 1.0], device=gpu)
+    got = taot.balance_loss_backward(dloss, x, b.counts, b.tokens, dz=dz, flags=flags)
+    assert torch.isfinite(got).all()
+    _grad_check(got, x, ids, b.counts.double(), b.tokens.double(), None, dloss, dz, None, flags != 0)
