@@ -18,7 +18,9 @@
  *     `status` array (TAOT_ST_*), which the caller reads after synchronising;
  *     device code never aborts.
  *   - Workspace: pass at least taot_*_workspace_size(...) bytes, 256-byte
- *     aligned (hipMalloc and torch allocations are).
+ *     aligned (hipMalloc and torch allocations are).  taot_block_norm_backward,
+ *     taot_balance_loss and taot_matmul_i8 refuse one that does not begin at a
+ *     multiple of 8 bytes (TAOT_ERR_WORKSPACE).
  */
 #ifndef TAOT_H
 #define TAOT_H

@@ -19,6 +19,11 @@ bool bad_weight_type(int32_t dtype, int32_t weight_dtype) {
 // A gate's rows: `gates` of them divide the T rows.
 bool bad_gates(const void* gate, int64_t gates, int64_t T) { return gate && (gates < 1 || T % gates); }
 
+// A workspace that is missing, too small, or begins where the kernels' atomics and scalar loads of its words may not.
+bool bad_room(const void* ws, size_t bytes, size_t needed) {
+  return !ws || bytes < needed || reinterpret_cast<uintptr_t>(ws) % 8;
+}
+
 constexpr int64_t kMaxGrid = 0x7fffffffLL;  // rows that one launch can number
 constexpr int32_t kMaxWide = 1 << 30;       // columns whose steps 32 bits can count
 
@@ -299,7 +304,7 @@ taot_status taot_block_norm_backward(const void* dy, const void* dh, const void*
   if (T > 0 && (!x || !dx || !dresidual || (weight && (!dy || !h || !rstd_h)) || (!weight && !dh) || (post && !rstd_x)))
     return TAOT_ERR_INVALID_ARG;
   const int64_t sets = gate ? gates : 1;
-  if (T > 0 && (!ws || ws_bytes < block_norm_backward_ws(T, H, sets))) return TAOT_ERR_WORKSPACE;
+  if (T > 0 && bad_room(ws, ws_bytes, block_norm_backward_ws(T, H, sets))) return TAOT_ERR_WORKSPACE;
   return launch_block_norm_backward(
       BlockNormGradArgs{dy, dh, x, h, rstd_x, rstd_h, post, gate, weight, T, sets, H, weight_dtype == TAOT_F32,
                         gate_dtype == TAOT_F32, alpha, dx, dresidual, dweight, dpost, dgate},
@@ -321,7 +326,7 @@ taot_status taot_balance_loss(const void* logits, const int32_t* ids, const uint
   if (E > TAOT_MAX_EXPERTS || rows > kMaxGrid || (n > 0 && rows > kMaxGrid / n)) return TAOT_ERR_UNSUPPORTED;
   if (rows == 0) return TAOT_OK;
   if ((tokens > 0 && (!logits || !ids)) || !loss || !counts || !prob) return TAOT_ERR_INVALID_ARG;
-  if (!ws || ws_bytes < balance_loss_ws(rows, tokens, E)) return TAOT_ERR_WORKSPACE;
+  if (bad_room(ws, ws_bytes, balance_loss_ws(rows, tokens, E))) return TAOT_ERR_WORKSPACE;
   return launch_balance_loss(logits, ids, mask, rows, tokens, E, k, flags, dtype, loss, z, counts, prob, counted, ws,
                              static_cast<hipStream_t>(stream));
 }
@@ -363,7 +368,7 @@ taot_status taot_matmul_i8(const int8_t* x, const float* scale, const int8_t* we
   if (K > TAOT_MAX_INNER || M > kMaxWide || N > kMaxWide || runs > kMaxWide) return TAOT_ERR_UNSUPPORTED;
   if (M == 0) return TAOT_OK;
   if (!x || !scale || !weight || !weight_scale || !out) return TAOT_ERR_INVALID_ARG;
-  if (offsets && (!ws || ws_bytes < matmul_i8_ws(M, runs))) return TAOT_ERR_WORKSPACE;
+  if (offsets && bad_room(ws, ws_bytes, matmul_i8_ws(M, runs))) return TAOT_ERR_WORKSPACE;
   return launch_matmul_i8(ProductArgs{x, scale, weight, weight_scale, offsets, experts, M, N, K, runs, G, out}, dtype, ws,
                           static_cast<hipStream_t>(stream));
 }
