@@ -411,6 +411,7 @@ taot_status taot_combine_rows_backward(const void* dout, const void* y, const in
  *   h        [T][H] dtype    rounded where it is stored only
  *   y        [T][H] dtype
  *   rstd_x, rstd_h [T] float  a and b, for the gradient (written with post and weight)
+ * Squares are summed in 32 bits: where their sum is no float, a or b is 0.
  * x and residual may be h or y's own storage only if the pointers are equal.
  * Limits: 1 <= H <= TAOT_MAX_WIDTH, 0 <= T <= 2^31 - 1. */
 taot_status taot_block_norm(const void* x, const void* residual, const void* post, const void* gate, int64_t gates,
@@ -473,14 +474,15 @@ taot_status taot_balance_loss_backward(const float* dloss, const float* dz, cons
  *   v = x, or gated: silu(g) * u of a row [g | u];  a = max_c |v|, of at least 1e-30
  *   q = v * (127 / a) to the nearest integer (even of two);  scale = a / 127
  *   x        [T][H] dtype, gated [T][2 H]
- * Outputs: q [T][H] int8, scale [T] float.  A row that holds NaN or an infinity has
- * scale NaN and q = 0, so that what is made of it is NaN.
+ * Outputs: q [T][H] int8, scale [T] float.  A row that holds NaN or an infinity, or
+ * whose product silu(g) * u is one, has scale NaN and q = 0, so that what is made of
+ * it is NaN.
  * Limits: 1 <= H <= TAOT_MAX_WIDTH, 0 <= T <= 2^31 - 1. */
 taot_status taot_quantize_rows(const void* x, int64_t T, int32_t H, int32_t gated, int32_t dtype, int8_t* q,
                                float* scale, void* stream);
 /* Products of such rows with 8-bit weights that have a scale for each channel:
  *   out[t][n] = scale[t] * weight_scale[e][n] * sum_k x[t][k] * weight[e][n][k]
- * with the sum exact and the product rounded once.
+ * with the sum exact, rounded to a float, multiplied by the scales in 32 bits and rounded to dtype.
  *   x        [M][K] int8, scale [M] float;  weight [G][N][K] int8, weight_scale [G][N] float
  *   offsets  [runs + 1] int32: run i has rows offsets[i] .. offsets[i + 1] - 1 (as
  *            taot_dispatch_map's instances have); offsets are taken within [0, M], each as at

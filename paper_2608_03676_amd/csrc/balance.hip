@@ -59,7 +59,8 @@ __device__ __forceinline__ void scores(Group<L>& g, int32_t E, f32x8 (&v)[CPL], 
     for (int i = 0; i < CPL; ++i)
 #pragma unroll
       for (int u = 0; u < 8; ++u) {
-        // below -87 the sigmoid is not a normal number, and 0 here; so is that of NaN
+        // below -87 the sigmoid is not a normal number, and 0 here; so is that of NaN.  The hardware's reciprocal is
+        // off by a unit in the last place, as the exponential is
         const float x = v[i][u], s = __builtin_amdgcn_rcpf(1.f + exponential(within(-x, -150.f, 88.f)));
         v[i][u] = x >= -87.f ? s : 0.f;
         total += v[i][u];

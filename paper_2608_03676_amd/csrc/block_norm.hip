@@ -179,8 +179,8 @@ __device__ __forceinline__ Three row_sums(Three v, f32x4 (*part)[16], int slot, 
 // With H = b h, X = a x, q = gate post, e = b dy w + dh and c = b mean(dy w H) it is
 // D = e - c H, so sum(D q X) = sum(e q X) - c sum(H q X): all sums of a row are taken at
 // once, of normed rows, for powers of b and a leave 32 bits where D and dx do not (8192 x 5120
-// bfloat16, dh, post, 4 gates: 136 us with a sum after the other, 109 so and with as many
-// workers as are resident).  102 us for 503 MB, 4.9 TB/s, and 6 for the workers' sums: of
+// bfloat16, dh, post, 4 gates: 136 us with a sum after the other, 108 so and with as many
+// workers as are resident).  101 us for 503 MB, 5.0 TB/s, and 6 for the workers' sums: of
 // the 16 waves whose registers a compute unit holds, a row of 5120 fills ten.
 template <typename T, bool FAR, bool MANY, Edge EDGE>
 __global__ void __launch_bounds__(1024)
@@ -268,7 +268,9 @@ block_norm_backward_kernel(const T* dy, const T* dh, const T* x, const T* h, con
 // The same for rows wider than the registers hold beside the sums (more than 8192
 // columns), and for those of less than eight: the 16 waves read a row's inputs three
 // times, the later ones out of the L2 cache, and keep their sums in memory, each lane its
-// own columns.  A gate that a worker has alone is summed where its gradient goes.
+// own columns.  A gate that a worker has alone is summed where its gradient goes.  4096 x
+// 8200 bfloat16, dh, post, a gate: 277 us for 403 MB (8192 columns 87), 2048 x 16384 234; the
+// sums in memory are another 16 bytes a column, read and written, and issue is 72.
 template <typename T, bool FAR, bool MANY>
 __global__ void __launch_bounds__(1024)
 block_norm_backward_wide_kernel(const T* dy, const T* dh, const T* x, const T* h, const float* __restrict__ rstd_x,

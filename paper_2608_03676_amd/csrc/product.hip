@@ -4,7 +4,7 @@
 //   out[t][n] = scale[t] weight_scale[e][n] sum_k x[t][k] weight[e][n][k]
 //
 // The sum is of whole numbers and exact in 32 bits (K up to TAOT_MAX_INNER); it is
-// rounded to a float, multiplied by the two scales and rounded once to the output's
+// rounded to a float, multiplied by the two scales in 32 bits and rounded to the output's
 // type.  The order of the sum does not matter, so waves and blocks may share it.
 //
 // runs_kernel lists the tiles of rows: a tile lies within one run.  The weights are
@@ -706,7 +706,7 @@ product_few_kernel(ProductArgs p, Work work, int32_t most) {
         k += kAll;
       }
     }
-    if (k < K) {  // the row's end: one wave has it
+    if (k < K) {  // the row's end: of one wave, or of two where words are shifted and it is 1 to 3 bytes
       const int left = K - k - mine;
       a[0].load_end(w + k + mine, shift_w, left);
       b[0].load_end(x + k + mine, shift_x, left);
@@ -794,7 +794,7 @@ product_some_kernel(ProductArgs p, Work work, int32_t most) {
 #pragma unroll
       for (int j = 0; j < TM; ++j) b[j] = next_b[j];
     }
-    if (k < K) {  // the row's end: one wave has it
+    if (k < K) {  // the row's end: of one wave, or of two where words are shifted and it is 1 to 3 bytes
       const int left = K - k - mine;
       a.load_end(w + k + mine, shift_w, left);
 #pragma unroll
@@ -840,6 +840,13 @@ product_some_kernel(ProductArgs p, Work work, int32_t most) {
 //   8192 64 2048   -   333   99 103  90   16384 64 2048   932  579 163 147  121    25180 8 5120 x 256 - 234  85  69  76
 // Rows that do not begin at multiples of 16 bytes have no half, and their 256 by 256 go
 // through registers.
+// The average is all that the host knows: the runs' own lengths live on the GPU, and rows of
+// no run count too.  Where one run has nearly all rows and the average says few, its weight is
+// read for each 16 of them (us, even split; one run has all but a row a run; one has all, the
+// others none; a product of one weight): 4096 rows of 256 runs, 2048 x 2048 260 449 241 25;
+// 1024 of 64, 4096 x 4096 255 443 232 22.  From 48 rows a run on: 4096 of 64, 2048 x 2048
+// 61 82 - 26, 8192 of 64 85 - 40 36, 16384 of 64 100 136; and where all but a 32nd of the rows
+// are of no run, 16384 of 64 take 130, 32768 191 (even 176).
 enum Kind { kFew, kSome, kMiddle, kHalf, kLarge };
 Kind kind_of(int64_t M, int32_t N, int32_t runs, bool pieces) {
   const int64_t sets = runs > 0 ? runs : 1, each = M / sets;
